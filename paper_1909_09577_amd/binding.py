@@ -20,6 +20,9 @@ NM_STATIC_SCRATCH_BYTES = 32 << 20
 NM_BF16, NM_F32 = 0, 1
 NM_RELU, NM_ACCUM_DW, NM_FORCE_DIRECT, NM_ACCUM_DX = 1, 2, 4, 8
 NM_OP_FWD, NM_OP_BWD_DATA, NM_OP_BWD_WEIGHT, NM_OP_BWD, NM_OP_BN_FWD, NM_OP_BN_BWD = 0, 1, 2, 3, 4, 5
+NM_OP_ATTN_FWD, NM_OP_ATTN_BWD = 16, 17
+NM_NORM_POST, NM_NORM_NEXT, NM_NORM_LAYER = 1, 2, 4
+NM_GATE_NONE, NM_GATE_ITEM, NM_GATE_ELEMENT = 0, 1, 2
 
 EXPORTS = ("nm_conv1d_out_len", "nm_conv1d_workspace_bytes", "nm_strerror", "nm_conv1d_block_fwd",
            "nm_conv1d_bwd_data", "nm_conv1d_bwd_weight", "nm_conv1d_bwd", "nm_conv1d_block_fwd_masked", "nm_conv1d_bwd_data_masked",
@@ -28,9 +31,19 @@ EXPORTS = ("nm_conv1d_out_len", "nm_conv1d_workspace_bytes", "nm_strerror", "nm_
            "nm_fp8_row_scales", "nm_fp8_quantize_rows", "nm_conv1d_fp8_supported", "nm_conv1d_fp8_workspace_bytes",
            "nm_conv1d_block_fwd_fp8", "nm_conv1d_bwd_data_fp8", "nm_conv1d_fp8_bwd_data_workspace_bytes",
            "nm_fp8_dgrad_weight_scales", "nm_conv1d_bwd_weight_fp8", "nm_conv1d_fp8_bwd_weight_workspace_bytes",
-           "nm_conv1d_bwd_fp8", "nm_conv1d_fp8_bwd_workspace_bytes")
+           "nm_conv1d_bwd_fp8", "nm_conv1d_fp8_bwd_workspace_bytes",
+           "nm_cross_attn_workspace_bytes", "nm_cross_attn_fwd", "nm_cross_attn_bwd",
+           "nm_residual_norm_fwd", "nm_residual_norm_bwd", "nm_residual_norm_bwd_workspace_bytes",
+           "nm_adamw_plan_bytes", "nm_adamw_plan", "nm_adamw_step")
 
 _lib = None
+
+
+class AdamWTensor(ctypes.Structure):
+    """nm_adamw_tensor of include/nm_adamw.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_longlong),
+                ("weight_decay", ctypes.c_float)]
 
 
 class NmError(RuntimeError):
@@ -108,6 +121,25 @@ def lib() -> ctypes.CDLL:
         L.nm_conv1d_bwd_fp8.restype = i
         L.nm_conv1d_fp8_bwd_workspace_bytes.argtypes = [i] * 8
         L.nm_conv1d_fp8_bwd_workspace_bytes.restype = sz
+        ll, f, d = ctypes.c_longlong, ctypes.c_float, ctypes.c_double
+        L.nm_cross_attn_workspace_bytes.argtypes = [i] * 8
+        L.nm_cross_attn_workspace_bytes.restype = sz
+        L.nm_cross_attn_fwd.argtypes = [i] * 6 + [vp, ll] * 3 + [vp] * 3 + [f, vp, ll, vp, i, vp, sz, vp]
+        L.nm_cross_attn_fwd.restype = i
+        L.nm_cross_attn_bwd.argtypes = [i] * 6 + [vp, ll] * 5 + [vp] * 4 + [f] + [vp, ll] * 3 + [i, vp, sz, vp]
+        L.nm_cross_attn_bwd.restype = i
+        L.nm_residual_norm_fwd.argtypes = [i] * 3 + [vp] * 3 + [i] + [vp] * 5 + [f] + [vp] * 3 + [u, i, vp]
+        L.nm_residual_norm_fwd.restype = i
+        L.nm_residual_norm_bwd_workspace_bytes.argtypes = [i] * 4
+        L.nm_residual_norm_bwd_workspace_bytes.restype = sz
+        L.nm_residual_norm_bwd.argtypes = [i] * 3 + [vp] * 5 + [i] + [vp] * 4 + [f] + [vp] * 9 + [u, i, vp, sz, vp]
+        L.nm_residual_norm_bwd.restype = i
+        L.nm_adamw_plan_bytes.argtypes = [ctypes.POINTER(AdamWTensor), i, i]
+        L.nm_adamw_plan_bytes.restype = sz
+        L.nm_adamw_plan.argtypes = [ctypes.POINTER(AdamWTensor), i, i, vp, sz]
+        L.nm_adamw_plan.restype = i
+        L.nm_adamw_step.argtypes = [vp, vp, sz, d, d, d, d, ll, vp, u, vp]
+        L.nm_adamw_step.restype = i
         _lib = L
     return _lib
 
@@ -599,3 +631,234 @@ def nm_conv1d_bwd_fp8(x, x_scale, dy, g_scale, w, wt_scales, y=None, scale=None,
     if st != NM_OK:
         raise NmError(st, "nm_conv1d_bwd_fp8")
     return dx, dres, dw
+
+
+# ---- cross attention (include/nm_attention.h) ---------------------------------------------------
+def _item_ptr(t, dtype, shape, name):
+    """(pointer, distance of the batch items) of a tensor whose items are dense."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    B, C, N = shape
+    if t.is_contiguous():
+        return t.data_ptr(), C * N
+    step, rows, cols = t.stride()
+    if (N > 1 and cols != 1) or (C > 1 and rows != N):
+        raise ValueError(f"{name} must have dense items [channels][positions]")
+    if B == 1:
+        step = C * N
+    if step < C * N:
+        raise ValueError(f"the items of {name} must not overlap")
+    return t.data_ptr(), step
+
+
+def nm_cross_attn_workspace_bytes(op: int, B, heads, kv_heads, D, U, T, dtype=NM_BF16) -> int:
+    return int(lib().nm_cross_attn_workspace_bytes(op, B, heads, kv_heads, D, U, T, dtype))
+
+
+def _attn_dims(q, k, heads, kv_heads, where):
+    kv_heads = heads if kv_heads is None else kv_heads
+    if q.dim() != 3 or k.dim() != 3 or heads <= 0 or kv_heads <= 0 or q.shape[1] % heads:
+        raise NmError(NM_ERR_BAD_ARG, where)
+    B, HD, U = q.shape
+    return B, heads, kv_heads, HD // heads, U, k.shape[2]
+
+
+def _attn_workspace(op, dims, code, workspace, like):
+    if workspace is None:
+        need = nm_cross_attn_workspace_bytes(op, *dims, code)
+        if not need:
+            return None, None, 0
+        workspace = like.new_empty(need, dtype=_torch().uint8)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def nm_cross_attn_fwd(q, k, v, *, heads, kv_heads=None, scale=None, lengths=None, q_lengths=None, windows=None, o=None,
+                      lse=None, want_lse=False, workspace=None, stream=None):
+    """Attention of the tokens q [B, heads*D, U] to the states k, v [B, kv_heads*D, T]; returns (o, lse), lse None unless given
+    or wanted.  scale: 1/sqrt(D) if None.  lengths, q_lengths int32 [B]: valid states and tokens of every item; windows int32
+    [B, U, 2]: first state and end of the states that a token looks at."""
+    torch = _torch()
+    dims = B, H, Hkv, D, U, T = _attn_dims(q, k, heads, kv_heads, "nm_cross_attn_fwd")
+    code = _dtype_code(q)
+    qp, qs = _item_ptr(q, q.dtype, (B, H * D, U), "q")
+    kp, ks = _item_ptr(k, q.dtype, (B, Hkv * D, T), "k")
+    vp, vs = _item_ptr(v, q.dtype, (B, Hkv * D, T), "v")
+    if o is None:
+        o = q.new_empty((B, H * D, U))
+    op, os_ = _item_ptr(o, q.dtype, (B, H * D, U), "o")
+    if lse is None and want_lse:
+        lse = q.new_empty((B, H, U), dtype=torch.float32)
+    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_FWD, dims, code, workspace, q)
+    st = lib().nm_cross_attn_fwd(
+        *dims, qp, qs, kp, ks, vp, vs, _ptr(lengths, torch.int32, (B,), "lengths"),
+        _ptr(q_lengths, torch.int32, (B,), "q_lengths"), _ptr(windows, torch.int32, (B, U, 2), "windows"),
+        D ** -0.5 if scale is None else scale, op, os_, _ptr(lse, torch.float32, (B, H, U), "lse"), code, ws_ptr, ws_bytes,
+        _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_cross_attn_fwd")
+    return o, lse
+
+
+def nm_cross_attn_bwd(do, q, k, v, o, lse, *, heads, kv_heads=None, scale=None, lengths=None, q_lengths=None, windows=None,
+                      dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dv) from the gradient do of o; o, lse and the other arguments as of the forward call."""
+    torch = _torch()
+    dims = B, H, Hkv, D, U, T = _attn_dims(q, k, heads, kv_heads, "nm_cross_attn_bwd")
+    code = _dtype_code(q)
+    q_shape, kv_shape = (B, H * D, U), (B, Hkv * D, T)
+    dq = q.new_empty(q_shape) if dq is None else dq
+    dk = q.new_empty(kv_shape) if dk is None else dk
+    dv = q.new_empty(kv_shape) if dv is None else dv
+    ins = [a for t, shape, name in ((do, q_shape, "do"), (q, q_shape, "q"), (k, kv_shape, "k"), (v, kv_shape, "v"), (o, q_shape, "o"))
+           for a in _item_ptr(t, q.dtype, shape, name)]
+    outs = [a for t, shape, name in ((dq, q_shape, "dq"), (dk, kv_shape, "dk"), (dv, kv_shape, "dv"))
+            for a in _item_ptr(t, q.dtype, shape, name)]
+    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_BWD, dims, code, workspace, q)
+    st = lib().nm_cross_attn_bwd(
+        *dims, *ins, _ptr(lse, torch.float32, (B, H, U), "lse"), _ptr(lengths, torch.int32, (B,), "lengths"),
+        _ptr(q_lengths, torch.int32, (B,), "q_lengths"), _ptr(windows, torch.int32, (B, U, 2), "windows"),
+        D ** -0.5 if scale is None else scale, *outs, code, ws_ptr, ws_bytes, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_cross_attn_bwd")
+    return dq, dk, dv
+
+
+# ---- norms around a block (include/nm_norm.h) ---------------------------------------------------
+def _gate_kind(gate, like, name="gate"):
+    """(kind, pointer) of a gate: None, [B, C] float32 or [B, C, T] in the storage dtype."""
+    B, C, T = like.shape
+    if gate is None:
+        return NM_GATE_NONE, None
+    if gate.dim() == 2:
+        return NM_GATE_ITEM, _ptr(gate, _torch().float32, (B, C), name)
+    return NM_GATE_ELEMENT, _ptr(gate, like.dtype, (B, C, T), name)
+
+
+def nm_residual_norm_fwd(x, f=None, *, gate=None, rscale=None, post_norm=None, post_weight=None, post_bias=None, next_norm=True,
+                         next_weight=None, next_bias=None, layer=False, eps=1e-5, lengths=None, y=None, n=None, stream=None):
+    """y = x + rscale*gate*h with h = f or its norm, n = norm(y); returns (y, n).  Without f: (x, norm(x)).
+    post_norm: whether f is normalised (None: if post_weight is given); next_norm: whether n is made (else None);
+    layer: LayerNorm instead of RMS norm.  lengths int32 [B]: zeros beyond."""
+    torch = _torch()
+    B, C, T = x.shape
+    post = (post_weight is not None) if post_norm is None else bool(post_norm)
+    if f is not None and y is None:
+        y = torch.empty_like(x)
+    if next_norm and n is None:
+        n = torch.empty_like(x)
+    kind, gp = _gate_kind(gate, x)
+    flags = (NM_NORM_POST if post else 0) | (NM_NORM_NEXT if next_norm else 0) | (NM_NORM_LAYER if layer else 0)
+    vec = lambda t, name: _ptr(t, torch.float32, (C,), name)  # noqa: E731
+    act = lambda t, name: _ptr(t, x.dtype, (B, C, T), name)  # noqa: E731
+    st = lib().nm_residual_norm_fwd(
+        B, C, T, act(x, "x"), act(f, "f"), gp, kind, vec(rscale, "rscale"), vec(post_weight, "post_weight"),
+        vec(post_bias, "post_bias"), vec(next_weight, "next_weight"), vec(next_bias, "next_bias"), eps,
+        _ptr(lengths, torch.int32, (B,), "lengths"), act(y, "y"), act(n, "n"), flags, _dtype_code(x), _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_residual_norm_fwd")
+    return (x if f is None else y), n
+
+
+def nm_residual_norm_bwd_workspace_bytes(B, C, T, dtype=NM_BF16) -> int:
+    return int(lib().nm_residual_norm_bwd_workspace_bytes(B, C, T, dtype))
+
+
+def nm_residual_norm_bwd(dy, dn, y, f=None, *, gate=None, rscale=None, post_norm=None, post_weight=None, post_bias=None,
+                         next_weight=None, next_bias=None, layer=False, eps=1e-5, lengths=None, out=None, workspace=None,
+                         stream=None):
+    """Gradients of nm_residual_norm_fwd from dy (or None) and dn (None: there was no next norm): a dict with dx, df, dgate, drscale,
+    dpost_weight, dpost_bias, dnext_weight, dnext_bias, None where there is nothing to differentiate.  y as the forward call
+    returned it.  Gradients of vectors are made for those that are given (float32); out: a dict of tensors to write them to."""
+    torch = _torch()
+    like = dn if dy is None else dy
+    B, C, T = like.shape
+    post = (post_weight is not None) if post_norm is None else bool(post_norm)
+    kind, gp = _gate_kind(gate, like)
+    flags = (NM_NORM_POST if post else 0) | (NM_NORM_NEXT if dn is not None else 0) | (NM_NORM_LAYER if layer else 0)
+    got = dict(out or {})
+    wanted = {"dx": like, "df": f, "dgate": gate, "drscale": rscale, "dpost_weight": post_weight, "dpost_bias": post_bias,
+              "dnext_weight": next_weight if dn is not None else None, "dnext_bias": next_bias if dn is not None else None}
+    for name, t in wanted.items():
+        if t is None:
+            got[name] = None
+        elif got.get(name) is None:
+            got[name] = torch.empty_like(t)
+    vec = lambda t, name: _ptr(t, torch.float32, (C,), name)  # noqa: E731
+    act = lambda t, name: _ptr(t, like.dtype, (B, C, T), name)  # noqa: E731
+    _, dgp = _gate_kind(got["dgate"], like, "dgate")
+    code = _dtype_code(like)
+    if workspace is None:
+        workspace = like.new_empty(max(nm_residual_norm_bwd_workspace_bytes(B, C, T, code), 256), dtype=torch.uint8)
+    st = lib().nm_residual_norm_bwd(
+        B, C, T, act(dy, "dy"), act(dn, "dn"), act(y, "y"), act(f, "f"), gp, kind, vec(rscale, "rscale"),
+        vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), vec(next_weight if dn is not None else None, "next_weight"), eps,
+        _ptr(lengths, torch.int32, (B,), "lengths"), act(got["dx"], "dx"), act(got["df"], "df"), dgp, vec(got["drscale"], "drscale"),
+        vec(got["dpost_weight"], "dpost_weight"), vec(got["dpost_bias"], "dpost_bias"), vec(got["dnext_weight"], "dnext_weight"),
+        vec(got["dnext_bias"], "dnext_bias"), flags, code, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_residual_norm_bwd")
+    return got
+
+
+# ---- AdamW over many tensors (include/nm_adamw.h) -----------------------------------------------
+class AdamWPlan:
+    """The tensors of a step and their description on host and device.  Keeps the tensors alive."""
+
+    def __init__(self, host, device, tensors, state_bits):
+        self.host, self.device, self.tensors, self.state_bits = host, device, tensors, state_bits
+
+
+def nm_adamw_plan(params, grads, m, v, *, m_scales=None, v_scales=None, copies=None, weight_decay=0.0) -> AdamWPlan:
+    """Plan of a step over lists of device tensors of any shapes: float32 params and grads, m and v (float32, or uint8 E4M3 codes
+    with the float32 scales of their blocks of 256: then states are held in 8 bits), copies (bfloat16 tensors or None each, or
+    None).  weight_decay: a number or one per tensor."""
+    torch = _torch()
+    count = len(params)
+    bits = 32 if m_scales is None else 8
+    if (m_scales is None) != (v_scales is None):
+        raise ValueError("m_scales and v_scales go together")
+    none = [None] * count
+    decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
+    lists = {"params": params, "grads": grads, "m": m, "v": v, "m_scales": m_scales or none, "v_scales": v_scales or none,
+             "copies": copies or none, "weight_decay": decay}
+    for name, ts in lists.items():
+        if len(ts) != count:
+            raise ValueError(f"{name} must have {count} entries, got {len(ts)}")
+    table = (AdamWTensor * max(count, 1))()
+    state = torch.float32 if bits == 32 else torch.uint8
+    for i in range(count):
+        n = params[i].numel()
+
+        def ptr(t, dtype, name, numel):
+            if t is not None and t.numel() != numel:
+                raise ValueError(f"{name}[{i}] must have {numel} elements, got {t.numel()}")
+            return _ptr(t, dtype, None, f"{name}[{i}]")
+
+        blocks = (n + 255) // 256
+        table[i] = AdamWTensor(ptr(params[i], torch.float32, "params", n), ptr(grads[i], torch.float32, "grads", n),
+                               ptr(m[i], state, "m", n), ptr(v[i], state, "v", n),
+                               ptr(lists["m_scales"][i], torch.float32, "m_scales", blocks),
+                               ptr(lists["v_scales"][i], torch.float32, "v_scales", blocks),
+                               ptr(lists["copies"][i], torch.bfloat16, "copies", n), n, float(decay[i]))
+    size = int(lib().nm_adamw_plan_bytes(table, count, bits))
+    if not size:
+        raise NmError(NM_ERR_BAD_ARG, "nm_adamw_plan_bytes")
+    host = torch.empty(size, dtype=torch.uint8)
+    st = lib().nm_adamw_plan(table, count, bits, host.data_ptr(), size)
+    if st != NM_OK:
+        raise NmError(st, "nm_adamw_plan")
+    return AdamWPlan(host, host.to(params[0].device), lists, bits)
+
+
+def nm_adamw_step(plan: AdamWPlan, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, step, grad_scale=None, seed=0, stream=None) -> None:
+    """One step over the tensors of the plan; step counts from 1.  grad_scale: float32 device tensor of one element that multiplies
+    the gradients.  seed: of the rounding of 8-bit states, another one each step."""
+    st = lib().nm_adamw_step(plan.host.data_ptr(), plan.device.data_ptr(), plan.host.numel(), lr, beta1, beta2, eps, step,
+                             _ptr(grad_scale, _torch().float32, None, "grad_scale"), seed & 0xFFFFFFFF, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_adamw_step")

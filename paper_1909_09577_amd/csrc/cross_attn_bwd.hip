@@ -1,0 +1,444 @@
+// Cross attention, backward (definition: include/nm_attention.h).
+//
+// Three kernels after one another: delta, the sums over channels of o * dout of every token; dk and dv, whose workgroups own
+// positions and go over all tokens of all heads that share them, so that nothing is added across workgroups; dq, whose workgroups
+// own tokens and go over the positions, in the two forms of the forward pass.  Scores and probabilities are made again in both
+// from the saved log-sum-exp: two of seven products, against writing and reading them.  In each kernel the result of the first
+// products (scores and dp) is the second operand of the next ones, in the registers it was made in (attn_tiles.h).
+#include "cross_attn.h"
+
+namespace nm {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Probability from a score and the log-sum-exp, both in halves of powers of two: the square of its root.  The exponential of the
+// hardware makes zeros of results below 2^-126, which scores and gradients of hundreds lift to values that a sum may consist of.
+__device__ __forceinline__ float probability(float score, float half_c, float half_lse)
+{
+    const float root = __builtin_amdgcn_exp2f(__builtin_fmaf(score, half_c, -half_lse));
+    return root * root;
+}
+
+template <typename S>
+__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a)
+{
+    __shared__ float s[8][33];
+    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int tiles = (a.U + 31) / 32, bh = blockIdx.x / tiles, u = (blockIdx.x - bh * tiles) * 32 + lane;
+    const int b = bh / a.H, h = bh - b * a.H;
+    const int q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
+    float t = 0.f;
+    if (u < q_len) {
+        const S *o = (const S *)a.o + (size_t)b * a.os + (size_t)h * a.D * a.U + u;
+        const S *g = (const S *)a.dout + (size_t)b * a.dos + (size_t)h * a.D * a.U + u;
+        for (int d = share; d < a.D; d += 8) t += load_as_f32(o, (size_t)d * a.U) * load_as_f32(g, (size_t)d * a.U);
+    }
+    s[share][lane] = t;
+    __syncthreads();
+    if (share == 0 && u < a.U) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v += s[i][lane];
+        a.delta[(size_t)bh * a.U + u] = v;
+    }
+}
+
+// ---- dk and dv: a wavefront owns 32 positions, the columns of its products; tokens are rows ------------------------------
+template <int TT>
+struct TokenRows {  // of a tile of tokens
+    float lse[TT], delta[TT];  // log-sum-exp in halves of powers of two, infinite where a token is not there
+    int lo[TT], hi[TT], range[2];
+};
+
+template <typename S, int DP, int NB, int NW>
+__global__ __launch_bounds__(NW * 64) void attn_dkv_kernel(AttnArgs a)
+{
+    typedef Mma<S> M;
+    constexpr int TT = NB * 32, NT = NW * 64, KS = DP / M::kSteps;
+    typedef Tile<S, DP, NB, NT> T;
+    typedef TokenRows<TT> Rows;
+    constexpr int kBuf = 2 * T::kBytes + (int)((sizeof(Rows) + 15) / 16 * 16);
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int bh = blockIdx.x % (a.B * a.Hkv), tile = blockIdx.x / (a.B * a.Hkv);
+    const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
+    const int w0 = (tile * NW + wave) * 32, t = w0 + (lane & 31);
+    const bool there = t < len;
+    const float half_c = 0.5f * a.c;
+
+    typename M::Frag kf[KS], vf[KS];
+    {
+        const size_t at = (size_t)kvh * a.D * a.T + min(t, a.T - 1);
+        const S *k = (const S *)a.k + (size_t)b * a.ks + at, *v = (const S *)a.v + (size_t)b * a.vs + at;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            kf[s] = M::column(k, s, half, a.D, a.T, there, a.flip);
+            vf[s] = M::column(v, s, half, a.D, a.T, there, 0u);
+        }
+    }
+    f32x16_t dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
+    int off[2];
+    M::template across_offsets<true>(lane, off);
+
+    const int tiles = (q_len + TT - 1) / TT, all = tile * NW * 32 < len ? tiles * a.G : 0;
+    T qt, gt;
+    float row_lse = 0.f, row_delta = 0.f;
+    int row_lo = 0, row_hi = 0;
+    auto load = [&](int i) {
+        const int g = i / tiles, u0 = (i - g * tiles) * TT, head = kvh * a.G + g;
+        qt.load((const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U, a.D, a.U, u0, threadIdx.x);
+        gt.load((const S *)a.dout + (size_t)b * a.dos + (size_t)head * a.D * a.U, a.D, a.U, u0, threadIdx.x);
+        if (threadIdx.x < TT) {
+            const int u = u0 + threadIdx.x, uc = min(u, a.U - 1);
+            const size_t row = ((size_t)b * a.H + head) * a.U + uc;
+            row_lse = a.lse[row];
+            row_delta = a.delta[row];
+            frames_of(a, b, uc, len, row_lo, row_hi);
+            if (u >= q_len) row_lo = row_hi = 0;
+        }
+    };
+    if (all > 0) load(0);
+    for (int i = 0; i < all; ++i) {
+        unsigned char *buf = smem + (i & 1) * kBuf;
+        Rows &rows = *reinterpret_cast<Rows *>(buf + 2 * T::kBytes);
+        const int u0 = (i % tiles) * TT;
+        qt.write(buf, a.D, a.U, q_len, u0, threadIdx.x);
+        gt.write(buf + T::kBytes, a.D, a.U, q_len, u0, threadIdx.x);
+        if (threadIdx.x < 64) {
+            const bool some = threadIdx.x < TT && row_lo < row_hi;
+            if (threadIdx.x < TT) {
+                rows.lse[threadIdx.x] = some && row_lse != -INFINITY ? row_lse * (0.5f * kLog2e) : INFINITY;
+                rows.delta[threadIdx.x] = some ? row_delta : 0.f;
+                rows.lo[threadIdx.x] = row_lo;
+                rows.hi[threadIdx.x] = row_hi;
+            }
+            if (a.windows) {
+                int lo = some ? row_lo : a.T, hi = some ? row_hi : 0;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    lo = min(lo, __shfl_xor(lo, d));
+                    hi = max(hi, __shfl_xor(hi, d));
+                }
+                rows.range[0] = lo;  // (the same value from every lane)
+                rows.range[1] = hi;
+            }
+        }
+        __syncthreads();
+        if (i + 1 < all) load(i + 1);
+        if (w0 >= len) continue;
+        if (a.windows && (rows.range[0] >= w0 + 32 || rows.range[1] <= w0)) continue;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const unsigned char *qb = buf + n * T::kBlock, *gb = qb + T::kBytes;
+            f32x16_t s, dp;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                s = M::mul(M::across(qb, off, st), kf[st], s);
+                dp = M::mul(M::across(gb, off, st), vf[st], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int u = 32 * n + M::position(r, half);
+                bool ok = there;
+                if (a.windows) ok = ok && t >= rows.lo[u] && t < rows.hi[u];
+                const float p = ok ? probability(s[r], half_c, rows.lse[u]) : 0.f;
+                s[r] = p;
+                dp[r] = p * (dp[r] - rows.delta[u]);
+            }
+            const typename M::Probs pp = M::probs(s), ds = M::probs(dp);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                dv[d] = M::mul(M::along(gb, d * 32, lane), pp, dv[d]);
+                dk[d] = M::mul(M::along(qb, d * 32, lane), ds, dk[d]);
+            }
+        }
+    }
+    if (t >= a.T) return;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            if (ch >= a.D) continue;
+            const size_t at = ((size_t)kvh * a.D + ch) * a.T + t;
+            store_from_f32((S *)a.dk, (size_t)b * a.dks + at, there ? dk[d][r] * a.scale : 0.f);
+            store_from_f32((S *)a.dv, (size_t)b * a.dvs + at, there ? dv[d][r] : 0.f);
+        }
+}
+
+// ---- dq: a wavefront's columns are tokens, rows are positions; shared and apart as in the forward pass ---------------------
+template <typename S, int DP, int NB, int NW, bool SHARED>
+__global__ __launch_bounds__(NW * 64) void attn_dq_kernel(AttnArgs a)
+{
+    typedef Mma<S> M;
+    constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;
+    typedef Tile<S, DP, NB, NT> T;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int ct = rest % a.col_tiles, split = rest / a.col_tiles;
+    const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
+    const S *krows = (const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T;
+    const S *vrows = (const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T;
+
+    const int m = (SHARED ? ct * NW + wave : ct) * 32 + (lane & 31);
+    const bool exists = m < a.G * a.U;
+    const int g = exists ? m / a.U : 0, u = exists ? m - g * a.U : 0, head = kvh * a.G + g;
+    const bool there = exists && u < q_len;
+    const float half_c = 0.5f * a.c;
+    int lo = 0, hi = 0x7fffffff, first = a.T, last = 0;
+    float lse = INFINITY, delta = 0.f;  // a token that is not there, or without frames: every probability is zero
+    if (there) {
+        frames_of(a, b, u, len, lo, hi);
+        first = lo;
+        last = hi;
+        if (lo < hi) {
+            lse = a.lse[((size_t)b * a.H + head) * a.U + u] * (0.5f * kLog2e);
+            if (lse == -INFINITY) lse = INFINITY;
+            delta = a.delta[((size_t)b * a.H + head) * a.U + u];
+        }
+    }
+    typename M::Frag q[KS], go[KS];
+    {
+        const size_t at = (size_t)head * a.D * a.U + u;
+        const S *qc = (const S *)a.q + (size_t)b * a.qs + at, *gc = (const S *)a.dout + (size_t)b * a.dos + at;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            q[s] = M::column(qc, s, half, a.D, a.U, there && lo < hi, a.flip);
+            go[s] = M::column(gc, s, half, a.D, a.U, there && lo < hi, 0u);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        first = min(first, __shfl_xor(first, d));
+        last = max(last, __shfl_xor(last, d));
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    const bool active = last > first;
+    if constexpr (SHARED) {  // of the workgroup
+        int *range = reinterpret_cast<int *>(smem);
+        if (lane == 0) {
+            range[wave] = first;
+            range[NW + wave] = last;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            first = min(first, range[w]);
+            last = max(last, range[NW + w]);
+        }
+        __syncthreads();
+    }
+    const int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+    f32x16_t acc[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    int off[2];
+    M::template across_offsets<true>(lane, off);
+
+    auto compute = [&](const unsigned char *ktile, const unsigned char *vtile, int t0) {
+        const bool whole = __all(lo <= t0 && t0 + TT <= hi);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const unsigned char *kb = ktile + n * T::kBlock, *vb = vtile + n * T::kBlock;
+            f32x16_t s, dp;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                s = M::mul(M::across(kb, off, st), q[st], s);
+                dp = M::mul(M::across(vb, off, st), go[st], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = probability(s[r], half_c, lse);
+                dp[r] = p * (dp[r] - delta);
+            }
+            if (!whole) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int t = t0 + 32 * n + M::position(r, half);
+                    dp[r] = t >= lo && t < hi ? dp[r] : 0.f;
+                }
+            }
+            const typename M::Probs ds = M::probs(dp);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) acc[d] = M::mul(M::along(kb, d * 32, lane), ds, acc[d]);
+        }
+    };
+    T kt, vt;
+    if constexpr (SHARED) {
+        if (t_begin < t_end) {
+            kt.load(krows, a.D, a.T, t_begin * TT, threadIdx.x);
+            vt.load(vrows, a.D, a.T, t_begin * TT, threadIdx.x);
+        }
+        for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
+            unsigned char *buf = smem + turn * 2 * T::kBytes;
+            kt.write(buf, a.D, a.T, len, t * TT, threadIdx.x);
+            vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, threadIdx.x);
+            __syncthreads();  // (the other buffer is written next: all are through with it before they pass here again)
+            if (t + 1 < t_end) {
+                kt.load(krows, a.D, a.T, (t + 1) * TT, threadIdx.x);
+                vt.load(vrows, a.D, a.T, (t + 1) * TT, threadIdx.x);
+            }
+            if (active) compute(buf, buf + T::kBytes, t * TT);
+        }
+    } else {
+        unsigned char *buf = smem + wave * 2 * T::kBytes;
+        int t = t_begin + wave;
+        if (t < t_end) {
+            kt.load(krows, a.D, a.T, t * TT, lane);
+            vt.load(vrows, a.D, a.T, t * TT, lane);
+        }
+        for (; t < t_end; t += NW) {
+            wave_fence();
+            kt.write(buf, a.D, a.T, len, t * TT, lane);
+            vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, lane);
+            wave_fence();
+            if (t + NW < t_end) {
+                kt.load(krows, a.D, a.T, (t + NW) * TT, lane);
+                vt.load(vrows, a.D, a.T, (t + NW) * TT, lane);
+            }
+            compute(buf, buf + T::kBytes, t * TT);
+        }
+    }
+    auto put = [&](int d, int r, float v) {
+        const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+        if (!exists || ch >= a.D) return;
+        if (!there) v = 0.f;
+        if (a.splits > 1)
+            a.part[(((size_t)split * a.B + b) * a.H + head) * a.D * a.U + (size_t)ch * a.U + u] = v;
+        else
+            store_from_f32((S *)a.dq, (size_t)b * a.dqs + ((size_t)head * a.D + ch) * a.U + u, v * a.scale);
+    };
+    if constexpr (SHARED) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) put(d, r, acc[d][r]);
+    } else {
+        constexpr int PAIRS = DP / 32 * 16;
+        float *prod = reinterpret_cast<float *>(smem);  // [NW][PAIRS][64]
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) prod[(wave * PAIRS + d * 16 + r) * 64 + lane] = acc[d][r];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < PAIRS / NW; ++n) {
+            const int pair = n * NW + wave;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) v += prod[(w * PAIRS + pair) * 64 + lane];
+            put(pair / 16, pair % 16, v);
+        }
+    }
+}
+
+// Adds the parts of dq of `splits` workgroups, in order.
+template <typename S>
+__global__ __launch_bounds__(256) void attn_dq_join_kernel(AttnArgs a)
+{
+    const size_t item = (size_t)a.H * a.D * a.U, all = item * a.B;
+    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= all) return;
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += a.part[s * all + e];
+    const size_t b = e / item;
+    store_from_f32((S *)a.dq, b * a.dqs + (e - b * item), v * a.scale);
+}
+
+// ---- sizes ------------------------------------------------------------------------------------------------------
+constexpr int kWaves = 4;
+
+template <typename S, int DP>
+hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
+{
+    static LdsOptIn opt;
+    constexpr int NB = sizeof(S) == 2 ? 2 : 1;
+    constexpr int bytes = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
+    static_assert(bytes <= 160 * 1024, "LDS of a CU");
+    auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;
+    const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
+    if (e != hipSuccess) return e;
+    const int per = kWaves * 32;
+    fn<<<dim3((unsigned)(a.B * a.Hkv) * ((a.T + per - 1) / per)), dim3(kWaves * 64), bytes, s>>>(a);
+    return hipGetLastError();
+}
+
+struct Form {
+    int columns, tile, waves;  // of a workgroup: tokens, positions of a tile, wavefronts with tiles of their own
+};
+constexpr bool two_blocks(bool bf16, int DP, bool shared) { return bf16 && (shared || DP <= 64); }
+// (float tiles of wide heads, one per wavefront, do not fit the registers)
+bool is_shared(bool bf16, int DP, long long columns) { return columns > 32 || (!bf16 && DP > 64); }
+Form form_of(bool bf16, int DP, long long columns)
+{
+    const bool shared = is_shared(bf16, DP, columns);
+    return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves};
+}
+template <typename S, int DP, bool SHARED>
+hipError_t run_dq(const AttnArgs &a, hipStream_t s)
+{
+    static LdsOptIn opt;
+    constexpr int NB = two_blocks(sizeof(S) == 2, DP, SHARED) ? 2 : 1, NT = SHARED ? kWaves * 64 : 64;
+    constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? 0 : kWaves * DP / 32 * 16 * 64 * 4;
+    constexpr int bytes = tiles > join ? tiles : join;
+    static_assert(bytes <= 160 * 1024, "LDS of a CU");
+    auto *fn = attn_dq_kernel<S, DP, NB, kWaves, SHARED>;
+    const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
+    if (e != hipSuccess) return e;
+    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.col_tiles * a.splits), dim3(kWaves * 64), bytes, s>>>(a);
+    return hipGetLastError();
+}
+template <typename S, int DP>
+hipError_t run_both(const AttnArgs &a, hipStream_t s)
+{
+    const hipError_t e = run_dkv<S, DP>(a, s);
+    if (e != hipSuccess) return e;
+    if constexpr (sizeof(S) == 2 || DP <= 64) {
+        if (!is_shared(sizeof(S) == 2, DP, (long long)a.G * a.U)) return run_dq<S, DP, false>(a, s);
+    }
+    return run_dq<S, DP, true>(a, s);
+}
+template <typename S>
+hipError_t run_any(const AttnArgs &a, hipStream_t s)
+{
+    attn_delta_kernel<S><<<dim3((unsigned)(a.B * a.H) * ((a.U + 31) / 32)), dim3(256), 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.D <= 32) e = run_both<S, 32>(a, s);
+    else if (a.D <= 64) e = run_both<S, 64>(a, s);
+    else if (a.D <= 96) e = run_both<S, 96>(a, s);
+    else e = run_both<S, 128>(a, s);
+    if (e != hipSuccess || a.splits == 1) return e;
+    attn_dq_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
+{
+    const int DP = (D + 31) / 32 * 32;
+    const long long columns = (long long)(H / Hkv) * U;
+    const Form f = form_of(bf16, DP, columns);
+    return attn_plan(f.columns, f.tile, f.waves, B, H, Hkv, D, U, T);
+}
+
+hipError_t launch_attn_bwd(bool bf16, const AttnArgs &a, hipStream_t s) { return bf16 ? run_any<bf16_t>(a, s) : run_any<float>(a, s); }
+
+}  // namespace nm

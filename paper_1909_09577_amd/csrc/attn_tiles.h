@@ -226,6 +226,43 @@ struct Tile {
     }
 };
 
+// A wavefront's result, 32 * (DP / 32) channels x 32 positions with the positions as columns, to rows of `len` elements in memory:
+// through LDS (`block`, DP rows, the wavefront's own), so that a lane stores 16 bytes of a row and four or eight lanes a whole
+// block's row.  Straight from the registers a store covers two bytes of a lane, and the address unit is what the kernel waits for.
+template <typename S, int DP>
+__device__ __forceinline__ void store_block(unsigned char *block, const f32x16_t (&acc)[DP / 32], float scale, S *rows, int D, int len, int t0, int valid,
+                                            int lane)
+{
+    typedef Mma<S> M;
+    constexpr int G = M::kPerGranule, GB = M::kRow / 16;
+    const int t = lane & 31, half = lane >> 5;
+    const bool there = t0 + t < valid;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            store_from_f32(reinterpret_cast<S *>(block + M::granule(ch, t / G)), t % G, there ? acc[d][r] * scale : 0.f);
+        }
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < DP * GB / 64; ++i) {
+        const int row = i * (64 / GB) + lane / GB, g = lane % GB, n = len - (t0 + g * G);
+        if (row >= D || n <= 0) continue;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(block + M::granule(row, g));
+        S *p = rows + (size_t)row * len + t0 + g * G;
+        if (n >= G) {
+            __builtin_memcpy(p, &v, 16);
+        } else {
+            S e[G];
+            __builtin_memcpy(e, &v, 16);
+#pragma unroll
+            for (int j = 0; j < G - 1; ++j)
+                if (j < n) p[j] = e[j];
+        }
+    }
+}
+
 __device__ __forceinline__ int clipped(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
 
 // Arguments of the kernels, forward and backward.

@@ -52,7 +52,7 @@ struct TokenRows {  // of a tile of tokens
 };
 
 template <typename S, int DP, int NB, int NW>
-__global__ __launch_bounds__(NW * 64) void attn_dkv_kernel(AttnArgs a)
+__global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = NW * 64, KS = DP / M::kSteps;
@@ -66,24 +66,30 @@ __global__ __launch_bounds__(NW * 64) void attn_dkv_kernel(AttnArgs a)
     const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
     const int w0 = (tile * NW + wave) * 32, t = w0 + (lane & 31);
     const bool there = t < len;
-    const float half_c = 0.5f * a.c;
+    const float c = (a.flip ? -0.5f : 0.5f) * a.c;
 
+    int off[2];
     typename M::Frag kf[KS], vf[KS];
-    {
-        const size_t at = (size_t)kvh * a.D * a.T + min(t, a.T - 1);
-        const S *k = (const S *)a.k + (size_t)b * a.ks + at, *v = (const S *)a.v + (size_t)b * a.vs + at;
+    if (tile * NW * 32 < len) {  // (uniform) the workgroup's positions of k and v go through LDS once
+        typedef Tile<S, DP, NW, NT> Own;
+        Own own;
+        M::template across_offsets<false>(lane, off);
+        auto fetch = [&](const S *rows, typename M::Frag (&f)[KS]) {
+            own.load(rows, a.D, a.T, tile * NW * 32, threadIdx.x);
+            own.write(smem, a.D, a.T, len, tile * NW * 32, threadIdx.x);
+            __syncthreads();
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            kf[s] = M::column(k, s, half, a.D, a.T, there, a.flip);
-            vf[s] = M::column(v, s, half, a.D, a.T, there, 0u);
-        }
+            for (int s = 0; s < KS; ++s) f[s] = M::across(smem + wave * Own::kBlock, off, s);
+            __syncthreads();
+        };
+        fetch((const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T, kf);
+        fetch((const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T, vf);
     }
     f32x16_t dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
-    int off[2];
     M::template across_offsets<true>(lane, off);
 
     const int tiles = (q_len + TT - 1) / TT, all = tile * NW * 32 < len ? tiles * a.G : 0;
@@ -149,7 +155,7 @@ __global__ __launch_bounds__(NW * 64) void attn_dkv_kernel(AttnArgs a)
                 const int u = 32 * n + M::position(r, half);
                 bool ok = there;
                 if (a.windows) ok = ok && t >= rows.lo[u] && t < rows.hi[u];
-                const float p = ok ? probability(s[r], half_c, rows.lse[u]) : 0.f;
+                const float p = ok ? probability(s[r], c, rows.lse[u]) : 0.f;
                 s[r] = p;
                 dp[r] = p * (dp[r] - rows.delta[u]);
             }
@@ -161,22 +167,18 @@ __global__ __launch_bounds__(NW * 64) void attn_dkv_kernel(AttnArgs a)
             }
         }
     }
-    if (t >= a.T) return;
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-            if (ch >= a.D) continue;
-            const size_t at = ((size_t)kvh * a.D + ch) * a.T + t;
-            store_from_f32((S *)a.dk, (size_t)b * a.dks + at, there ? dk[d][r] * a.scale : 0.f);
-            store_from_f32((S *)a.dv, (size_t)b * a.dvs + at, there ? dv[d][r] : 0.f);
-        }
+    __syncthreads();  // (the tiles give way to the results)
+    if (w0 >= a.T) return;
+    unsigned char *block = smem + wave * DP * M::kRow;
+    const size_t at = (size_t)kvh * a.D * a.T;
+    store_block<S, DP>(block, dk, a.scale, (S *)a.dk + (size_t)b * a.dks + at, a.D, a.T, w0, len, lane);
+    wave_fence();
+    store_block<S, DP>(block, dv, 1.f, (S *)a.dv + (size_t)b * a.dvs + at, a.D, a.T, w0, len, lane);
 }
 
 // ---- dq: a wavefront's columns are tokens, rows are positions; shared and apart as in the forward pass ---------------------
 template <typename S, int DP, int NB, int NW, bool SHARED>
-__global__ __launch_bounds__(NW * 64) void attn_dq_kernel(AttnArgs a)
+__global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192) ? 2 : 1) void attn_dq_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;
@@ -368,8 +370,9 @@ template <typename S, int DP>
 hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
-    constexpr int NB = sizeof(S) == 2 ? 2 : 1;
-    constexpr int bytes = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
+    constexpr int NB = sizeof(S) == 2 && DP <= 96 ? 2 : 1;
+    constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
+    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, bytes = tiles > own ? tiles : own;
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);

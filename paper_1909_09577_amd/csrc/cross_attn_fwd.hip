@@ -17,7 +17,7 @@ namespace nm {
 namespace {
 
 template <typename S, int DP, int NU, int NB, int NW, bool SHARED>
-__global__ __launch_bounds__(NW * 64) void attn_fwd_kernel(AttnArgs a)
+__global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;

@@ -68,21 +68,31 @@ struct Mma<bf16_t> {
         u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(block + off[1] + step * 1024));
         return u.v;
     }
-    // the same operand of 32 columns straight from memory: channels d0.. of the lane's column, `pitch` elements apart
-    static __device__ __forceinline__ Frag column(const bf16_t *p, int step, int half, int D, size_t pitch, bool there, uint32_t flip)
+    // the same operand of 32 columns straight from memory: channels of the lane's column p, `pitch` elements apart (a head's
+    // rows span less than 4 GiB); zeros unless `there`.  Every load is made, from a channel that exists: a branch around each is what
+    // the call would wait for.
+    static __device__ __forceinline__ Frag column(const bf16_t *p, int step, int half, int D, uint32_t pitch, bool there, uint32_t flip)
     {
-        union {
-            bf16_t e[8];
-            bf16x8_t v;
-        } u;
+        bf16_t e[8];
+        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int d = 16 * step + 8 * half + j;
-            u.e[j] = there && d < D ? (bf16_t)(p[(size_t)d * pitch] ^ (flip >> 16)) : (bf16_t)0;
+        for (int j = 0; j < 8; ++j) e[j] = *reinterpret_cast<const bf16_t *>(reinterpret_cast<const char *>(p) + (size_t)((uint32_t)min(16 * step + 8 * half + j, D - 1) * pitch * 2u));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 16 * step + 8 * half + 2 * j;
+            w[j] = ((uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16) ^ (flip | flip >> 16);
+            w[j] &= !there || d >= D ? 0u : (d + 1 < D ? 0xffffffffu : 0xffffu);
         }
-        return u.v;
+        return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
     }
     static __device__ __forceinline__ f32x16_t mul(Frag a, Frag b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float dot(Frag a, Frag b)
+    {
+        float t = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t += (float)a[j] * (float)b[j];
+        return t;
+    }
 
     static __device__ __forceinline__ Probs probs(const f32x16_t &p)  // rounds to bfloat16
     {
@@ -137,12 +147,14 @@ struct Mma<float> {
     {
         return *reinterpret_cast<const float *>(block + off[0] + (off[1] ^ ((step & 7) << 4)) + step * 2 * kRow);
     }
-    static __device__ __forceinline__ Frag column(const float *p, int step, int half, int D, size_t pitch, bool there, uint32_t flip)
+    static __device__ __forceinline__ Frag column(const float *p, int step, int half, int D, uint32_t pitch, bool there, uint32_t flip)
     {
         const int d = 2 * step + half;
-        return there && d < D ? __uint_as_float(__float_as_uint(p[(size_t)d * pitch]) ^ flip) : 0.f;
+        const float v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p) + (size_t)((uint32_t)min(d, D - 1) * pitch * 4u));
+        return there && d < D ? __uint_as_float(__float_as_uint(v) ^ flip) : 0.f;
     }
     static __device__ __forceinline__ f32x16_t mul(Frag a, Frag b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float dot(Frag a, Frag b) { return a * b; }
     static __device__ __forceinline__ Probs probs(const f32x16_t &p) { return p; }
     struct Along {
         f32x4_t s[4];
@@ -178,7 +190,7 @@ struct Mma<float> {
     }
 };
 
-// A tile of NB blocks, loaded by NT threads: `count` granules each, held in registers between the load and the write.
+// A tile of NB blocks, loaded by NT threads: kCount granules each, held in registers between the load and the write.
 template <typename S, int DP, int NB, int NT>
 struct Tile {
     typedef Mma<S> M;
@@ -187,21 +199,43 @@ struct Tile {
     static constexpr int kPerRow = NB * M::kRow / 16;  // granules
     static constexpr int kCount = DP * kPerRow / NT;
     static_assert(DP * kPerRow % NT == 0, "whole granules per thread");
+
+    // A thread's places in the tiles of a sequence: byte offsets from channel 0 of a tile's first position, in 32 bits beside a base
+    // that all threads share (a head's rows span less than 4 GiB).  Sequences of equal shape have the same.
+    struct Places {
+        uint32_t off[kCount];
+        __device__ __forceinline__ void set(int D, int len, int thread)
+        {
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const int e = i * NT + thread, row = min(e / kPerRow, D - 1);
+                off[i] = ((uint32_t)row * (uint32_t)len + (uint32_t)(e % kPerRow) * M::kPerGranule) * (uint32_t)sizeof(S);
+            }
+        }
+    };
     u32x4_t r[kCount];
 
-    // rows: channel 0 at step 0 of the sequence, `len` elements a row, D rows; t0: the tile's first position
-    __device__ __forceinline__ void load(const S *rows, int D, int len, int t0, int thread)
+    // rows: channel 0 at step 0 of the sequence, `len` elements a row; t0: the tile's first position (below len)
+    __device__ __forceinline__ void load(const S *rows, const Places &at, int len, int t0, int thread)
     {
         constexpr int G = M::kPerGranule;
+        const char *base = reinterpret_cast<const char *>(rows + t0);
+        if (t0 + NB * 32 <= len) {  // (uniform)
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            const int e = i * NT + thread, row = min(e / kPerRow, D - 1), t = t0 + (e % kPerRow) * G;
-            if (len >= G) {  // (uniform)
-                __builtin_memcpy(&r[i], rows + (size_t)row * len + min(t, len - G), 16);
-            } else {
+            for (int i = 0; i < kCount; ++i) __builtin_memcpy(&r[i], base + at.off[i], 16);
+        } else if (len >= G) {  // groups that reach over the end are read from the row's last whole one
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const int t = t0 + (i * NT + thread) % kPerRow * G;
+                __builtin_memcpy(&r[i], reinterpret_cast<const char *>(rows) + (at.off[i] + (uint32_t)(t0 + min(len - G - t, 0)) * (uint32_t)sizeof(S)), 16);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const int t = (i * NT + thread) % kPerRow * G;  // (t0 is 0)
                 S v[G];
 #pragma unroll
-                for (int j = 0; j < G; ++j) v[j] = t + j < len ? rows[(size_t)row * len + t + j] : S(0);
+                for (int j = 0; j < G; ++j) v[j] = t + j < len ? *reinterpret_cast<const S *>(base + at.off[i] + j * sizeof(S)) : S(0);
                 __builtin_memcpy(&r[i], v, 16);
             }
         }
@@ -209,26 +243,31 @@ struct Tile {
     // zeros for rows from D on and positions from `valid` (<= len) on
     __device__ __forceinline__ void write(unsigned char *tile, int D, int len, int valid, int t0, int thread)
     {
-        constexpr int G = M::kPerGranule;
-        const bool ends = t0 + NB * 32 > valid;  // (uniform)
+        constexpr int G = M::kPerGranule, GB = M::kRow / 16;
+        if (t0 + NB * 32 > valid) {  // (uniform)
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const int t = t0 + (i * NT + thread) % kPerRow * G;
+                if (len >= G) r[i] = M::down(r[i], t, len);
+                r[i] = M::first(r[i], valid - t);
+            }
+        }
+        if (D < DP) {  // (uniform)
+#pragma unroll
+            for (int i = 0; i < kCount; ++i)
+                if ((i * NT + thread) / kPerRow >= D) r[i] = u32x4_t{0u, 0u, 0u, 0u};
+        }
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int e = i * NT + thread, row = e / kPerRow, gi = e % kPerRow, t = t0 + gi * G;
-            u32x4_t v = r[i];
-            if (ends) {
-                if (len >= G) v = M::down(v, t, len);
-                v = M::first(v, valid - t);
-            }
-            if (row >= D) v = u32x4_t{0u, 0u, 0u, 0u};
-            constexpr int GB = M::kRow / 16;
-            *reinterpret_cast<u32x4_t *>(tile + (gi / GB) * kBlock + M::granule(row, gi % GB)) = v;
+            const int e = i * NT + thread, row = e / kPerRow, gi = e % kPerRow;
+            *reinterpret_cast<u32x4_t *>(tile + (gi / GB) * kBlock + M::granule(row, gi % GB)) = r[i];
         }
     }
 };
 
 // A wavefront's result, 32 * (DP / 32) channels x 32 positions with the positions as columns, to rows of `len` elements in memory:
 // through LDS (`block`, DP rows, the wavefront's own), so that a lane stores 16 bytes of a row and four or eight lanes a whole
-// block's row.  Straight from the registers a store covers two bytes of a lane, and the address unit is what the kernel waits for.
+// block's row.  `scale` may differ from lane to lane (a lane is a position).  Straight from the registers a store covers two bytes of a lane, and the address unit is what the kernel waits for.
 template <typename S, int DP>
 __device__ __forceinline__ void store_block(unsigned char *block, const f32x16_t (&acc)[DP / 32], float scale, S *rows, int D, int len, int t0, int valid,
                                             int lane)
@@ -240,9 +279,18 @@ __device__ __forceinline__ void store_block(unsigned char *block, const f32x16_t
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; r += 2) {
             const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-            store_from_f32(reinterpret_cast<S *>(block + M::granule(ch, t / G)), t % G, there ? acc[d][r] * scale : 0.f);
+            const float v0 = there ? acc[d][r] * scale : 0.f, v1 = there ? acc[d][r + 1] * scale : 0.f;
+            S *p0 = reinterpret_cast<S *>(block + M::granule(ch, t / G)) + t % G, *p1 = reinterpret_cast<S *>(block + M::granule(ch + 1, t / G)) + t % G;
+            if constexpr (sizeof(S) == 2) {
+                const uint32_t w = pack_bf16x2(v0, v1);
+                *p0 = (S)(w & 0xffffu);
+                *p1 = (S)(w >> 16);
+            } else {
+                *p0 = v0;
+                *p1 = v1;
+            }
         }
     wave_fence();
 #pragma unroll
@@ -280,6 +328,8 @@ struct AttnArgs {
     float *part, *part_ml;  // sums of the workgroups that share tokens, their maxima and sums
     float *delta;           // [B][H][U]
     int col_tiles, splits, tiles_per_split;
+    float *kv_part;  // [parts][2][B][Hkv][D][T]: sums of the workgroups that share positions
+    int pos_tiles, parts, units_per_part;
 };
 
 // The frames a token may look at, [lo, hi).

@@ -5,16 +5,34 @@
 
 namespace nm {
 
-// A workgroup takes `rounds` rounds of tiles; where there are too few workgroups to fill the chip twice, rounds are shared out.
+// of the estimates below, in microseconds: a round of 64 positions at 64 channels, what comes before and after the rounds, a second launch
+constexpr double kRoundUs = 1.2, kStartUs = 3.0, kJoinUs = 4.0;
+
+// Two workgroups run on a CU, so that `slots` go on at a time.
+int attn_share(long long groups, int rounds, double round_us, double join_bytes)
+{
+    const long long slots = 512;
+    double best = 0;
+    int per = rounds;
+    for (int n = 1; n <= rounds && n <= kMaxSplits; ++n) {
+        const int each = (rounds + n - 1) / n;
+        if ((rounds + each - 1) / each != n) continue;
+        const double us = (double)((groups * n + slots - 1) / slots) * (kStartUs + each * round_us) + (n > 1 ? kJoinUs + n * join_bytes / 4.0e6 : 0.0);
+        if (n == 1 || us < best) {
+            best = us;
+            per = each;
+        }
+    }
+    return per;
+}
+
+// A workgroup takes rounds of `waves` tiles.
 AttnPlan attn_plan(int columns, int tile, int waves, int B, int H, int Hkv, int D, int U, int T)
 {
     AttnPlan p = {};
     p.col_tiles = (int)(((long long)(H / Hkv) * U + columns - 1) / columns);
     const int tiles = (T + tile - 1) / tile, rounds = (tiles + waves - 1) / waves;
-    const long long groups = (long long)B * Hkv * p.col_tiles, want = (512 + groups - 1) / groups;
-    int splits = (int)(want < 1 ? 1 : want > rounds ? rounds : want);
-    splits = splits > 64 ? 64 : splits;
-    const int per = (rounds + splits - 1) / splits;
+    const int per = attn_share((long long)B * Hkv * p.col_tiles, rounds, kRoundUs * D / 64 * tile / 64, 2.0 * 4 * B * H * U * D);
     p.splits = (rounds + per - 1) / per;
     p.tiles_per_split = per * waves;
     const size_t rows = (size_t)B * H * U;
@@ -31,6 +49,8 @@ int check(int B, int H, int Hkv, int D, int U, int T, int dtype)
 {
     if (B <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || U <= 0 || T <= 0 || H % Hkv || (dtype != NM_BF16 && dtype != NM_F32)) return NM_ERR_BAD_ARG;
     const long long most = (1LL << 31) - 1;
+    const int element = dtype == NM_BF16 ? 2 : 4;
+    if ((long long)D * element > ((1LL << 32) - 1) / U || (long long)D * element > ((1LL << 32) - 1) / T) return NM_ERR_UNSUPPORTED;  // a head's rows
     if (D > kMaxD || (long long)H * D > most / U || (long long)Hkv * D > most / T || (long long)B * H > (1 << 24)) return NM_ERR_UNSUPPORTED;
     if ((long long)B * H * U > most / 2) return NM_ERR_UNSUPPORTED;
     // the grids, with as many column tiles, position tiles and parts as there can be
@@ -97,7 +117,7 @@ size_t nm_cross_attn_workspace_bytes(int op, int B, int heads, int kv_heads, int
     }
     if (op == NM_OP_ATTN_BWD) {
         const AttnPlan p = attn_bwd_plan(dtype == NM_BF16, B, heads, kv_heads, D, U, T);
-        return align_up((size_t)B * heads * U * sizeof(float), 256) + p.part_bytes;
+        return align_up(align_up((size_t)B * heads * U * sizeof(float), 256) + p.part_bytes + p.kv_part_bytes, 256);
     }
     return 0;
 }
@@ -158,7 +178,7 @@ int nm_cross_attn_bwd(int B, int heads, int kv_heads, int D, int U, int T, const
     }
     const AttnPlan p = attn_bwd_plan(dtype == NM_BF16, B, heads, kv_heads, D, U, T);
     const size_t delta_bytes = align_up((size_t)B * heads * U * sizeof(float), 256);
-    const int ws = workspace_status(workspace, workspace_bytes, delta_bytes + p.part_bytes);
+    const int ws = workspace_status(workspace, workspace_bytes, delta_bytes + p.part_bytes + p.kv_part_bytes);
     if (ws != NM_OK) return ws;
     a.B = B; a.H = heads; a.Hkv = kv_heads; a.G = heads / kv_heads; a.D = D; a.U = U; a.T = T;
     a.q = q; a.k = k; a.v = v; a.o = o; a.dout = dout;
@@ -168,6 +188,8 @@ int nm_cross_attn_bwd(int B, int heads, int kv_heads, int D, int U, int T, const
     a.lse = const_cast<float *>(lse);
     a.delta = (float *)workspace;
     a.part = (float *)((char *)workspace + delta_bytes);
+    a.kv_part = (float *)((char *)workspace + delta_bytes + p.part_bytes);
+    a.pos_tiles = p.pos_tiles; a.parts = p.parts; a.units_per_part = p.units_per_part;
     a.col_tiles = p.col_tiles; a.splits = p.splits; a.tiles_per_split = p.tiles_per_split;
     return dev(launch_attn_bwd(dtype == NM_BF16, a, (hipStream_t)hip_stream));
 }

@@ -1,10 +1,11 @@
 // Cross attention, backward (definition: include/nm_attention.h).
 //
-// Three kernels after one another: delta, the sums over channels of o * dout of every token; dk and dv, whose workgroups own
-// positions and go over all tokens of all heads that share them, so that nothing is added across workgroups; dq, whose workgroups
-// own tokens and go over the positions, in the two forms of the forward pass.  Scores and probabilities are made again in both
-// from the saved log-sum-exp: two of seven products, against writing and reading them.  In each kernel the result of the first
-// products (scores and dp) is the second operand of the next ones, in the registers it was made in (attn_tiles.h).
+// Two kernels after one another: dq, whose workgroups own tokens and go over the positions, in the two forms of the forward pass,
+// and which leaves delta, the sums over channels of o * dout of its tokens, in the workspace; dk and dv, whose workgroups own positions
+// and go over the tokens of all heads that share them.  Scores and probabilities are made again in both from the saved
+// log-sum-exp: two of seven products, against writing and reading them.  In each kernel the result of the first products (scores
+// and dp) is the second operand of the next ones, in the registers it was made in (attn_tiles.h).  Where either has too few
+// workgroups, several share one's positions or tokens, and their sums are joined by another kernel, in order.
 #include "cross_attn.h"
 
 namespace nm {
@@ -20,31 +21,9 @@ __device__ __forceinline__ float probability(float score, float half_c, float ha
     return root * root;
 }
 
-template <typename S>
-__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a)
-{
-    __shared__ float s[8][33];
-    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const int tiles = (a.U + 31) / 32, bh = blockIdx.x / tiles, u = (blockIdx.x - bh * tiles) * 32 + lane;
-    const int b = bh / a.H, h = bh - b * a.H;
-    const int q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
-    float t = 0.f;
-    if (u < q_len) {
-        const S *o = (const S *)a.o + (size_t)b * a.os + (size_t)h * a.D * a.U + u;
-        const S *g = (const S *)a.dout + (size_t)b * a.dos + (size_t)h * a.D * a.U + u;
-        for (int d = share; d < a.D; d += 8) t += load_as_f32(o, (size_t)d * a.U) * load_as_f32(g, (size_t)d * a.U);
-    }
-    s[share][lane] = t;
-    __syncthreads();
-    if (share == 0 && u < a.U) {
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v += s[i][lane];
-        a.delta[(size_t)bh * a.U + u] = v;
-    }
-}
-
 // ---- dk and dv: a wavefront owns 32 positions, the columns of its products; tokens are rows ------------------------------
+constexpr int kReach = 256;  // tiles of tokens
+
 template <int TT>
 struct TokenRows {  // of a tile of tokens
     float lse[TT], delta[TT];  // log-sum-exp in halves of powers of two, infinite where a token is not there
@@ -61,11 +40,11 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     constexpr int kBuf = 2 * T::kBytes + (int)((sizeof(Rows) + 15) / 16 * 16);
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int bh = blockIdx.x % (a.B * a.Hkv), tile = blockIdx.x / (a.B * a.Hkv);
+    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int tile = rest % a.pos_tiles, part = rest / a.pos_tiles;
     const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
     const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
     const int w0 = (tile * NW + wave) * 32, t = w0 + (lane & 31);
-    const bool there = t < len;
     const float c = (a.flip ? -0.5f : 0.5f) * a.c;
 
     int off[2];
@@ -73,9 +52,11 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     if (tile * NW * 32 < len) {  // (uniform) the workgroup's positions of k and v go through LDS once
         typedef Tile<S, DP, NW, NT> Own;
         Own own;
+        typename Own::Places at;
+        at.set(a.D, a.T, threadIdx.x);
         M::template across_offsets<false>(lane, off);
         auto fetch = [&](const S *rows, typename M::Frag (&f)[KS]) {
-            own.load(rows, a.D, a.T, tile * NW * 32, threadIdx.x);
+            own.load(rows, at, a.T, tile * NW * 32, threadIdx.x);
             own.write(smem, a.D, a.T, len, tile * NW * 32, threadIdx.x);
             __syncthreads();
 #pragma unroll
@@ -92,14 +73,51 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
     M::template across_offsets<true>(lane, off);
 
-    const int tiles = (q_len + TT - 1) / TT, all = tile * NW * 32 < len ? tiles * a.G : 0;
+    // Frames that the tokens of a tile look at, so that tiles which look elsewhere are left out (as many as there is room for;
+    // tiles behind those are taken).
+    __shared__ int reach[2][kReach];
+    const int tiles = (q_len + TT - 1) / TT, t_first = tile * NW * 32, t_last = t_first + NW * 32;
+    if (a.windows) {
+        for (int u0 = wave * 64; u0 < min(tiles * TT, kReach * TT); u0 += NT) {
+            const int u = u0 + lane;
+            int lo = a.T, hi = 0;
+            if (u < q_len) frames_of(a, b, u, len, lo, hi);
+            if (lo >= hi) {
+                lo = a.T;
+                hi = 0;
+            }
+#pragma unroll
+            for (int d = 1; d < TT; d <<= 1) {
+                lo = min(lo, __shfl_xor(lo, d));
+                hi = max(hi, __shfl_xor(hi, d));
+            }
+            if (lane % TT == 0 && u / TT < kReach) {
+                reach[0][u / TT] = lo;
+                reach[1][u / TT] = hi;
+            }
+        }
+        __syncthreads();
+    }
+    // units: tiles of the heads, one head after the other; this workgroup's are those of its part
+    const int units = t_first < len ? tiles * a.G : 0, unit_end = min(units, (part + 1) * a.units_per_part);
+    auto next_from = [&](int i) {  // (uniform) the first unit from i on that has something to look at
+        if (a.windows) {
+            for (; i < unit_end; ++i) {
+                const int at = i % tiles;
+                if (at >= kReach || (reach[0][at] < t_last && reach[1][at] > t_first)) break;
+            }
+        }
+        return __builtin_amdgcn_readfirstlane(i);
+    };
     T qt, gt;
+    typename T::Places at;
+    at.set(a.D, a.U, threadIdx.x);
     float row_lse = 0.f, row_delta = 0.f;
     int row_lo = 0, row_hi = 0;
     auto load = [&](int i) {
         const int g = i / tiles, u0 = (i - g * tiles) * TT, head = kvh * a.G + g;
-        qt.load((const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U, a.D, a.U, u0, threadIdx.x);
-        gt.load((const S *)a.dout + (size_t)b * a.dos + (size_t)head * a.D * a.U, a.D, a.U, u0, threadIdx.x);
+        qt.load((const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U, at, a.U, u0, threadIdx.x);
+        gt.load((const S *)a.dout + (size_t)b * a.dos + (size_t)head * a.D * a.U, at, a.U, u0, threadIdx.x);
         if (threadIdx.x < TT) {
             const int u = u0 + threadIdx.x, uc = min(u, a.U - 1);
             const size_t row = ((size_t)b * a.H + head) * a.U + uc;
@@ -109,9 +127,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
             if (u >= q_len) row_lo = row_hi = 0;
         }
     };
-    if (all > 0) load(0);
-    for (int i = 0; i < all; ++i) {
-        unsigned char *buf = smem + (i & 1) * kBuf;
+    int i = next_from(part * a.units_per_part), turn = 0;
+    if (i < unit_end) load(i);
+    for (int after; i < unit_end; i = after, turn ^= 1) {
+        unsigned char *buf = smem + turn * kBuf;
         Rows &rows = *reinterpret_cast<Rows *>(buf + 2 * T::kBytes);
         const int u0 = (i % tiles) * TT;
         qt.write(buf, a.D, a.U, q_len, u0, threadIdx.x);
@@ -136,7 +155,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
             }
         }
         __syncthreads();
-        if (i + 1 < all) load(i + 1);
+        after = next_from(i + 1);
+        if (after < unit_end) load(after);
         if (w0 >= len) continue;
         if (a.windows && (rows.range[0] >= w0 + 32 || rows.range[1] <= w0)) continue;
 #pragma unroll
@@ -153,11 +173,18 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int u = 32 * n + M::position(r, half);
-                bool ok = there;
-                if (a.windows) ok = ok && t >= rows.lo[u] && t < rows.hi[u];
-                const float p = ok ? probability(s[r], c, rows.lse[u]) : 0.f;
+                const float p = probability(s[r], c, rows.lse[u]);  // (columns beyond the sequence are not stored)
                 s[r] = p;
                 dp[r] = p * (dp[r] - rows.delta[u]);
+            }
+            if (a.windows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int u = 32 * n + M::position(r, half);
+                    const bool ok = t >= rows.lo[u] && t < rows.hi[u];
+                    s[r] = ok ? s[r] : 0.f;
+                    dp[r] = ok ? dp[r] : 0.f;
+                }
             }
             const typename M::Probs pp = M::probs(s), ds = M::probs(dp);
 #pragma unroll
@@ -169,11 +196,37 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     }
     __syncthreads();  // (the tiles give way to the results)
     if (w0 >= a.T) return;
+    const size_t item = (size_t)kvh * a.D * a.T;
+    if (a.parts > 1) {
+        unsigned char *block = smem + wave * DP * 128;
+        const size_t all = (size_t)a.B * a.Hkv * a.D * a.T, to = ((size_t)part * 2 * a.B + b) * a.Hkv * a.D * a.T + item;
+        store_block<float, DP>(block, dk, 1.f, a.kv_part + to, a.D, a.T, w0, len, lane);
+        wave_fence();
+        store_block<float, DP>(block, dv, 1.f, a.kv_part + all + to, a.D, a.T, w0, len, lane);
+        return;
+    }
     unsigned char *block = smem + wave * DP * M::kRow;
-    const size_t at = (size_t)kvh * a.D * a.T;
-    store_block<S, DP>(block, dk, a.scale, (S *)a.dk + (size_t)b * a.dks + at, a.D, a.T, w0, len, lane);
+    store_block<S, DP>(block, dk, a.scale, (S *)a.dk + (size_t)b * a.dks + item, a.D, a.T, w0, len, lane);
     wave_fence();
-    store_block<S, DP>(block, dv, 1.f, (S *)a.dv + (size_t)b * a.dvs + at, a.D, a.T, w0, len, lane);
+    store_block<S, DP>(block, dv, 1.f, (S *)a.dv + (size_t)b * a.dvs + item, a.D, a.T, w0, len, lane);
+}
+
+// Adds the parts of dk and dv, in order.
+template <typename S>
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(AttnArgs a)
+{
+    const size_t item = (size_t)a.Hkv * a.D * a.T, all = item * a.B;
+    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= all) return;
+    float k = 0.f, v = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+        k += a.kv_part[2 * p * all + e];
+        v += a.kv_part[(2 * p + 1) * all + e];
+    }
+    const size_t b = e / item;
+    store_from_f32((S *)a.dk, b * a.dks + (e - b * item), k * a.scale);
+    store_from_f32((S *)a.dv, b * a.dvs + (e - b * item), v);
 }
 
 // ---- dq: a wavefront's columns are tokens, rows are positions; shared and apart as in the forward pass ---------------------
@@ -206,7 +259,6 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         if (lo < hi) {
             lse = a.lse[((size_t)b * a.H + head) * a.U + u] * (0.5f * kLog2e);
             if (lse == -INFINITY) lse = INFINITY;
-            delta = a.delta[((size_t)b * a.H + head) * a.U + u];
         }
     }
     typename M::Frag q[KS], go[KS];
@@ -218,6 +270,11 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             q[s] = M::column(qc, s, half, a.D, a.U, there && lo < hi, a.flip);
             go[s] = M::column(gc, s, half, a.D, a.U, there && lo < hi, 0u);
         }
+        const S *oc = (const S *)a.o + (size_t)b * a.os + at;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) delta += M::dot(M::column(oc, s, half, a.D, a.U, there && lo < hi, 0u), go[s]);
+        delta = half_sum(delta);
+        if (exists && half == 0 && split == 0 && (SHARED || wave == 0)) a.delta[((size_t)b * a.H + head) * a.U + u] = delta;
     }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -226,7 +283,7 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
     }
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
-    const bool active = last > first;
+    const int wave_first = first, wave_last = last;
     if constexpr (SHARED) {  // of the workgroup
         int *range = reinterpret_cast<int *>(smem);
         if (lane == 0) {
@@ -281,10 +338,12 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         }
     };
     T kt, vt;
+    typename T::Places at;
+    at.set(a.D, a.T, SHARED ? threadIdx.x : lane);
     if constexpr (SHARED) {
         if (t_begin < t_end) {
-            kt.load(krows, a.D, a.T, t_begin * TT, threadIdx.x);
-            vt.load(vrows, a.D, a.T, t_begin * TT, threadIdx.x);
+            kt.load(krows, at, a.T, t_begin * TT, threadIdx.x);
+            vt.load(vrows, at, a.T, t_begin * TT, threadIdx.x);
         }
         for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
             unsigned char *buf = smem + turn * 2 * T::kBytes;
@@ -292,17 +351,17 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, threadIdx.x);
             __syncthreads();  // (the other buffer is written next: all are through with it before they pass here again)
             if (t + 1 < t_end) {
-                kt.load(krows, a.D, a.T, (t + 1) * TT, threadIdx.x);
-                vt.load(vrows, a.D, a.T, (t + 1) * TT, threadIdx.x);
+                kt.load(krows, at, a.T, (t + 1) * TT, threadIdx.x);
+                vt.load(vrows, at, a.T, (t + 1) * TT, threadIdx.x);
             }
-            if (active) compute(buf, buf + T::kBytes, t * TT);
+            if (t * TT < wave_last && (t + 1) * TT > wave_first) compute(buf, buf + T::kBytes, t * TT);
         }
     } else {
         unsigned char *buf = smem + wave * 2 * T::kBytes;
         int t = t_begin + wave;
         if (t < t_end) {
-            kt.load(krows, a.D, a.T, t * TT, lane);
-            vt.load(vrows, a.D, a.T, t * TT, lane);
+            kt.load(krows, at, a.T, t * TT, lane);
+            vt.load(vrows, at, a.T, t * TT, lane);
         }
         for (; t < t_end; t += NW) {
             wave_fence();
@@ -310,8 +369,8 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, lane);
             wave_fence();
             if (t + NW < t_end) {
-                kt.load(krows, a.D, a.T, (t + NW) * TT, lane);
-                vt.load(vrows, a.D, a.T, (t + NW) * TT, lane);
+                kt.load(krows, at, a.T, (t + NW) * TT, lane);
+                vt.load(vrows, at, a.T, (t + NW) * TT, lane);
             }
             compute(buf, buf + T::kBytes, t * TT);
         }
@@ -326,6 +385,18 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             store_from_f32((S *)a.dq, (size_t)b * a.dqs + ((size_t)head * a.D + ch) * a.U + u, v * a.scale);
     };
     if constexpr (SHARED) {
+        const int m0 = (ct * NW + wave) * 32, g0 = m0 / a.U, u0 = m0 - g0 * a.U;
+        __syncthreads();  // (the tiles give way to the results)
+        if (m0 >= a.G * a.U) return;
+        if (g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
+            unsigned char *block = smem + wave * DP * (a.splits > 1 ? 128 : M::kRow);
+            const size_t item = (size_t)(kvh * a.G + g0) * a.D * a.U;
+            if (a.splits > 1)
+                store_block<float, DP>(block, acc, 1.f, a.part + ((size_t)split * a.B + b) * a.H * a.D * a.U + item, a.D, a.U, u0, q_len, lane);
+            else
+                store_block<S, DP>(block, acc, a.scale, (S *)a.dq + (size_t)b * a.dqs + item, a.D, a.U, u0, q_len, lane);
+            return;
+        }
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -365,20 +436,21 @@ __global__ __launch_bounds__(256) void attn_dq_join_kernel(AttnArgs a)
 
 // ---- sizes ------------------------------------------------------------------------------------------------------
 constexpr int kWaves = 4;
+constexpr int token_blocks(bool bf16, int DP) { return bf16 && DP <= 96 ? 2 : 1; }  // of a tile of the kernel of dk and dv
 
 template <typename S, int DP>
 hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
-    constexpr int NB = sizeof(S) == 2 && DP <= 96 ? 2 : 1;
+    constexpr int NB = token_blocks(sizeof(S) == 2, DP);
     constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
-    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, bytes = tiles > own ? tiles : own;
+    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, out = kWaves * DP * 128;
+    constexpr int bytes = tiles > own ? (tiles > out ? tiles : out) : (own > out ? own : out);
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
     if (e != hipSuccess) return e;
-    const int per = kWaves * 32;
-    fn<<<dim3((unsigned)(a.B * a.Hkv) * ((a.T + per - 1) / per)), dim3(kWaves * 64), bytes, s>>>(a);
+    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.pos_tiles * a.parts), dim3(kWaves * 64), bytes, s>>>(a);
     return hipGetLastError();
 }
 
@@ -398,7 +470,7 @@ hipError_t run_dq(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
     constexpr int NB = two_blocks(sizeof(S) == 2, DP, SHARED) ? 2 : 1, NT = SHARED ? kWaves * 64 : 64;
-    constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? 0 : kWaves * DP / 32 * 16 * 64 * 4;
+    constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? kWaves * DP * 128 : kWaves * DP / 32 * 16 * 64 * 4;
     constexpr int bytes = tiles > join ? tiles : join;
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dq_kernel<S, DP, NB, kWaves, SHARED>;
@@ -410,36 +482,46 @@ hipError_t run_dq(const AttnArgs &a, hipStream_t s)
 template <typename S, int DP>
 hipError_t run_both(const AttnArgs &a, hipStream_t s)
 {
-    const hipError_t e = run_dkv<S, DP>(a, s);
-    if (e != hipSuccess) return e;
-    if constexpr (sizeof(S) == 2 || DP <= 64) {
-        if (!is_shared(sizeof(S) == 2, DP, (long long)a.G * a.U)) return run_dq<S, DP, false>(a, s);
+    hipError_t e = hipSuccess;
+    if (is_shared(sizeof(S) == 2, DP, (long long)a.G * a.U)) {
+        e = run_dq<S, DP, true>(a, s);
+    } else {
+        if constexpr (sizeof(S) == 2 || DP <= 64) e = run_dq<S, DP, false>(a, s);
     }
-    return run_dq<S, DP, true>(a, s);
+    return e == hipSuccess ? run_dkv<S, DP>(a, s) : e;
 }
 template <typename S>
 hipError_t run_any(const AttnArgs &a, hipStream_t s)
 {
-    attn_delta_kernel<S><<<dim3((unsigned)(a.B * a.H) * ((a.U + 31) / 32)), dim3(256), 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    hipError_t e;
     if (a.D <= 32) e = run_both<S, 32>(a, s);
     else if (a.D <= 64) e = run_both<S, 64>(a, s);
     else if (a.D <= 96) e = run_both<S, 96>(a, s);
     else e = run_both<S, 128>(a, s);
-    if (e != hipSuccess || a.splits == 1) return e;
-    attn_dq_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
+    if (e != hipSuccess) return e;
+    if (a.splits > 1) attn_dq_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
+    if (a.parts > 1) attn_dkv_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.Hkv * a.T * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
+
+// a unit of the kernel of dk and dv, in microseconds at 64 tokens and channels
+constexpr double kUnitUs = 2.0;
 
 AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
 {
     const int DP = (D + 31) / 32 * 32;
     const long long columns = (long long)(H / Hkv) * U;
     const Form f = form_of(bf16, DP, columns);
-    return attn_plan(f.columns, f.tile, f.waves, B, H, Hkv, D, U, T);
+    AttnPlan p = attn_plan(f.columns, f.tile, f.waves, B, H, Hkv, D, U, T);
+    // dk and dv: units of a tile of tokens of a head
+    const int per = kWaves * 32, tokens = 32 * token_blocks(bf16, DP), units = (U + tokens - 1) / tokens * (H / Hkv);
+    p.pos_tiles = (T + per - 1) / per;
+    p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D);
+    p.parts = (units + p.units_per_part - 1) / p.units_per_part;
+    p.kv_part_bytes = p.parts > 1 ? (size_t)p.parts * 2 * B * Hkv * D * T * sizeof(float) : 0;
+    return p;
 }
 
 hipError_t launch_attn_bwd(bool bf16, const AttnArgs &a, hipStream_t s) { return bf16 ? run_any<bf16_t>(a, s) : run_any<float>(a, s); }

@@ -16,7 +16,9 @@
 namespace nm {
 namespace {
 
-template <typename S, int DP, int NU, int NB, int NW, bool SHARED>
+constexpr float kLag = 8.f;
+
+template <typename S, int DP, int NB, int NW, bool SHARED>
 __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
@@ -31,29 +33,23 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
     const S *krows = (const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T;
     const S *vrows = (const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T;
 
-    // columns of this lane
-    int head[NU], u[NU], lo[NU], hi[NU];
-    bool exists[NU], there[NU];
-    typename M::Frag q[NU][KS];
-    int first = a.T, last = 0;  // frames that some column may look at
+    // this lane's column
+    const int m = (SHARED ? ct * NW + wave : ct) * 32 + (lane & 31);
+    const bool exists = m < a.G * a.U;
+    const int g = exists ? m / a.U : 0, u = exists ? m - g * a.U : 0, head = kvh * a.G + g;
+    const bool there = exists && u < q_len;
+    int lo = 0, hi = 0x7fffffff;  // a column that is not there is masked nowhere: it must not slow the others down
+    int first = a.T, last = 0;    // frames that some column may look at
+    if (there) {
+        frames_of(a, b, u, len, lo, hi);
+        first = lo;
+        last = hi;
+    }
+    typename M::Frag q[KS];
+    {
+        const S *col = (const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U + u;
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        const int m = (SHARED ? (ct * NW + wave) * NU + i : ct * NU + i) * 32 + (lane & 31);
-        exists[i] = m < a.G * a.U;
-        const int g = exists[i] ? m / a.U : 0;
-        u[i] = exists[i] ? m - g * a.U : 0;
-        head[i] = kvh * a.G + g;
-        there[i] = exists[i] && u[i] < q_len;
-        lo[i] = 0;
-        hi[i] = 0x7fffffff;  // a column that is not there is masked nowhere: it must not slow the others down
-        if (there[i]) {
-            frames_of(a, b, u[i], len, lo[i], hi[i]);
-            first = min(first, lo[i]);
-            last = max(last, hi[i]);
-        }
-        const S *col = (const S *)a.q + (size_t)b * a.qs + (size_t)head[i] * a.D * a.U + u[i];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) q[i][s] = M::column(col, s, half, a.D, a.U, there[i], a.flip);
+        for (int s = 0; s < KS; ++s) q[s] = M::column(col, s, half, a.D, a.U, there, a.flip);
     }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -79,88 +75,78 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
     }
     int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
 
-    float mx[NU], sum[NU];  // in powers of two, and of this lane's positions
-    f32x16_t acc[NU][DP / 32];
+    float mx = -INFINITY, sum = 0.f;  // in powers of two, and of this lane's positions
+    f32x16_t acc[DP / 32];
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        mx[i] = -INFINITY;
-        sum[i] = 0.f;
+    for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.f;
-    }
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
     int koff[2];
     M::template across_offsets<true>(lane, koff);
 
     auto compute = [&](const unsigned char *kt, const unsigned char *vt, int t0) {
-        f32x16_t s[NU][NB];
+        f32x16_t s[NB];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int i = 0; i < NU; ++i)
+            for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[i][n][r] = 0.f;
+        for (int st = 0; st < KS; ++st)
 #pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                const typename M::Frag f = M::across(kt + n * T::kBlock, koff, st);
-#pragma unroll
-                for (int i = 0; i < NU; ++i) s[i][n] = M::mul(f, q[i][st], s[i][n]);
-            }
-        }
-        typename M::Probs p[NU][NB];
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            if (!__all(lo[i] <= t0 && t0 + TT <= hi[i])) {
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int t = t0 + 32 * n + M::position(r, half);
-                        s[i][n][r] = t >= lo[i] && t < hi[i] ? s[i][n][r] : -INFINITY;
-                    }
-            }
-            float top = s[i][0][0];
+            for (int n = 0; n < NB; ++n) s[n] = M::mul(M::across(kt + n * T::kBlock, koff, st), q[st], s[n]);
+        if (!__all(lo <= t0 && t0 + TT <= hi)) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][n][r]);
-            top = fmaxf(mx[i], half_max(top) * a.c);
-            const float base = top == -INFINITY ? 0.f : top;  // (nothing allowed so far: every probability is zero)
-            if (!__all(top == mx[i])) {
-                const float shrink = __builtin_amdgcn_exp2f(mx[i] - base);
-                sum[i] *= shrink;
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[i][d][r] *= shrink;
-                mx[i] = top;
-            }
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-#pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[i][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][n][r], a.c, -base));
-                    sum[i] += s[i][n][r];
+                    const int t = t0 + 32 * n + M::position(r, half);
+                    s[n][r] = t >= lo && t < hi ? s[n][r] : -INFINITY;
                 }
-                p[i][n] = M::probs(s[i][n]);
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+        top = half_max(top) * a.c;
+        // The base that sums are taken to follows the maximum only where that has grown by kLag powers of two: probabilities up to
+        // 2^kLag do no harm, and multiplying what has been added so far is a third of the work otherwise.
+        if (__any(top > mx + kLag)) {
+            top = fmaxf(top, mx);
+            const float shrink = __builtin_amdgcn_exp2f(mx - (top == -INFINITY ? 0.f : top));
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[d][r] *= shrink;
+            mx = top;
+        }
+        const float base = mx == -INFINITY ? 0.f : mx;  // (nothing allowed so far: every probability is zero)
+        typename M::Probs p[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            float part = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.c, -base));
+                part += s[n][r];
             }
+            sum += part;
+            p[n] = M::probs(s[n]);
         }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) {
-                const typename M::Along f = M::along(vt + n * T::kBlock, d * 32, lane);
-#pragma unroll
-                for (int i = 0; i < NU; ++i) acc[i][d] = M::mul(f, p[i][n], acc[i][d]);
-            }
+            for (int d = 0; d < DP / 32; ++d) acc[d] = M::mul(M::along(vt + n * T::kBlock, d * 32, lane), p[n], acc[d]);
     };
 
     T kt, vt;
+    typename T::Places at;
+    at.set(a.D, a.T, SHARED ? threadIdx.x : lane);
     if constexpr (SHARED) {
         if (t_begin < t_end) {
-            kt.load(krows, a.D, a.T, t_begin * TT, threadIdx.x);
-            vt.load(vrows, a.D, a.T, t_begin * TT, threadIdx.x);
+            kt.load(krows, at, a.T, t_begin * TT, threadIdx.x);
+            vt.load(vrows, at, a.T, t_begin * TT, threadIdx.x);
         }
         for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
             unsigned char *buf = smem + turn * 2 * T::kBytes;
@@ -168,8 +154,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, threadIdx.x);
             __syncthreads();  // (the other buffer is written next: all are through with it before they pass here again)
             if (t + 1 < t_end) {
-                kt.load(krows, a.D, a.T, (t + 1) * TT, threadIdx.x);
-                vt.load(vrows, a.D, a.T, (t + 1) * TT, threadIdx.x);
+                kt.load(krows, at, a.T, (t + 1) * TT, threadIdx.x);
+                vt.load(vrows, at, a.T, (t + 1) * TT, threadIdx.x);
             }
             if (active) compute(buf, buf + T::kBytes, t * TT);
         }
@@ -177,8 +163,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
         unsigned char *buf = smem + wave * 2 * T::kBytes;
         int t = t_begin + wave;
         if (t < t_end) {
-            kt.load(krows, a.D, a.T, t * TT, lane);
-            vt.load(vrows, a.D, a.T, t * TT, lane);
+            kt.load(krows, at, a.T, t * TT, lane);
+            vt.load(vrows, at, a.T, t * TT, lane);
         }
         for (; t < t_end; t += NW) {
             wave_fence();
@@ -186,109 +172,124 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, lane);
             wave_fence();
             if (t + NW < t_end) {
-                kt.load(krows, a.D, a.T, (t + NW) * TT, lane);
-                vt.load(vrows, a.D, a.T, (t + NW) * TT, lane);
+                kt.load(krows, at, a.T, (t + NW) * TT, lane);
+                vt.load(vrows, at, a.T, (t + NW) * TT, lane);
             }
             compute(buf, buf + T::kBytes, t * TT);
         }
     }
 
-    // one value per (column, channel) and its place
-    auto put = [&](int i, int d, int r, float v, float mx_all, float sum_all) {
+    // one value per (column, channel) and its place; sum_all: of the column
+    auto put = [&](int d, int r, float v, float sum_all) {
         const int ch = d * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-        if (!exists[i] || ch >= a.D) return;
+        if (!exists || ch >= a.D) return;
         if (a.splits > 1) {
-            a.part[(((size_t)split * a.B + b) * a.H + head[i]) * a.D * a.U + (size_t)ch * a.U + u[i]] = v;
+            a.part[(((size_t)split * a.B + b) * a.H + head) * a.D * a.U + (size_t)ch * a.U + u] = there ? v : 0.f;
         } else {
             const float inv = sum_all == 0.f ? 0.f : 1.f / sum_all;
-            store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)head[i] * a.D + ch) * a.U + u[i], there[i] ? v * inv : 0.f);
+            store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)head * a.D + ch) * a.U + u, there ? v * inv : 0.f);
         }
     };
-    auto put_sums = [&](int i, float mx_all, float sum_all) {
-        if (!exists[i] || half) return;
-        const size_t row = ((size_t)b * a.H + head[i]) * a.U + u[i];
+    auto put_sums = [&](float mx_all, float sum_all) {
+        if (!exists || half) return;
+        const size_t row = ((size_t)b * a.H + head) * a.U + u;
         if (a.splits > 1) {
             float *ml = a.part_ml + ((size_t)split * a.B * a.H * a.U + row) * 2;
-            ml[0] = there[i] ? mx_all : -INFINITY;
-            ml[1] = there[i] ? sum_all : 0.f;
+            ml[0] = there ? mx_all : -INFINITY;
+            ml[1] = there ? sum_all : 0.f;
         } else if (a.lse) {
-            a.lse[row] = there[i] && sum_all != 0.f ? (mx_all + __builtin_amdgcn_logf(sum_all)) * 0.69314718055994531f : -INFINITY;
+            a.lse[row] = there && sum_all != 0.f ? (mx_all + __builtin_amdgcn_logf(sum_all)) * 0.69314718055994531f : -INFINITY;
         }
     };
     if constexpr (SHARED) {
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const float total = half_sum(sum[i]);
-            put_sums(i, mx[i], total);
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) put(i, d, r, acc[i][d][r], mx[i], total);
+        __syncthreads();  // (the tiles give way to the results)
+        const float total = half_sum(sum);
+        put_sums(mx, total);
+        const int m0 = (ct * NW + wave) * 32, g0 = m0 / a.U, u0 = m0 - g0 * a.U;
+        if (m0 >= a.G * a.U) return;
+        if (g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
+            unsigned char *block = smem + wave * DP * (a.splits > 1 ? 128 : M::kRow);
+            const size_t item = (size_t)(kvh * a.G + g0) * a.D * a.U;
+            if (a.splits > 1)
+                store_block<float, DP>(block, acc, 1.f, a.part + ((size_t)split * a.B + b) * a.H * a.D * a.U + item, a.D, a.U, u0, q_len, lane);
+            else
+                store_block<S, DP>(block, acc, total == 0.f ? 0.f : 1.f / total, (S *)a.out + (size_t)b * a.os + item, a.D, a.U, u0, q_len, lane);
+            return;
         }
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) put(d, r, acc[d][r], total);
     } else {
-        // joined through LDS: every wavefront's maxima and sums, then its products, one column block after the other
+        // joined through LDS: every wavefront's maxima and sums, and its products
         constexpr int PAIRS = DP / 32 * 16;
-        float *sums = reinterpret_cast<float *>(smem);            // [NW][2][64]
-        float *prod = sums + NW * 128;                            // [NW][PAIRS][64]
+        float *sums = reinterpret_cast<float *>(smem);  // [NW][2][64]
+        float *prod = sums + NW * 128;                  // [NW][PAIRS][64]
+        __syncthreads();
+        sums[wave * 128 + lane] = mx;
+        sums[wave * 128 + 64 + lane] = half_sum(sum);
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            __syncthreads();
-            sums[wave * 128 + lane] = mx[i];
-            sums[wave * 128 + 64 + lane] = half_sum(sum[i]);
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
+            for (int r = 0; r < 16; ++r) prod[(wave * PAIRS + d * 16 + r) * 64 + lane] = acc[d][r];
+        __syncthreads();
+        float top = -INFINITY, total = 0.f, weight[NW];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) prod[(wave * PAIRS + d * 16 + r) * 64 + lane] = acc[i][d][r];
-            __syncthreads();
-            float top = -INFINITY, total = 0.f, weight[NW];
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, sums[w * 128 + lane]);
 #pragma unroll
-            for (int w = 0; w < NW; ++w) top = fmaxf(top, sums[w * 128 + lane]);
+        for (int w = 0; w < NW; ++w) {
+            weight[w] = __builtin_amdgcn_exp2f(sums[w * 128 + lane] - (top == -INFINITY ? 0.f : top));
+            total += weight[w] * sums[w * 128 + 64 + lane];
+        }
+        if (wave == 0) put_sums(top, total);
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                weight[w] = __builtin_amdgcn_exp2f(sums[w * 128 + lane] - (top == -INFINITY ? 0.f : top));
-                total += weight[w] * sums[w * 128 + 64 + lane];
-            }
-            if (wave == 0) put_sums(i, top, total);
+        for (int n = 0; n < PAIRS / NW; ++n) {
+            const int pair = n * NW + wave;
+            float v = 0.f;
 #pragma unroll
-            for (int n = 0; n < PAIRS / NW; ++n) {
-                const int pair = n * NW + wave;
-                float v = 0.f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) v += weight[w] * prod[(w * PAIRS + pair) * 64 + lane];
-                put(i, pair / 16, pair % 16, v, top, total);
-            }
+            for (int w = 0; w < NW; ++w) v += weight[w] * prod[(w * PAIRS + pair) * 64 + lane];
+            put(pair / 16, pair % 16, v, total);
         }
     }
 }
 
-// Joins the sums of `splits` workgroups, in order.
+// Joins the sums of `splits` workgroups, in order: a workgroup takes 64 tokens of a head, whose weights lie in LDS, and 32 channels.
 template <typename S>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    const size_t rows = (size_t)a.B * a.H * a.U, all = rows * a.D;
-    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= all) return;
-    const int u = (int)(e % a.U);
-    const size_t hd = e / a.U, bh = hd / a.D;
-    const int d = (int)(hd - bh * a.D), b = (int)(bh / a.H), h = (int)(bh - (size_t)b * a.H);
-    const size_t row = bh * a.U + u;
-    float top = -INFINITY, total = 0.f, v = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[(s * rows + row) * 2]);
-    const float base = top == -INFINITY ? 0.f : top;
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[(s * rows + row) * 2] - base);
-        total += w * a.part_ml[(s * rows + row) * 2 + 1];
-        v += w * a.part[s * all + e];
+    __shared__ float weight[kMaxSplits][64];
+    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
+    const int tiles = (a.U + 63) / 64, bh = blockIdx.x / tiles, u = (blockIdx.x - bh * tiles) * 64 + lane;
+    const int b = bh / a.H, h = bh - b * a.H;
+    const size_t rows = (size_t)a.B * a.H * a.U, all = rows * a.D, row = (size_t)bh * a.U + min(u, a.U - 1);
+    if (share == 0) {
+        float top = -INFINITY, total = 0.f;
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[(s * rows + row) * 2]);
+        const float base = top == -INFINITY ? 0.f : top;
+        for (int s = 0; s < a.splits; ++s) {
+            const float w = __builtin_amdgcn_exp2f(a.part_ml[(s * rows + row) * 2] - base);
+            weight[s][lane] = w;
+            total += w * a.part_ml[(s * rows + row) * 2 + 1];
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        for (int s = 0; s < a.splits; ++s) weight[s][lane] *= inv;
+        if (a.lse && u < a.U && blockIdx.y == 0) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f : -INFINITY;
     }
-    store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)h * a.D + d) * a.U + u, total == 0.f ? 0.f : v / total);
-    if (a.lse && d == 0) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f : -INFINITY;
+    __syncthreads();
+    if (u >= a.U) return;
+    for (int d = blockIdx.y * 32 + share; d < min(a.D, (int)blockIdx.y * 32 + 32); d += 4) {
+        const size_t e = ((size_t)bh * a.D + d) * a.U + u;
+        float v = 0.f;
+        for (int s = 0; s < a.splits; ++s) v += weight[s][lane] * a.part[s * all + e];
+        store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)h * a.D + d) * a.U + u, v);
+    }
 }
 
 // ---- which form, and its sizes --------------------------------------------------------------------------------
-template <typename S, int DP, int NU, int NB, int NW, bool SHARED>
+template <typename S, int DP, int NB, int NW, bool SHARED>
 constexpr int lds_bytes()
 {
-    if constexpr (SHARED) return 4 * Tile<S, DP, NB, NW * 64>::kBytes;
+    if constexpr (SHARED) return 4 * Tile<S, DP, NB, NW * 64>::kBytes;  // (results of NW wavefronts fit: float blocks of 32)
     constexpr int tiles = NW * 2 * Tile<S, DP, NB, 64>::kBytes, join = NW * 128 * 4 + NW * (DP / 32 * 16) * 64 * 4;
     return tiles > join ? tiles : join;
 }
@@ -296,13 +297,13 @@ constexpr int lds_bytes()
 struct Form {
     int columns, tile, waves;  // of a workgroup: tokens, positions of a tile, wavefronts with tiles of their own
 };
-template <typename S, int DP, int NU, int NB, int NW, bool SHARED>
+template <typename S, int DP, int NB, int NW, bool SHARED>
 hipError_t run(AttnArgs a, hipStream_t s)
 {
     static LdsOptIn opt;
-    constexpr int bytes = lds_bytes<S, DP, NU, NB, NW, SHARED>();
+    constexpr int bytes = lds_bytes<S, DP, NB, NW, SHARED>();
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
-    auto *fn = attn_fwd_kernel<S, DP, NU, NB, NW, SHARED>;
+    auto *fn = attn_fwd_kernel<S, DP, NB, NW, SHARED>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
     if (e != hipSuccess) return e;
     fn<<<dim3((unsigned)(a.B * a.Hkv) * a.col_tiles * a.splits), dim3(NW * 64), bytes, s>>>(a);
@@ -314,8 +315,7 @@ Form form_of(bool bf16, int DP, long long columns)
 {
     // (float tiles of wide heads, one per wavefront, do not fit the registers)
     if (columns <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, 4};
-    if (!bf16) return {128, 32, 1};
-    return columns <= 128 || DP > 64 ? Form{128, 64, 1} : Form{256, 64, 1};
+    return {128, bf16 ? 64 : 32, 1};
 }
 
 template <typename S, int DP>
@@ -324,12 +324,9 @@ hipError_t run_form(const AttnArgs &a, hipStream_t s)
     constexpr bool bf16 = sizeof(S) == 2;
     const Form f = form_of(bf16, DP, (long long)a.G * a.U);
     if constexpr (bf16 || DP <= 64) {
-        if (f.columns == 32) return run<S, DP, 1, bf16 && DP <= 64 ? 2 : 1, 4, false>(a, s);
+        if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, 4, false>(a, s);
     }
-    if constexpr (bf16 && DP <= 64) {
-        if (f.columns == 256) return run<S, DP, 2, 2, 4, true>(a, s);
-    }
-    return run<S, DP, 1, bf16 ? 2 : 1, 4, true>(a, s);
+    return run<S, DP, bf16 ? 2 : 1, 4, true>(a, s);
 }
 template <typename S>
 hipError_t run_any(const AttnArgs &a, hipStream_t s)
@@ -340,7 +337,7 @@ hipError_t run_any(const AttnArgs &a, hipStream_t s)
     else if (a.D <= 96) e = run_form<S, 96>(a, s);
     else e = run_form<S, 128>(a, s);
     if (e != hipSuccess || a.splits == 1) return e;
-    attn_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
+    attn_join_kernel<S><<<dim3((unsigned)(a.B * a.H) * ((a.U + 63) / 64), (a.D + 31) / 32), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -71,7 +71,7 @@ struct Mma<bf16_t> {
     // the same operand of 32 columns straight from memory: channels of the lane's column p, `pitch` elements apart (a head's
     // rows span less than 4 GiB); zeros unless `there`.  Every load is made, from a channel that exists: a branch around each is what
     // the call would wait for.
-    static __device__ __forceinline__ Frag column(const bf16_t *p, int step, int half, int D, uint32_t pitch, bool there, uint32_t flip)
+    static __device__ __forceinline__ Frag column(const bf16_t *p, int step, int half, int D, uint32_t pitch, bool there)
     {
         bf16_t e[8];
         uint32_t w[4];
@@ -80,12 +80,20 @@ struct Mma<bf16_t> {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = 16 * step + 8 * half + 2 * j;
-            w[j] = ((uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16) ^ (flip | flip >> 16);
+            w[j] = (uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16;
             w[j] &= !there || d >= D ? 0u : (d + 1 < D ? 0xffffffffu : 0xffffu);
         }
         return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
     }
     static __device__ __forceinline__ f32x16_t mul(Frag a, Frag b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Frag flipped(Frag a, uint32_t flip)
+    {
+        const uint32_t both = flip | flip >> 16;
+        u32x4_t w = __builtin_bit_cast(u32x4_t, a);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] ^= both;
+        return __builtin_bit_cast(bf16x8_t, w);
+    }
     static __device__ __forceinline__ float dot(Frag a, Frag b)
     {
         float t = 0.f;
@@ -147,13 +155,14 @@ struct Mma<float> {
     {
         return *reinterpret_cast<const float *>(block + off[0] + (off[1] ^ ((step & 7) << 4)) + step * 2 * kRow);
     }
-    static __device__ __forceinline__ Frag column(const float *p, int step, int half, int D, uint32_t pitch, bool there, uint32_t flip)
+    static __device__ __forceinline__ Frag column(const float *p, int step, int half, int D, uint32_t pitch, bool there)
     {
         const int d = 2 * step + half;
         const float v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p) + (size_t)((uint32_t)min(d, D - 1) * pitch * 4u));
-        return there && d < D ? __uint_as_float(__float_as_uint(v) ^ flip) : 0.f;
+        return there && d < D ? v : 0.f;
     }
     static __device__ __forceinline__ f32x16_t mul(Frag a, Frag b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Frag flipped(Frag a, uint32_t flip) { return __uint_as_float(__float_as_uint(a) ^ flip); }
     static __device__ __forceinline__ float dot(Frag a, Frag b) { return a * b; }
     static __device__ __forceinline__ Probs probs(const f32x16_t &p) { return p; }
     struct Along {
@@ -197,8 +206,7 @@ struct Tile {
     static constexpr int kBlock = DP * M::kRow + (NB > 1 ? 128 : 0);  // (blocks side by side begin at other banks)
     static constexpr int kBytes = NB * kBlock;
     static constexpr int kPerRow = NB * M::kRow / 16;  // granules
-    static constexpr int kCount = DP * kPerRow / NT;
-    static_assert(DP * kPerRow % NT == 0, "whole granules per thread");
+    static constexpr int kAll = DP * kPerRow, kCount = (kAll + NT - 1) / NT;  // (beyond the last granule a thread loads a row that is there)
 
     // A thread's places in the tiles of a sequence: byte offsets from channel 0 of a tile's first position, in 32 bits beside a base
     // that all threads share (a head's rows span less than 4 GiB).  Sequences of equal shape have the same.
@@ -260,7 +268,7 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int e = i * NT + thread, row = e / kPerRow, gi = e % kPerRow;
-            *reinterpret_cast<u32x4_t *>(tile + (gi / GB) * kBlock + M::granule(row, gi % GB)) = r[i];
+            if (kAll % NT == 0 || e < kAll) *reinterpret_cast<u32x4_t *>(tile + (gi / GB) * kBlock + M::granule(row, gi % GB)) = r[i];
         }
     }
 };
@@ -328,8 +336,35 @@ struct AttnArgs {
     float *part, *part_ml;  // sums of the workgroups that share tokens, their maxima and sums
     float *delta;           // [B][H][U]
     int col_tiles, splits, tiles_per_split;
+    int head_tiles;  // column tiles of a head, or 0: tiles run over the heads that share keys and values
     float *kv_part;  // [parts][2][B][Hkv][D][T]: sums of the workgroups that share positions
     int pos_tiles, parts, units_per_part;
+};
+
+// A workgroup's NW blocks of a head's tokens or positions as operands of its wavefronts, through LDS (`smem`).  All that a kernel wants
+// is loaded before the first is taken: taking waits.
+template <typename S, int DP, int NW>
+struct OwnColumns {
+    typedef Tile<S, DP, NW, NW * 64> Own;
+    typedef Mma<S> M;
+    Own own;
+    __device__ __forceinline__ void load(const S *rows, int D, int len, int t0)
+    {
+        typename Own::Places at;
+        at.set(D, len, threadIdx.x);
+        own.load(rows, at, len, t0, threadIdx.x);
+    }
+    template <int KS>
+    __device__ __forceinline__ void take(unsigned char *smem, int D, int len, int valid, int t0, int wave, int lane, typename M::Frag (&f)[KS])
+    {
+        int off[2];
+        M::template across_offsets<false>(lane, off);
+        own.write(smem, D, len, valid, t0, threadIdx.x);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) f[s] = M::across(smem + wave * Own::kBlock, off, s);
+        __syncthreads();
+    }
 };
 
 // The frames a token may look at, [lo, hi).

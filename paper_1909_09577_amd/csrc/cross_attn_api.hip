@@ -8,10 +8,9 @@ namespace nm {
 // of the estimates below, in microseconds: a round of 64 positions at 64 channels, what comes before and after the rounds, a second launch
 constexpr double kRoundUs = 1.2, kStartUs = 3.0, kJoinUs = 4.0;
 
-// Two workgroups run on a CU, so that `slots` go on at a time.
-int attn_share(long long groups, int rounds, double round_us, double join_bytes)
+int attn_share(long long groups, int rounds, double round_us, double join_bytes, int per_cu)
 {
-    const long long slots = 512;
+    const long long slots = 256LL * per_cu;
     double best = 0;
     int per = rounds;
     for (int n = 1; n <= rounds && n <= kMaxSplits; ++n) {
@@ -26,15 +25,19 @@ int attn_share(long long groups, int rounds, double round_us, double join_bytes)
     return per;
 }
 
-// A workgroup takes rounds of `waves` tiles.
-AttnPlan attn_plan(int columns, int tile, int waves, int B, int H, int Hkv, int D, int U, int T)
+AttnPlan attn_plan(const AttnForm &f, int B, int H, int Hkv, int D, int U, int T)
 {
     AttnPlan p = {};
-    p.col_tiles = (int)(((long long)(H / Hkv) * U + columns - 1) / columns);
-    const int tiles = (T + tile - 1) / tile, rounds = (tiles + waves - 1) / waves;
-    const int per = attn_share((long long)B * Hkv * p.col_tiles, rounds, kRoundUs * D / 64 * tile / 64, 2.0 * 4 * B * H * U * D);
+    const int columns = f.columns;
+    // Tiles of one head have their tokens side by side in memory, which are then read in 16-byte groups; where they would be less than
+    // two thirds full, tiles run over the heads.
+    const int G = H / Hkv, head_tiles = (U + columns - 1) / columns;
+    p.head_tiles = G == 1 || 3LL * U >= 2LL * head_tiles * columns ? head_tiles : 0;
+    p.col_tiles = p.head_tiles ? G * head_tiles : (int)(((long long)G * U + columns - 1) / columns);
+    const int tiles = (T + f.tile - 1) / f.tile, rounds = (tiles + f.waves - 1) / f.waves;
+    const int per = attn_share((long long)B * Hkv * p.col_tiles, rounds, kRoundUs * D / 64 * f.tile / 64, 2.0 * 4 * B * H * U * D, f.per_cu);
     p.splits = (rounds + per - 1) / per;
-    p.tiles_per_split = per * waves;
+    p.tiles_per_split = per * f.waves;
     const size_t rows = (size_t)B * H * U;
     p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * rows * D * sizeof(float), 256) : 0;
     p.ml_bytes = p.splits > 1 ? align_up((size_t)p.splits * rows * 2 * sizeof(float), 256) : 0;
@@ -148,7 +151,7 @@ int nm_cross_attn_fwd(int B, int heads, int kv_heads, int D, int U, int T, const
     a.out = o; a.os = o_stride; a.lse = lse;
     a.part = (float *)workspace;
     a.part_ml = (float *)((char *)workspace + p.part_bytes);
-    a.col_tiles = p.col_tiles; a.splits = p.splits; a.tiles_per_split = p.tiles_per_split;
+    a.col_tiles = p.col_tiles; a.head_tiles = p.head_tiles; a.splits = p.splits; a.tiles_per_split = p.tiles_per_split;
     return dev(launch_attn_fwd(dtype == NM_BF16, a, (hipStream_t)hip_stream));
 }
 
@@ -190,7 +193,7 @@ int nm_cross_attn_bwd(int B, int heads, int kv_heads, int D, int U, int T, const
     a.part = (float *)((char *)workspace + delta_bytes);
     a.kv_part = (float *)((char *)workspace + delta_bytes + p.part_bytes);
     a.pos_tiles = p.pos_tiles; a.parts = p.parts; a.units_per_part = p.units_per_part;
-    a.col_tiles = p.col_tiles; a.splits = p.splits; a.tiles_per_split = p.tiles_per_split;
+    a.col_tiles = p.col_tiles; a.head_tiles = p.head_tiles; a.splits = p.splits; a.tiles_per_split = p.tiles_per_split;
     return dev(launch_attn_bwd(dtype == NM_BF16, a, (hipStream_t)hip_stream));
 }
 

@@ -46,37 +46,22 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
     const int w0 = (tile * NW + wave) * 32, t = w0 + (lane & 31);
     const float c = (a.flip ? -0.5f : 0.5f) * a.c;
-
-    int off[2];
+    const int t_first = tile * NW * 32, t_last = t_first + NW * 32;
     typename M::Frag kf[KS], vf[KS];
-    if (tile * NW * 32 < len) {  // (uniform) the workgroup's positions of k and v go through LDS once
-        typedef Tile<S, DP, NW, NT> Own;
-        Own own;
-        typename Own::Places at;
-        at.set(a.D, a.T, threadIdx.x);
-        M::template across_offsets<false>(lane, off);
-        auto fetch = [&](const S *rows, typename M::Frag (&f)[KS]) {
-            own.load(rows, at, a.T, tile * NW * 32, threadIdx.x);
-            own.write(smem, a.D, a.T, len, tile * NW * 32, threadIdx.x);
-            __syncthreads();
-#pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = M::across(smem + wave * Own::kBlock, off, s);
-            __syncthreads();
-        };
-        fetch((const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T, kf);
-        fetch((const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T, vf);
+    OwnColumns<S, DP, NW> k_own, v_own;
+    if (t_first < len) {  // (uniform)
+        k_own.load((const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T, a.D, a.T, t_first);
+        v_own.load((const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T, a.D, a.T, t_first);
     }
     f32x16_t dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
-    M::template across_offsets<true>(lane, off);
-
     // Frames that the tokens of a tile look at, so that tiles which look elsewhere are left out (as many as there is room for;
     // tiles behind those are taken).
     __shared__ int reach[2][kReach];
-    const int tiles = (q_len + TT - 1) / TT, t_first = tile * NW * 32, t_last = t_first + NW * 32;
+    const int tiles = (q_len + TT - 1) / TT;
     if (a.windows) {
         for (int u0 = wave * 64; u0 < min(tiles * TT, kReach * TT); u0 += NT) {
             const int u = u0 + lane;
@@ -129,6 +114,12 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     };
     int i = next_from(part * a.units_per_part), turn = 0;
     if (i < unit_end) load(i);
+    if (t_first < len) {
+        k_own.take(smem, a.D, a.T, len, t_first, wave, lane, kf);
+        v_own.take(smem, a.D, a.T, len, t_first, wave, lane, vf);
+    }
+    int off[2];
+    M::template across_offsets<true>(lane, off);
     for (int after; i < unit_end; i = after, turn ^= 1) {
         unsigned char *buf = smem + turn * kBuf;
         Rows &rows = *reinterpret_cast<Rows *>(buf + 2 * T::kBytes);
@@ -245,9 +236,22 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
     const S *krows = (const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T;
     const S *vrows = (const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T;
 
-    const int m = (SHARED ? ct * NW + wave : ct) * 32 + (lane & 31);
-    const bool exists = m < a.G * a.U;
-    const int g = exists ? m / a.U : 0, u = exists ? m - g * a.U : 0, head = kvh * a.G + g;
+    // this lane's column
+    const int block = SHARED ? wave : 0;
+    int g, u;
+    bool exists;
+    if (a.head_tiles) {
+        g = ct / a.head_tiles;
+        u = ((ct - g * a.head_tiles) * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        exists = u < a.U;
+    } else {
+        const int m = (ct * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        exists = m < a.G * a.U;
+        g = exists ? m / a.U : 0;
+        u = m - g * a.U;
+    }
+    if (!exists) u = 0;
+    const int head = kvh * a.G + g;
     const bool there = exists && u < q_len;
     const float half_c = 0.5f * a.c;
     int lo = 0, hi = 0x7fffffff, first = a.T, last = 0;
@@ -260,21 +264,6 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             lse = a.lse[((size_t)b * a.H + head) * a.U + u] * (0.5f * kLog2e);
             if (lse == -INFINITY) lse = INFINITY;
         }
-    }
-    typename M::Frag q[KS], go[KS];
-    {
-        const size_t at = (size_t)head * a.D * a.U + u;
-        const S *qc = (const S *)a.q + (size_t)b * a.qs + at, *gc = (const S *)a.dout + (size_t)b * a.dos + at;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            q[s] = M::column(qc, s, half, a.D, a.U, there && lo < hi, a.flip);
-            go[s] = M::column(gc, s, half, a.D, a.U, there && lo < hi, 0u);
-        }
-        const S *oc = (const S *)a.o + (size_t)b * a.os + at;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) delta += M::dot(M::column(oc, s, half, a.D, a.U, there && lo < hi, 0u), go[s]);
-        delta = half_sum(delta);
-        if (exists && half == 0 && split == 0 && (SHARED || wave == 0)) a.delta[((size_t)b * a.H + head) * a.U + u] = delta;
     }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -299,6 +288,50 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         __syncthreads();
     }
     const int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+
+    // the first tiles and the tokens are loaded together
+    T kt, vt;
+    typename T::Places at;
+    const int loader = SHARED ? threadIdx.x : lane, t_mine = SHARED ? t_begin : t_begin + wave;
+    at.set(a.D, a.T, loader);
+    if (t_mine < t_end) {
+        kt.load(krows, at, a.T, t_mine * TT, loader);
+        vt.load(vrows, at, a.T, t_mine * TT, loader);
+    }
+    typename M::Frag q[KS], go[KS];
+    {
+        const size_t item = (size_t)head * a.D * a.U;
+        const S *qr = (const S *)a.q + (size_t)b * a.qs + item, *gr = (const S *)a.dout + (size_t)b * a.dos + item;
+        const S *orow = (const S *)a.o + (size_t)b * a.os + item;
+        bool taken = false;
+        if constexpr (SHARED) {
+            if (a.head_tiles) {  // (uniform)
+                const int u0 = (ct - g * a.head_tiles) * NW * 32;
+                OwnColumns<S, DP, NW> q_own, g_own, o_own;
+                o_own.load(orow, a.D, a.U, u0);
+                g_own.load(gr, a.D, a.U, u0);
+                q_own.load(qr, a.D, a.U, u0);
+                o_own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
+                g_own.take(smem, a.D, a.U, q_len, u0, wave, lane, go);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) delta += M::dot(q[s], go[s]);
+                q_own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
+                taken = true;
+            }
+        }
+        if (!taken) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                q[s] = M::column(qr + u, s, half, a.D, a.U, there);
+                go[s] = M::column(gr + u, s, half, a.D, a.U, there);
+                delta += M::dot(M::column(orow + u, s, half, a.D, a.U, there), go[s]);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = M::flipped(q[s], a.flip);
+        delta = half_sum(delta);
+        if (exists && half == 0 && split == 0 && (SHARED || wave == 0)) a.delta[((size_t)b * a.H + head) * a.U + u] = delta;
+    }
     f32x16_t acc[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -337,14 +370,7 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             for (int d = 0; d < DP / 32; ++d) acc[d] = M::mul(M::along(kb, d * 32, lane), ds, acc[d]);
         }
     };
-    T kt, vt;
-    typename T::Places at;
-    at.set(a.D, a.T, SHARED ? threadIdx.x : lane);
     if constexpr (SHARED) {
-        if (t_begin < t_end) {
-            kt.load(krows, at, a.T, t_begin * TT, threadIdx.x);
-            vt.load(vrows, at, a.T, t_begin * TT, threadIdx.x);
-        }
         for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
             unsigned char *buf = smem + turn * 2 * T::kBytes;
             kt.write(buf, a.D, a.T, len, t * TT, threadIdx.x);
@@ -358,12 +384,7 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         }
     } else {
         unsigned char *buf = smem + wave * 2 * T::kBytes;
-        int t = t_begin + wave;
-        if (t < t_end) {
-            kt.load(krows, at, a.T, t * TT, lane);
-            vt.load(vrows, at, a.T, t * TT, lane);
-        }
-        for (; t < t_end; t += NW) {
+        for (int t = t_mine; t < t_end; t += NW) {
             wave_fence();
             kt.write(buf, a.D, a.T, len, t * TT, lane);
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, lane);
@@ -385,10 +406,10 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             store_from_f32((S *)a.dq, (size_t)b * a.dqs + ((size_t)head * a.D + ch) * a.U + u, v * a.scale);
     };
     if constexpr (SHARED) {
-        const int m0 = (ct * NW + wave) * 32, g0 = m0 / a.U, u0 = m0 - g0 * a.U;
+        const int u0 = __builtin_amdgcn_readfirstlane(u), g0 = __builtin_amdgcn_readfirstlane(g);  // of column 0
         __syncthreads();  // (the tiles give way to the results)
-        if (m0 >= a.G * a.U) return;
-        if (g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
+        if (!__any(exists)) return;
+        if (a.head_tiles || g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
             unsigned char *block = smem + wave * DP * (a.splits > 1 ? 128 : M::kRow);
             const size_t item = (size_t)(kvh * a.G + g0) * a.D * a.U;
             if (a.splits > 1)
@@ -454,16 +475,13 @@ hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-struct Form {
-    int columns, tile, waves;  // of a workgroup: tokens, positions of a tile, wavefronts with tiles of their own
-};
 constexpr bool two_blocks(bool bf16, int DP, bool shared) { return bf16 && (shared || DP <= 64); }
 // (float tiles of wide heads, one per wavefront, do not fit the registers)
 bool is_shared(bool bf16, int DP, long long columns) { return columns > 32 || (!bf16 && DP > 64); }
-Form form_of(bool bf16, int DP, long long columns)
+AttnForm form_of(bool bf16, int DP, long long columns)
 {
     const bool shared = is_shared(bf16, DP, columns);
-    return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves};
+    return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves, 2};
 }
 template <typename S, int DP, bool SHARED>
 hipError_t run_dq(const AttnArgs &a, hipStream_t s)
@@ -471,7 +489,7 @@ hipError_t run_dq(const AttnArgs &a, hipStream_t s)
     static LdsOptIn opt;
     constexpr int NB = two_blocks(sizeof(S) == 2, DP, SHARED) ? 2 : 1, NT = SHARED ? kWaves * 64 : 64;
     constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? kWaves * DP * 128 : kWaves * DP / 32 * 16 * 64 * 4;
-    constexpr int bytes = tiles > join ? tiles : join;
+    constexpr int bytes = tiles > join ? tiles : join;  // (a workgroup's tokens fit the room of its results)
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dq_kernel<S, DP, NB, kWaves, SHARED>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
@@ -513,12 +531,11 @@ AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
 {
     const int DP = (D + 31) / 32 * 32;
     const long long columns = (long long)(H / Hkv) * U;
-    const Form f = form_of(bf16, DP, columns);
-    AttnPlan p = attn_plan(f.columns, f.tile, f.waves, B, H, Hkv, D, U, T);
+    AttnPlan p = attn_plan(form_of(bf16, DP, columns), B, H, Hkv, D, U, T);
     // dk and dv: units of a tile of tokens of a head
     const int per = kWaves * 32, tokens = 32 * token_blocks(bf16, DP), units = (U + tokens - 1) / tokens * (H / Hkv);
     p.pos_tiles = (T + per - 1) / per;
-    p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D);
+    p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D, 2);
     p.parts = (units + p.units_per_part - 1) / p.units_per_part;
     p.kv_part_bytes = p.parts > 1 ? (size_t)p.parts * 2 * B * Hkv * D * T * sizeof(float) : 0;
     return p;

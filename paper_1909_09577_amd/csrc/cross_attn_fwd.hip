@@ -18,8 +18,13 @@ namespace {
 
 constexpr float kLag = 8.f;
 
+// Wavefronts of a SIMD that the registers are made to last for: two, and four where a workgroup's eight wavefronts have narrow heads
+// (a tile's groups are then few for each of them).
+template <typename S, int DP, int NW>
+constexpr int kSimdWaves = sizeof(S) * DP > 256 ? NW / 4 : (NW == 8 && sizeof(S) * DP <= 128 ? 4 : 2);
+
 template <typename S, int DP, int NB, int NW, bool SHARED>
-__global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
+__global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW>)) void attn_fwd_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;
@@ -34,9 +39,21 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
     const S *vrows = (const S *)a.v + (size_t)b * a.vs + (size_t)kvh * a.D * a.T;
 
     // this lane's column
-    const int m = (SHARED ? ct * NW + wave : ct) * 32 + (lane & 31);
-    const bool exists = m < a.G * a.U;
-    const int g = exists ? m / a.U : 0, u = exists ? m - g * a.U : 0, head = kvh * a.G + g;
+    const int block = SHARED ? wave : 0;
+    int g, u;
+    bool exists;
+    if (a.head_tiles) {
+        g = ct / a.head_tiles;
+        u = ((ct - g * a.head_tiles) * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        exists = u < a.U;
+    } else {
+        const int m = (ct * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        exists = m < a.G * a.U;
+        g = exists ? m / a.U : 0;
+        u = m - g * a.U;
+    }
+    if (!exists) u = 0;
+    const int head = kvh * a.G + g;
     const bool there = exists && u < q_len;
     int lo = 0, hi = 0x7fffffff;  // a column that is not there is masked nowhere: it must not slow the others down
     int first = a.T, last = 0;    // frames that some column may look at
@@ -45,12 +62,6 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
         first = lo;
         last = hi;
     }
-    typename M::Frag q[KS];
-    {
-        const S *col = (const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U + u;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = M::column(col, s, half, a.D, a.U, there, a.flip);
-    }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         first = min(first, __shfl_xor(first, d));
@@ -58,7 +69,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
     }
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
-    const bool active = last > first;
+    const int wave_first = first, wave_last = last;
     if constexpr (SHARED) {  // of the workgroup
         int *range = reinterpret_cast<int *>(smem);
         if (lane == 0) {
@@ -73,7 +84,37 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
         }
         __syncthreads();
     }
-    int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+    const int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+
+    // the first tiles and the tokens are loaded together
+    T kt, vt;
+    typename T::Places at;
+    const int loader = SHARED ? threadIdx.x : lane, t_mine = SHARED ? t_begin : t_begin + wave;
+    at.set(a.D, a.T, loader);
+    if (t_mine < t_end) {
+        kt.load(krows, at, a.T, t_mine * TT, loader);
+        vt.load(vrows, at, a.T, t_mine * TT, loader);
+    }
+    typename M::Frag q[KS];
+    {
+        const S *rows = (const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U;
+        bool taken = false;
+        if constexpr (SHARED) {
+            if (a.head_tiles) {  // (uniform)
+                const int u0 = (ct - g * a.head_tiles) * NW * 32;
+                OwnColumns<S, DP, NW> own;
+                own.load(rows, a.D, a.U, u0);
+                own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
+                taken = true;
+            }
+        }
+        if (!taken) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) q[s] = M::column(rows + u, s, half, a.D, a.U, there);
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = M::flipped(q[s], a.flip);
+    }
 
     float mx = -INFINITY, sum = 0.f;  // in powers of two, and of this lane's positions
     f32x16_t acc[DP / 32];
@@ -140,14 +181,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
             for (int d = 0; d < DP / 32; ++d) acc[d] = M::mul(M::along(vt + n * T::kBlock, d * 32, lane), p[n], acc[d]);
     };
 
-    T kt, vt;
-    typename T::Places at;
-    at.set(a.D, a.T, SHARED ? threadIdx.x : lane);
     if constexpr (SHARED) {
-        if (t_begin < t_end) {
-            kt.load(krows, at, a.T, t_begin * TT, threadIdx.x);
-            vt.load(vrows, at, a.T, t_begin * TT, threadIdx.x);
-        }
         for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
             unsigned char *buf = smem + turn * 2 * T::kBytes;
             kt.write(buf, a.D, a.T, len, t * TT, threadIdx.x);
@@ -157,16 +191,11 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
                 kt.load(krows, at, a.T, (t + 1) * TT, threadIdx.x);
                 vt.load(vrows, at, a.T, (t + 1) * TT, threadIdx.x);
             }
-            if (active) compute(buf, buf + T::kBytes, t * TT);
+            if (t * TT < wave_last && (t + 1) * TT > wave_first) compute(buf, buf + T::kBytes, t * TT);
         }
     } else {
         unsigned char *buf = smem + wave * 2 * T::kBytes;
-        int t = t_begin + wave;
-        if (t < t_end) {
-            kt.load(krows, at, a.T, t * TT, lane);
-            vt.load(vrows, at, a.T, t * TT, lane);
-        }
-        for (; t < t_end; t += NW) {
+        for (int t = t_mine; t < t_end; t += NW) {
             wave_fence();
             kt.write(buf, a.D, a.T, len, t * TT, lane);
             vt.write(buf + T::kBytes, a.D, a.T, len, t * TT, lane);
@@ -205,9 +234,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_f
         __syncthreads();  // (the tiles give way to the results)
         const float total = half_sum(sum);
         put_sums(mx, total);
-        const int m0 = (ct * NW + wave) * 32, g0 = m0 / a.U, u0 = m0 - g0 * a.U;
-        if (m0 >= a.G * a.U) return;
-        if (g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
+        const int u0 = __builtin_amdgcn_readfirstlane(u), g0 = __builtin_amdgcn_readfirstlane(g);  // of column 0
+        if (!__any(exists)) return;
+        if (a.head_tiles || g0 == a.G - 1 || u0 + 32 <= a.U) {  // (uniform) tokens of one head
             unsigned char *block = smem + wave * DP * (a.splits > 1 ? 128 : M::kRow);
             const size_t item = (size_t)(kvh * a.G + g0) * a.D * a.U;
             if (a.splits > 1)
@@ -289,14 +318,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 template <typename S, int DP, int NB, int NW, bool SHARED>
 constexpr int lds_bytes()
 {
-    if constexpr (SHARED) return 4 * Tile<S, DP, NB, NW * 64>::kBytes;  // (results of NW wavefronts fit: float blocks of 32)
+    if constexpr (SHARED) {
+        constexpr int tiles = 4 * Tile<S, DP, NB, NW * 64>::kBytes, out = NW * DP * 128;  // (room for results as float blocks)
+        return tiles > out ? tiles : out;
+    }
     constexpr int tiles = NW * 2 * Tile<S, DP, NB, 64>::kBytes, join = NW * 128 * 4 + NW * (DP / 32 * 16) * 64 * 4;
     return tiles > join ? tiles : join;
 }
 
-struct Form {
-    int columns, tile, waves;  // of a workgroup: tokens, positions of a tile, wavefronts with tiles of their own
-};
 template <typename S, int DP, int NB, int NW, bool SHARED>
 hipError_t run(AttnArgs a, hipStream_t s)
 {
@@ -311,20 +340,25 @@ hipError_t run(AttnArgs a, hipStream_t s)
 }
 
 constexpr int kApartColumns = 32;
-Form form_of(bool bf16, int DP, long long columns)
+// Few columns go apart (but float tiles of wide heads, one per wavefront, do not fit the registers).  Of the others, 256 share keys and
+// values where there are that many: they are then read and written to LDS half as often.
+AttnForm form_of(bool bf16, int DP, int U, int G)
 {
-    // (float tiles of wide heads, one per wavefront, do not fit the registers)
-    if (columns <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, 4};
-    return {128, bf16 ? 64 : 32, 1};
+    if ((long long)U * G <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, 4, 2};
+    if (bf16 && U > 128) return {256, 64, 1, DP <= 64 ? 2 : 1};
+    return {128, bf16 ? 64 : 32, 1, 2};
 }
 
 template <typename S, int DP>
 hipError_t run_form(const AttnArgs &a, hipStream_t s)
 {
     constexpr bool bf16 = sizeof(S) == 2;
-    const Form f = form_of(bf16, DP, (long long)a.G * a.U);
+    const AttnForm f = form_of(bf16, DP, a.U, a.G);
     if constexpr (bf16 || DP <= 64) {
         if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, 4, false>(a, s);
+    }
+    if constexpr (bf16) {
+        if (f.columns == 256) return run<S, DP, 2, 8, true>(a, s);
     }
     return run<S, DP, bf16 ? 2 : 1, 4, true>(a, s);
 }
@@ -345,10 +379,7 @@ hipError_t run_any(const AttnArgs &a, hipStream_t s)
 
 AttnPlan attn_fwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
 {
-    const int DP = (D + 31) / 32 * 32;
-    const long long columns = (long long)(H / Hkv) * U;
-    const Form f = form_of(bf16, DP, columns);
-    return attn_plan(f.columns, f.tile, f.waves, B, H, Hkv, D, U, T);
+    return attn_plan(form_of(bf16, (D + 31) / 32 * 32, U, H / Hkv), B, H, Hkv, D, U, T);
 }
 
 hipError_t launch_attn_fwd(bool bf16, const AttnArgs &a, hipStream_t s) { return bf16 ? run_any<bf16_t>(a, s) : run_any<float>(a, s); }

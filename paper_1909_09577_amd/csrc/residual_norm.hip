@@ -114,6 +114,11 @@ __device__ __forceinline__ int length_of(const int *len, int b, int T)
     return n < 0 ? 0 : (n > T ? T : n);
 }
 
+// Neighbouring tiles share lines of memory: they go to workgroups of one XCD (every eighth), one after the other.  The grid is a
+// multiple of eight; numbers beyond the work return.
+__device__ __forceinline__ int neighbours_together() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+inline dim3 eights(size_t n) { return dim3((unsigned)((n + 7) / 8 * 8)); }
+
 // Sums N quantities of each of the V positions over all lanes that hold the same positions (lane % TG): over a wavefront by
 // exchanges, over the wavefronts by one thread for every sum, which all threads then read.  (The first barrier keeps a call's
 // writes of `total` behind the last call's reads of it, the second one its writes of `part`.)
@@ -160,7 +165,9 @@ __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(NormFwd p)
     __shared__ ColumnSums<TG, V, 1> lds;
     const int tg = threadIdx.x % TG, cl = threadIdx.x / TG;
     const int tiles = (p.T + TW - 1) / TW;
-    const int b = blockIdx.x / tiles, tile = blockIdx.x - b * tiles;
+    const int at_tile = neighbours_together();
+    if (at_tile >= p.B * tiles) return;
+    const int b = at_tile / tiles, tile = at_tile - b * tiles;
     const int t_own = tile * TW + tg * V;  // the group's place; it is read at t0
     const int t0 = min(t_own, p.T - V);
     const bool store = t_own < p.T;
@@ -333,29 +340,33 @@ __global__ __launch_bounds__(kPlainThreads) void residual_norm_fwd_plain_kernel(
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------
-// A workgroup owns every splits-th tile of an item and adds its sums over time in registers: the four lanes of a row add
-// theirs and each keeps every fourth sum, so that six sums of a row take two registers.
-__device__ __forceinline__ float quad_sum(float v)
+// A workgroup owns every splits-th tile of an item and adds its sums over time in registers: the TG lanes of a row add
+// theirs and each keeps every TG-th sum, so that the six sums of a row take 6/TG registers.
+template <int TG>
+__device__ __forceinline__ float row_sum(float v)
 {
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));         // lanes 1 0 3 2
-    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));  // lanes 2 3 0 1
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));              // lanes 1 0 3 2
+    if constexpr (TG > 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));  // 2 3 0 1
+    if constexpr (TG > 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 5 4 3 2 1 0
+    return v;
 }
 
-template <typename S, int NR, bool LAYER>
+template <typename S, int TG, int NR, bool LAYER>
 struct NormBwdLds {
-    ColumnSums<4, Group<S>::V, LAYER ? 4 : 3> sums;
-    float vectors[5][NR * kThreads / 4];
+    ColumnSums<TG, Group<S>::V, LAYER ? 4 : 3> sums;
+    float vectors[5][NR * kThreads / TG];
     u32x4_t f[NR * kThreads];  // behind it as much for an element gate
 };
 
+// Few channels have many positions in a tile (TG), so that a thread has groups enough for the work around them.
 // The per-channel vectors lie in LDS, ones and zeros for those that are not given, so that nothing branches between the rows.
 // The groups of f and of an element gate wait in LDS, each thread's its own, until g is made: five tensors' groups and all that is
 // made of them do not fit the registers.  NR = ceil(C / 128): only the last row of a thread can lie beyond the channels.
-template <typename S, int NR, bool LAYER>
-__global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
+template <typename S, int TG, int NR, bool LAYER>
+__global__ __launch_bounds__(kThreads, sizeof(S) == 2 && NR == 4 ? 2 : 4) void residual_norm_bwd_kernel(NormBwd p)
 {
-    constexpr int V = Group<S>::V, TG = 4, CL = kThreads / TG, TW = TG * V, NQ = LAYER ? 4 : 3;
-    typedef NormBwdLds<S, NR, LAYER> Lds;
+    constexpr int V = Group<S>::V, CL = kThreads / TG, TW = TG * V, NQ = LAYER ? 4 : 3;
+    typedef NormBwdLds<S, TG, NR, LAYER> Lds;
     extern __shared__ __align__(16) unsigned char smem[];
     Lds &shared = *reinterpret_cast<Lds *>(smem);
     auto &lds = shared.sums;
@@ -363,7 +374,9 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
     u32x4_t *fl = shared.f + threadIdx.x, *gl = reinterpret_cast<u32x4_t *>(smem + sizeof(Lds)) + threadIdx.x;  // row i: kThreads * i further
     const int tg = threadIdx.x % TG;
     const int tiles = (p.T + TW - 1) / TW;
-    const int b = blockIdx.x / p.splits, split = blockIdx.x - b * p.splits;
+    const int id = neighbours_together();
+    if (id >= p.B * p.splits) return;
+    const int b = id / p.splits, split = id - b * p.splits;
     const int len = length_of(p.len, b, p.T);
     const float per_c = 1.f / (float)p.C;
     const size_t item = (size_t)b * p.C * p.T;
@@ -379,14 +392,18 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
         rscale[c] = p.rscale ? p.rscale[c] : 1.f;
         gate_of[c] = p.gate_kind == NM_GATE_ITEM ? ((const float *)p.gate)[(size_t)b * p.C + c] : 1.f;
     }
-    __syncthreads();
-    float sums[2][NR];  // of quantities tg and tg + 4
+    // (the barrier in front of their first use comes when the first tile has been asked for)
+    bool filled = false;
+    constexpr int kKept = (kSums + TG - 1) / TG;
+    float sums[kKept][NR];  // of quantities tg, tg + TG ..
 #pragma unroll
-    for (int i = 0; i < NR; ++i) sums[0][i] = sums[1][i] = 0.f;
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int q = 0; q < kKept; ++q) sums[q][i] = 0.f;
     auto keep = [&](int quantity, int i, float v) {
-        v = quad_sum(v);
-        if (tg == (quantity & 3)) sums[quantity >> 2][i] += v;
-        asm volatile("" : "+v"(sums[quantity >> 2][i]));  // (added here, not at the end, which keeps all the summands)
+        v = row_sum<TG>(v);
+        if (tg == quantity % TG) sums[quantity / TG][i] += v;
+        asm volatile("" : "+v"(sums[quantity / TG][i]));  // (added here, not at the end, which keeps all the summands)
     };
 
     for (int tile = split; tile < tiles; tile += p.splits) {
@@ -422,10 +439,18 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
                 for (int i = 0; i < NR; ++i) r[i] = first_positions<S>(r[i], len - t0);
             }
         };
+        u32x4_t gr[NR];
+        load(gate, gate != nullptr, gr);
+        load(f, f != nullptr, fr);
         load(y, p.next, yr);
         load(dn, p.next, dnr);
-        load(f, f != nullptr, fr);
         load(dy, dy != nullptr, dyr);
+        if (!filled) __syncthreads();
+        filled = true;
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) gl[i * kThreads] = gr[i];
+        }
         if (f) {
 #pragma unroll
             for (int i = 0; i < NR; ++i) fl[i * kThreads] = fr[i];
@@ -506,11 +531,6 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
         // g, in the place of dy and dn; dx and the sums over time of the norm of y.  (Without that norm dn = 0, and all of this
         // adds nothing to dy.)
         float g[NR][V];
-        if (gate) {
-            load(gate, true, fr);
-#pragma unroll
-            for (int i = 0; i < NR; ++i) gl[i * kThreads] = fr[i];
-        }
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             asm volatile("" : "+v"(cl));
@@ -598,8 +618,9 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(NormBwd p)
     for (int i = 0; i < NR; ++i) {
         const int c = threadIdx.x / TG + i * CL;
         if (c >= p.C) break;
-        if (p.sums >> tg & 1) p.part[(tg * rows + blockIdx.x) * p.C + c] = sums[0][i];
-        if (tg + 4 < kSums && (p.sums >> (tg + 4) & 1)) p.part[((tg + 4) * rows + blockIdx.x) * p.C + c] = sums[1][i];
+#pragma unroll
+        for (int q = 0; q < kKept; ++q)
+            if (q * TG + tg < kSums && (p.sums >> (q * TG + tg) & 1)) p.part[((q * TG + tg) * rows + id) * p.C + c] = sums[q][i];
     }
 }
 
@@ -700,7 +721,7 @@ __global__ __launch_bounds__(kPlainThreads) void residual_norm_bwd_plain_kernel(
     }
 }
 
-// out[c] = sum over `rows` rows of part[rows][C], a fixed order: 32 channels by 8 shares of the rows per workgroup.
+// out[c] = sum over `rows` rows of part[rows][C], a fixed order: 32 channels by 32 shares of the rows per workgroup.
 // blockIdx.y: one of up to five sums over all items, behind them an item's gate sums over its `splits` rows
 struct ReduceArgs {
     const float *part;
@@ -709,9 +730,9 @@ struct ReduceArgs {
     float *dgate;
     int B, C, splits;
 };
-__global__ __launch_bounds__(256) void residual_norm_sums_kernel(ReduceArgs a)
+__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(ReduceArgs a)
 {
-    __shared__ float s[8][33];
+    __shared__ float s[32][33];
     const int cl = threadIdx.x & 31, share = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + cl, cc = min(c, a.C - 1);
     const int rows = a.B * a.splits;
@@ -720,24 +741,26 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(ReduceArgs a)
     const int q = item ? (int)kDgate : a.quantity[blockIdx.y], first = item ? b * a.splits : 0, n = item ? a.splits : rows;
     const float *p = a.part + ((size_t)q * rows + first) * a.C + cc;
     float t = 0.f;
-    for (int r = share; r < n; r += 8) t += p[(size_t)r * a.C];
+#pragma unroll 4
+    for (int r = share; r < n; r += 32) t += p[(size_t)r * a.C];
     s[share][cl] = t;
     __syncthreads();
-    if (share == 0 && c < a.C) {
-        float v = 0.f;
+    // 32 sums of a channel: a wavefront's half adds those of one channel by exchanges
+    float v = s[cl][share];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v += s[i][cl];
-        (item ? a.dgate + (size_t)b * a.C : a.out[blockIdx.y])[c] = v;
-    }
+    for (int d = 1; d < 32; d <<= 1) v += __shfl_xor(v, d);
+    const int co = blockIdx.x * 32 + share;
+    if (cl == 0 && co < a.C) (item ? a.dgate + (size_t)b * a.C : a.out[blockIdx.y])[co] = v;
 }
 
-constexpr int kFwdTG = 8, kBwdTG = 4;
-constexpr int kFwdLanes = kThreads / kFwdTG, kBwdLanes = kThreads / kBwdTG;  // channels side by side
+constexpr int kFwdTG = 4;
+constexpr int kFwdLanes = kThreads / kFwdTG;  // channels side by side
+constexpr int bwd_tg(int C) { return C <= kThreads / 2 ? 8 : (C <= kThreads ? 4 : 2); }  // at most four rows of a thread
 
-// Whether the kernels that hold an item's tile in registers serve a call: up to 1024 channels (eight groups of four tensors a
+// Whether the kernels that hold an item's tile in registers serve a call: up to 1024 channels (four or eight groups of a tensor a
 // thread), rows of a group at least, items whose byte offsets fit 32 bits.
-constexpr int kMaxInRegisters = 8 * kBwdLanes;
-static_assert(kMaxInRegisters == 16 * kFwdLanes, "one limit for both passes");
+constexpr int kMaxInRegisters = 4 * kThreads / 2;
+static_assert(kMaxInRegisters == 8 * kFwdLanes, "one limit for both passes");
 bool in_registers(int C, int T, size_t element) { return C <= kMaxInRegisters && T >= (int)(16 / element) && (size_t)C * T * element < (size_t)1 << 32; }
 
 // Positions side by side in a workgroup of the plain kernels: a power of two, no more than 64
@@ -753,8 +776,8 @@ int plain_positions(int T)
 int bwd_splits(int B, int C, int T, int dtype)
 {
     const size_t element = dtype == NM_BF16 ? 2 : 4;
-    const int width = in_registers(C, T, element) ? kBwdTG * (int)(16 / element) : plain_positions(T);
-    const int tiles = (T + width - 1) / width, want = (512 + B - 1) / B;
+    const int width = in_registers(C, T, element) ? bwd_tg(C) * (int)(16 / element) : plain_positions(T);
+    const int tiles = (T + width - 1) / width, want = (1024 + B - 1) / B;
     return tiles < want ? tiles : want;
 }
 
@@ -762,7 +785,7 @@ template <typename S, int NR>
 hipError_t fwd_rows(const NormFwd &p, hipStream_t s)
 {
     constexpr int TW = kFwdTG * Group<S>::V;
-    const dim3 grid((unsigned)p.B * ((p.T + TW - 1) / TW));
+    const dim3 grid = eights((size_t)p.B * ((p.T + TW - 1) / TW));
     if (p.layer)
         residual_norm_fwd_kernel<S, kFwdTG, NR, true><<<grid, dim3(kThreads), 0, s>>>(p);
     else
@@ -777,24 +800,29 @@ hipError_t fwd_any(const NormFwd &p, hipStream_t s)
         residual_norm_fwd_plain_kernel<S><<<dim3((unsigned)p.B * ((p.T + positions - 1) / positions)), dim3(kPlainThreads), 0, s>>>(p, positions);
         return hipGetLastError();
     }
-    return p.C <= 8 * kFwdLanes ? fwd_rows<S, 8>(p, s) : fwd_rows<S, 16>(p, s);
+    return p.C <= 4 * kFwdLanes ? fwd_rows<S, 4>(p, s) : fwd_rows<S, 8>(p, s);
 }
 
-template <typename S, int NR, bool LAYER>
+template <typename S, int TG, int NR, bool LAYER>
 hipError_t bwd_rows_of(const NormBwd &p, hipStream_t s)
 {
     static LdsOptIn opt;
-    constexpr int base = (int)sizeof(NormBwdLds<S, NR, LAYER>), most = base + NR * kThreads * 16;
+    constexpr int base = (int)sizeof(NormBwdLds<S, TG, NR, LAYER>), most = base + NR * kThreads * 16;
     static_assert(most <= 160 * 1024, "LDS of a CU");
-    const hipError_t e = ensure_dynamic_lds(opt, (const void *)residual_norm_bwd_kernel<S, NR, LAYER>, most);
+    const hipError_t e = ensure_dynamic_lds(opt, (const void *)residual_norm_bwd_kernel<S, TG, NR, LAYER>, most);
     if (e != hipSuccess) return e;
-    residual_norm_bwd_kernel<S, NR, LAYER><<<dim3((unsigned)p.B * p.splits), dim3(kThreads), p.gate_kind == NM_GATE_ELEMENT ? most : base, s>>>(p);
+    residual_norm_bwd_kernel<S, TG, NR, LAYER><<<eights((size_t)p.B * p.splits), dim3(kThreads), p.gate_kind == NM_GATE_ELEMENT ? most : base, s>>>(p);
     return hipGetLastError();
 }
-template <typename S, int NR>
+template <typename S, int TG>
 hipError_t bwd_rows(const NormBwd &p, hipStream_t s)
 {
-    return p.layer ? bwd_rows_of<S, NR, true>(p, s) : bwd_rows_of<S, NR, false>(p, s);
+    switch ((p.C * TG + kThreads - 1) / kThreads) {
+    case 1: return p.layer ? bwd_rows_of<S, TG, 1, true>(p, s) : bwd_rows_of<S, TG, 1, false>(p, s);
+    case 2: return p.layer ? bwd_rows_of<S, TG, 2, true>(p, s) : bwd_rows_of<S, TG, 2, false>(p, s);
+    case 3: return p.layer ? bwd_rows_of<S, TG, 3, true>(p, s) : bwd_rows_of<S, TG, 3, false>(p, s);
+    default: return p.layer ? bwd_rows_of<S, TG, 4, true>(p, s) : bwd_rows_of<S, TG, 4, false>(p, s);
+    }
 }
 template <typename S>
 hipError_t bwd_any(const NormBwd &p, hipStream_t s)
@@ -803,16 +831,8 @@ hipError_t bwd_any(const NormBwd &p, hipStream_t s)
         residual_norm_bwd_plain_kernel<S><<<dim3((unsigned)p.B * p.splits), dim3(kPlainThreads), 0, s>>>(p, plain_positions(p.T));
         return hipGetLastError();
     }
-    switch ((p.C + kBwdLanes - 1) / kBwdLanes) {
-    case 1: return bwd_rows<S, 1>(p, s);
-    case 2: return bwd_rows<S, 2>(p, s);
-    case 3: return bwd_rows<S, 3>(p, s);
-    case 4: return bwd_rows<S, 4>(p, s);
-    case 5: return bwd_rows<S, 5>(p, s);
-    case 6: return bwd_rows<S, 6>(p, s);
-    case 7: return bwd_rows<S, 7>(p, s);
-    default: return bwd_rows<S, 8>(p, s);
-    }
+    const int tg = bwd_tg(p.C);
+    return tg == 8 ? bwd_rows<S, 8>(p, s) : (tg == 4 ? bwd_rows<S, 4>(p, s) : bwd_rows<S, 2>(p, s));
 }
 
 int check_shape(int B, int C, int T, int dtype)
@@ -909,7 +929,7 @@ int nm_residual_norm_bwd(int B, int C, int T, const void *dy, const void *dn, co
     r.part = (const float *)workspace;
     r.dgate = (float *)dgate;
     r.B = B; r.C = C; r.splits = p.splits;
-    residual_norm_sums_kernel<<<dim3((C + 31) / 32, r.count + (item ? B : 0)), dim3(256), 0, s>>>(r);
+    residual_norm_sums_kernel<<<dim3((C + 31) / 32, r.count + (item ? B : 0)), dim3(1024), 0, s>>>(r);
     return dev(hipGetLastError());
 }
 

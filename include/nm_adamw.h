@@ -48,7 +48,7 @@ size_t nm_adamw_plan_bytes(const nm_adamw_tensor *tensors, int count, int state_
 int nm_adamw_plan(const nm_adamw_tensor *tensors, int count, int state_bits, void *plan, size_t plan_bytes);
 
 /* One step.  plan: the host copy; plan_device: the same bytes in device memory (256-byte aligned).  step counts from 1.
- * 0 <= beta < 1, eps > 0, lr finite.  grad_scale [1] float, device, or NULL (1).  seed: another one each step; unused with
+ * 0 <= beta < 1, eps at least 2^-126, lr finite.  grad_scale [1] float, device, or NULL (1).  seed: another one each step; unused with
  * 32 state bits. */
 int nm_adamw_step(const void *plan, const void *plan_device, size_t plan_bytes, double lr, double beta1, double beta2,
                   double eps, long long step, const float *grad_scale, unsigned seed, void *hip_stream);

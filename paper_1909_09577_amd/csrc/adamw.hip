@@ -1,7 +1,9 @@
 // AdamW over the tensors of a plan in one launch (definition: include/nm_adamw.h).
 //
 // Bound by memory: 30 bytes an element with float states (parameter, both moments in and out, gradient in, bfloat16 copy
-// out), 18 with 8-bit states.  A wavefront owns a block of 256 elements, four neighbours per lane, so that every access is
+// out), 18 with 8-bit states, whose 64-bit arithmetic takes about as long: roots and reciprocals come from the float instructions
+// and steps of Newton's iteration (library roots and divisions: 1530 us instead of 1190 over 322 million weights; with float
+// states 1590 to 1840 us, 5.3 to 6.1 TB/s).  A wavefront owns a block of 256 elements, four neighbours per lane, so that every access is
 // 16 bytes (float), 8 (copy) or 4 (codes) per lane and contiguous over the wavefront, and so that the maximum of a block of
 // 8-bit states needs no LDS.  A workgroup takes kChunkBlocks blocks of one tensor; the plan names the tensor of every chunk.
 #include "../../include/nm_adamw.h"
@@ -17,7 +19,6 @@ namespace {
 constexpr int kBlock = 256;       // elements of a block
 constexpr int kChunkBlocks = 16;  // blocks of a workgroup: four per wavefront
 constexpr uint32_t kMagic = 0x4e4d4157u;
-constexpr float kE4M3Max = 448.f;
 
 struct PlanHeader {  // the first 64 bytes of a plan; the records and then the chunks' tensors (int32) follow
     uint32_t magic;
@@ -73,9 +74,17 @@ __device__ __forceinline__ void store4(T *p, int n, bool whole, const T (&in)[4]
     }
 }
 
-__device__ __forceinline__ uint32_t mixed(uint32_t element, uint32_t seed)
+// A pointer that was read from the plan: to global memory (taken for a generic one, every access would go by the path that also serves LDS).
+template <typename T>
+__device__ __forceinline__ T *global(T *p)
 {
-    uint32_t h = (element * 0x9E3779B9u) ^ seed;
+    return (T *)(__attribute__((address_space(1))) T *)p;
+}
+
+// times_element: the element's number * 0x9E3779B9
+__device__ __forceinline__ uint32_t mixed(uint32_t times_element, uint32_t seed)
+{
+    uint32_t h = times_element ^ seed;
     h = (h ^ (h >> 16)) * 0x6A09E667u;
     h = (h ^ (h >> 13)) * 0xBB67AE85u;
     return h ^ (h >> 16);
@@ -85,11 +94,28 @@ __device__ __forceinline__ uint32_t mixed(uint32_t element, uint32_t seed)
 // lanes' own scales are reduced.
 __device__ __forceinline__ float block_scale(double amax)
 {
-    float s = (float)(amax / (double)kE4M3Max);
+    double q = amax * (1.0 / 448.0);
+    q = __builtin_fma(__builtin_fma(-q, 448.0, amax), 1.0 / 448.0, q);  // amax / 448, rounded as a division is
+    float s = (float)q;
     s = amax > 0.0 ? fmaxf(s, 0x1p-126f) : 0.f;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s = fmaxf(s, __shfl_xor(s, d));
     return s > 0.f ? s : 1.f;
+}
+
+// 1/s to a double's precision or an ulp of it, s a float from 2^-126 on: two steps of Newton's iteration from the float reciprocal.
+__device__ __forceinline__ double reciprocal(float s)
+{
+    double y = (double)__builtin_amdgcn_rcpf(s);
+    y = __builtin_fma(__builtin_fma(-(double)s, y, 1.0), y, y);
+    return __builtin_fma(__builtin_fma(-(double)s, y, 1.0), y, y);
+}
+// The root of v to some 1e-14: one step of Newton's iteration from the float root, for v that is a normal float with room around it.
+__device__ __forceinline__ double quick_root(double v)
+{
+    const float r = __builtin_amdgcn_sqrtf((float)v);
+    const double d = (double)r;
+    return __builtin_fma(__builtin_fma(-d, d, v), (double)(0.5f * __builtin_amdgcn_rcpf(r)), d);
 }
 
 // E4M3 code of magnitude z (>= 0, in units of the scale) rounded by the 16 bits u.  With e the exponent of z (at least that of
@@ -112,9 +138,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
     const uint32_t n = rec.n;
     const float decay = 1.f - a.lr * rec.weight_decay;
     const float gs = a.grad_scale ? a.grad_scale[0] : 1.f;
-    float *__restrict__ param = rec.param;
-    const float *__restrict__ grad = rec.grad;
-    bf16_t *__restrict__ copy = rec.copy;
+    float *__restrict__ param = global(rec.param);
+    const float *__restrict__ grad = global(rec.grad);
+    bf16_t *__restrict__ copy = global(rec.copy);
     const uint32_t block0 = (uint32_t)((int)blockIdx.x - rec.first_chunk) * kChunkBlocks + wave;
 #pragma unroll
     for (int i = 0; i < kChunkBlocks / 4; ++i) {
@@ -127,7 +153,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
         load4<float4>(param + at, left, whole, p);
         load4<float4>(grad + at, left, whole, g);
         if constexpr (BITS == 32) {
-            float *mp = (float *)rec.m + at, *vp = (float *)rec.v + at;
+            float *mp = global((float *)rec.m) + at, *vp = global((float *)rec.v) + at;
             float m[4], v[4];
             load4<float4>(mp, left, whole, m);
             load4<float4>(vp, left, whole, v);
@@ -141,36 +167,50 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
             store4<float4>(mp, left, whole, m);
             store4<float4>(vp, left, whole, v);
         } else {
-            unsigned char *mp = (unsigned char *)rec.m + at, *rp = (unsigned char *)rec.v + at;
+            unsigned char *mp = global((unsigned char *)rec.m) + at, *rp = global((unsigned char *)rec.v) + at;
+            float *m_scales = global(rec.m_scale), *r_scales = global(rec.v_scale);
             unsigned char mc[4], rc[4];
             load4<uint32_t>(mp, left, whole, mc);
             load4<uint32_t>(rp, left, whole, rc);
-            const double ms = rec.m_scale[block], rs = rec.v_scale[block];
+            const double ms = m_scales[block], rs = r_scales[block];
             double m[4], r[4], m_max = 0.0, r_max = 0.0;
             const uint32_t mw = mc[0] | mc[1] << 8 | mc[2] << 16 | (uint32_t)mc[3] << 24;
             const uint32_t rw = rc[0] | rc[1] << 8 | rc[2] << 16 | (uint32_t)rc[3] << 24;
             const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mw, true);
             const auto r01 = __builtin_amdgcn_cvt_pk_f32_fp8(rw, false), r23 = __builtin_amdgcn_cvt_pk_f32_fp8(rw, true);
             const float mf[4] = {m01[0], m01[1], m23[0], m23[1]}, rf[4] = {r01[0], r01[1], r23[0], r23[1]};
+            double v[4];
+            bool plain = true;  // all of the lane's v have a float root
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const double gj = g[j] * gs;
                 m[j] = a.beta1_d * ((double)mf[j] * ms) + a.one_minus_beta1_d * gj;
                 const double rj = (double)rf[j] * rs;
-                r[j] = sqrt(a.beta2_d * (rj * rj) + a.one_minus_beta2_d * (gj * gj));
-                update[j] = (float)m[j] / ((float)r[j] * a.root_correction + a.eps);
-                if (j >= left) m[j] = r[j] = 0.0;
+                v[j] = a.beta2_d * (rj * rj) + a.one_minus_beta2_d * (gj * gj);
+                if (j >= left) m[j] = v[j] = 0.0;
+                plain = plain && v[j] < 0x1p100 && (v[j] > 0x1p-100 || v[j] == 0.0);
+            }
+            if (__all(plain)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = v[j] > 0.0 ? quick_root(v[j]) : 0.0;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = sqrt(v[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                update[j] = (float)m[j] * __builtin_amdgcn_rcpf((float)r[j] * a.root_correction + a.eps);  // (an ulp or two; the denominator is no subnormal)
                 // (a comparison with infinity is false for a NaN)
                 const double ma = fabs(m[j]);
                 if (ma < INFINITY) m_max = fmax(m_max, ma);
                 if (r[j] < INFINITY) r_max = fmax(r_max, r[j]);
             }
             const float m_scale = block_scale(m_max), r_scale = block_scale(r_max);
-            const double per_m = 1.0 / (double)m_scale, per_r = 1.0 / (double)r_scale;
-            const uint32_t element = (rec.first_block + block) * kBlock + 4 * lane;
+            const double per_m = reciprocal(m_scale), per_r = reciprocal(r_scale);
+            const uint32_t element = ((rec.first_block + block) * kBlock + 4 * lane) * 0x9E3779B9u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t u = mixed(element + j, a.seed);
+                const uint32_t u = mixed(element + j * 0x9E3779B9u, a.seed);
                 const double ma = fabs(m[j]);
                 uint32_t cm = e4m3_steps(ma * per_m, u & 0xffffu) | (m[j] < 0.0 ? 0x80u : 0u);
                 uint32_t cr = e4m3_steps(r[j] * per_r, u >> 16);
@@ -183,8 +223,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
             store4<uint32_t>(mp, left, whole, mc);
             store4<uint32_t>(rp, left, whole, rc);
             if (lane == 0) {
-                rec.m_scale[block] = m_scale;
-                rec.v_scale[block] = r_scale;
+                m_scales[block] = m_scale;
+                r_scales[block] = r_scale;
             }
         }
 #pragma unroll
@@ -192,8 +232,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
         store4<float4>(param + at, left, whole, p);
         if (copy) {
             bf16_t c[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) c[j] = f32_to_bf16(p[j]);
+            const uint32_t w[2] = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
+            __builtin_memcpy(c, w, 8);
             store4<uint2>(copy + at, left, whole, c);
         }
     }
@@ -277,7 +317,7 @@ int nm_adamw_step(const void *plan, const void *plan_device, size_t plan_bytes, 
     if (!plan || !plan_device || plan_bytes < sizeof(PlanHeader) || (uintptr_t)plan % 8 || (uintptr_t)plan_device % 256) return NM_ERR_BAD_ARG;
     const PlanHeader *h = (const PlanHeader *)plan;
     if (h->magic != kMagic || h->bytes > plan_bytes || h->count <= 0 || h->chunks <= 0 || h->bytes != plan_size(h->count, h->chunks)) return NM_ERR_BAD_ARG;
-    if (!isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) || isinf(eps) || step < 1) return NM_ERR_BAD_ARG;
+    if (!isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0x1p-126) || isinf(eps) || step < 1) return NM_ERR_BAD_ARG;
     StepArgs a;
     a.lr = (float)lr;
     a.step_size = (float)(lr / (1.0 - pow(beta1, (double)step)));

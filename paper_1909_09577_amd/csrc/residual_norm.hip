@@ -346,7 +346,7 @@ template <int TG>
 __device__ __forceinline__ float row_sum(float v)
 {
     v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));              // lanes 1 0 3 2
-    if constexpr (TG > 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));  // 2 3 0 1
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));                                // 2 3 0 1
     if constexpr (TG > 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 5 4 3 2 1 0
     return v;
 }
@@ -363,7 +363,7 @@ struct NormBwdLds {
 // The groups of f and of an element gate wait in LDS, each thread's its own, until g is made: five tensors' groups and all that is
 // made of them do not fit the registers.  NR = ceil(C / 128): only the last row of a thread can lie beyond the channels.
 template <typename S, int TG, int NR, bool LAYER>
-__global__ __launch_bounds__(kThreads, sizeof(S) == 2 && NR == 4 ? 2 : 4) void residual_norm_bwd_kernel(NormBwd p)
+__global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_kernel(NormBwd p)
 {
     constexpr int V = Group<S>::V, CL = kThreads / TG, TW = TG * V, NQ = LAYER ? 4 : 3;
     typedef NormBwdLds<S, TG, NR, LAYER> Lds;
@@ -755,11 +755,11 @@ __global__ __launch_bounds__(1024) void residual_norm_sums_kernel(ReduceArgs a)
 
 constexpr int kFwdTG = 4;
 constexpr int kFwdLanes = kThreads / kFwdTG;  // channels side by side
-constexpr int bwd_tg(int C) { return C <= kThreads / 2 ? 8 : (C <= kThreads ? 4 : 2); }  // at most four rows of a thread
+constexpr int bwd_tg(int C) { return C <= kThreads / 2 ? 8 : 4; }  // 16 x 768 x 777: 63 us with four lanes along a row, 72 with two and two workgroups a CU
 
 // Whether the kernels that hold an item's tile in registers serve a call: up to 1024 channels (four or eight groups of a tensor a
 // thread), rows of a group at least, items whose byte offsets fit 32 bits.
-constexpr int kMaxInRegisters = 4 * kThreads / 2;
+constexpr int kMaxInRegisters = 8 * kThreads / 4;
 static_assert(kMaxInRegisters == 8 * kFwdLanes, "one limit for both passes");
 bool in_registers(int C, int T, size_t element) { return C <= kMaxInRegisters && T >= (int)(16 / element) && (size_t)C * T * element < (size_t)1 << 32; }
 
@@ -821,8 +821,17 @@ hipError_t bwd_rows(const NormBwd &p, hipStream_t s)
     case 1: return p.layer ? bwd_rows_of<S, TG, 1, true>(p, s) : bwd_rows_of<S, TG, 1, false>(p, s);
     case 2: return p.layer ? bwd_rows_of<S, TG, 2, true>(p, s) : bwd_rows_of<S, TG, 2, false>(p, s);
     case 3: return p.layer ? bwd_rows_of<S, TG, 3, true>(p, s) : bwd_rows_of<S, TG, 3, false>(p, s);
-    default: return p.layer ? bwd_rows_of<S, TG, 4, true>(p, s) : bwd_rows_of<S, TG, 4, false>(p, s);
+    case 4: return p.layer ? bwd_rows_of<S, TG, 4, true>(p, s) : bwd_rows_of<S, TG, 4, false>(p, s);
     }
+    if constexpr (TG == 4) {
+        switch ((p.C * TG + kThreads - 1) / kThreads) {
+        case 5: return p.layer ? bwd_rows_of<S, TG, 5, true>(p, s) : bwd_rows_of<S, TG, 5, false>(p, s);
+        case 6: return p.layer ? bwd_rows_of<S, TG, 6, true>(p, s) : bwd_rows_of<S, TG, 6, false>(p, s);
+        case 7: return p.layer ? bwd_rows_of<S, TG, 7, true>(p, s) : bwd_rows_of<S, TG, 7, false>(p, s);
+        case 8: return p.layer ? bwd_rows_of<S, TG, 8, true>(p, s) : bwd_rows_of<S, TG, 8, false>(p, s);
+        }
+    }
+    return hipErrorInvalidValue;  // (in_registers() lets no more through)
 }
 template <typename S>
 hipError_t bwd_any(const NormBwd &p, hipStream_t s)
@@ -831,8 +840,7 @@ hipError_t bwd_any(const NormBwd &p, hipStream_t s)
         residual_norm_bwd_plain_kernel<S><<<dim3((unsigned)p.B * p.splits), dim3(kPlainThreads), 0, s>>>(p, plain_positions(p.T));
         return hipGetLastError();
     }
-    const int tg = bwd_tg(p.C);
-    return tg == 8 ? bwd_rows<S, 8>(p, s) : (tg == 4 ? bwd_rows<S, 4>(p, s) : bwd_rows<S, 2>(p, s));
+    return bwd_tg(p.C) == 8 ? bwd_rows<S, 8>(p, s) : bwd_rows<S, 4>(p, s);
 }
 
 int check_shape(int B, int C, int T, int dtype)

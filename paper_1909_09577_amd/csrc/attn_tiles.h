@@ -113,7 +113,31 @@ struct Mma<bf16_t> {
         }
         return out;
     }
-    // the `along` operand of 32 channels from row d0 on, and its product with up to NC columns' probabilities
+    // Twice as many bits: what the rounding leaves is a second operand.  ds takes this form: it is made with the delta of rounded outputs,
+    // and the two errors together would be a third more than those that the stored outputs have anyway.
+    // Products of channels with the block's values, eight of a lane's at a time, so that few operands are in registers at once.
+    template <int ND>
+    static __device__ __forceinline__ void add_in_two_terms(f32x16_t (&acc)[ND], const unsigned char *block, int lane, const f32x16_t &p)
+    {
+        const int row = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            u32x4_t hi, lo;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = p[8 * s + 2 * j], b = p[8 * s + 2 * j + 1];
+                hi[j] = pack_bf16x2(a, b);
+                lo[j] = pack_bf16x2(a - __uint_as_float(hi[j] << 16), b - __uint_as_float(hi[j] & 0xffff0000u));
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const bf16x8_t rows = *reinterpret_cast<const bf16x8_t *>(block + granule(32 * d + row, 2 * s + half));
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows, __builtin_bit_cast(bf16x8_t, lo), acc[d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows, __builtin_bit_cast(bf16x8_t, hi), acc[d], 0, 0, 0);
+            }
+        }
+    }
+    // the `along` operand of 32 channels from row d0 on, and its product with a block's probabilities
     struct Along {
         bf16x8_t s[2];
     };
@@ -165,6 +189,12 @@ struct Mma<float> {
     static __device__ __forceinline__ Frag flipped(Frag a, uint32_t flip) { return __uint_as_float(__float_as_uint(a) ^ flip); }
     static __device__ __forceinline__ float dot(Frag a, Frag b) { return a * b; }
     static __device__ __forceinline__ Probs probs(const f32x16_t &p) { return p; }
+    template <int ND>
+    static __device__ __forceinline__ void add_in_two_terms(f32x16_t (&acc)[ND], const unsigned char *block, int lane, const f32x16_t &p)
+    {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] = mul(along(block, d * 32, lane), p, acc[d]);
+    }
     struct Along {
         f32x4_t s[4];
     };

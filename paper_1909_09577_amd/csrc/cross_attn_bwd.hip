@@ -30,6 +30,10 @@ struct TokenRows {  // of a tile of tokens
     int lo[TT], hi[TT], range[2];
 };
 
+// Of the widest heads, keys and values of a wavefront's positions and both sums do not fit the registers of two wavefronts a SIMD: the
+// values stay in LDS (60 registers went to scratch memory otherwise).
+constexpr bool values_in_lds(bool bf16, int DP) { return bf16 && DP > 96; }
+
 template <typename S, int DP, int NB, int NW>
 __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
 {
@@ -38,6 +42,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     typedef Tile<S, DP, NB, NT> T;
     typedef TokenRows<TT> Rows;
     constexpr int kBuf = 2 * T::kBytes + (int)((sizeof(Rows) + 15) / 16 * 16);
+    constexpr bool kValuesInLds = values_in_lds(sizeof(S) == 2, DP);
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
@@ -47,7 +52,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     const int w0 = (tile * NW + wave) * 32, t = w0 + (lane & 31);
     const float c = (a.flip ? -0.5f : 0.5f) * a.c;
     const int t_first = tile * NW * 32, t_last = t_first + NW * 32;
-    typename M::Frag kf[KS], vf[KS];
+    typename M::Frag kf[KS], vf[kValuesInLds ? 1 : KS];
+    unsigned char *values = smem + 2 * kBuf;
     OwnColumns<S, DP, NW> k_own, v_own;
     if (t_first < len) {  // (uniform)
         k_own.load((const S *)a.k + (size_t)b * a.ks + (size_t)kvh * a.D * a.T, a.D, a.T, t_first);
@@ -116,10 +122,15 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     if (i < unit_end) load(i);
     if (t_first < len) {
         k_own.take(smem, a.D, a.T, len, t_first, wave, lane, kf);
-        v_own.take(smem, a.D, a.T, len, t_first, wave, lane, vf);
+        if constexpr (kValuesInLds)
+            v_own.own.write(values, a.D, a.T, len, t_first, threadIdx.x);  // (read behind the barrier of the first unit)
+        else
+            v_own.take(smem, a.D, a.T, len, t_first, wave, lane, vf);
     }
-    int off[2];
+    values += wave * OwnColumns<S, DP, NW>::Own::kBlock;
+    int off[2], own_off[2];
     M::template across_offsets<true>(lane, off);
+    M::template across_offsets<false>(lane, own_off);
     for (int after; i < unit_end; i = after, turn ^= 1) {
         unsigned char *buf = smem + turn * kBuf;
         Rows &rows = *reinterpret_cast<Rows *>(buf + 2 * T::kBytes);
@@ -159,7 +170,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
 #pragma unroll
             for (int st = 0; st < KS; ++st) {
                 s = M::mul(M::across(qb, off, st), kf[st], s);
-                dp = M::mul(M::across(gb, off, st), vf[st], dp);
+                if constexpr (kValuesInLds)
+                    dp = M::mul(M::across(gb, off, st), M::across(values, own_off, st), dp);
+                else
+                    dp = M::mul(M::across(gb, off, st), vf[st], dp);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -177,12 +191,11 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
                     dp[r] = ok ? dp[r] : 0.f;
                 }
             }
-            const typename M::Probs pp = M::probs(s), ds = M::probs(dp);
+            const typename M::Probs pp = M::probs(s);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) {
-                dv[d] = M::mul(M::along(gb, d * 32, lane), pp, dv[d]);
-                dk[d] = M::mul(M::along(qb, d * 32, lane), ds, dk[d]);
-            }
+            for (int d = 0; d < DP / 32; ++d) dv[d] = M::mul(M::along(gb, d * 32, lane), pp, dv[d]);
+            __builtin_amdgcn_sched_barrier(0);
+            M::add_in_two_terms(dk, qb, lane, dp);
         }
     }
     __syncthreads();  // (the tiles give way to the results)
@@ -365,9 +378,7 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
                     dp[r] = t >= lo && t < hi ? dp[r] : 0.f;
                 }
             }
-            const typename M::Probs ds = M::probs(dp);
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d) acc[d] = M::mul(M::along(kb, d * 32, lane), ds, acc[d]);
+            M::add_in_two_terms(acc, kb, lane, dp);
         }
     };
     if constexpr (SHARED) {
@@ -464,8 +475,10 @@ hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
     constexpr int NB = token_blocks(sizeof(S) == 2, DP);
-    constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
-    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, out = kWaves * DP * 128;
+    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes;
+    constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16)) +
+                          (values_in_lds(sizeof(S) == 2, DP) ? own : 0);
+    constexpr int out = kWaves * DP * 128;
     constexpr int bytes = tiles > own ? (tiles > out ? tiles : out) : (own > out ? own : out);
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;

@@ -9,6 +9,7 @@ been built, loading raises: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -655,6 +656,7 @@ def _item_ptr(t, dtype, shape, name):
     return t.data_ptr(), step
 
 
+@functools.lru_cache(maxsize=1024)
 def nm_cross_attn_workspace_bytes(op: int, B, heads, kv_heads, D, U, T, dtype=NM_BF16) -> int:
     return int(lib().nm_cross_attn_workspace_bytes(op, B, heads, kv_heads, D, U, T, dtype))
 
@@ -763,6 +765,7 @@ def nm_residual_norm_fwd(x, f=None, *, gate=None, rscale=None, post_norm=None, p
     return (x if f is None else y), n
 
 
+@functools.lru_cache(maxsize=1024)
 def nm_residual_norm_bwd_workspace_bytes(B, C, T, dtype=NM_BF16) -> int:
     return int(lib().nm_residual_norm_bwd_workspace_bytes(B, C, T, dtype))
 

@@ -365,8 +365,9 @@ struct AttnArgs {
     float *lse;
     float *part, *part_ml;  // sums of the workgroups that share tokens, their maxima and sums
     float *delta;           // [B][H][U]
-    int col_tiles, splits, tiles_per_split;
+    int col_tiles, splits;
     int head_tiles;  // column tiles of a head, or 0: tiles run over the heads that share keys and values
+    int head_waves_log;  // log2 of the heads whose tokens a workgroup's wavefronts take side by side
     float *kv_part;  // [parts][2][B][Hkv][D][T]: sums of the workgroups that share positions
     int pos_tiles, parts, units_per_part;
 };
@@ -394,6 +395,33 @@ struct OwnColumns {
 #pragma unroll
         for (int s = 0; s < KS; ++s) f[s] = M::across(smem + wave * Own::kBlock, off, s);
         __syncthreads();
+    }
+};
+
+// The same for a wavefront with a block of its own, through LDS of its own.  (Rows of a group at least: shorter ones have no tiles
+// of several heads.)
+template <typename S, int DP>
+struct WaveColumns {
+    typedef Tile<S, DP, 1, 64> Own;
+    typedef Mma<S> M;
+    Own own;
+    __device__ __forceinline__ void load(const S *rows, int D, int len, int t0, int lane)
+    {
+        typename Own::Places at;
+        at.set(D, len, lane);
+        own.load(rows, at, len, t0, lane);
+    }
+    template <int KS>
+    __device__ __forceinline__ void take(unsigned char *block, int D, int len, int valid, int t0, int lane, typename M::Frag (&f)[KS])
+    {
+        int off[2];
+        M::template across_offsets<false>(lane, off);
+        wave_fence();
+        own.write(block, D, len, valid, t0, lane);
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) f[s] = M::across(block, off, s);
+        wave_fence();
     }
 };
 

@@ -10,7 +10,7 @@ namespace nm {
 constexpr int kMaxSplits = 64;
 
 struct AttnPlan {
-    int col_tiles, head_tiles, splits, tiles_per_split;   // of the forward pass or of dq
+    int col_tiles, head_tiles, head_waves_log, splits;   // of the forward pass or of dq
     int pos_tiles, parts, units_per_part;     // of dk and dv
     size_t part_bytes, ml_bytes, kv_part_bytes;  // of workspace
 };

@@ -27,7 +27,8 @@ constexpr int kReach = 256;  // tiles of tokens
 template <int TT>
 struct TokenRows {  // of a tile of tokens
     float lse[TT], delta[TT];  // log-sum-exp in halves of powers of two, infinite where a token is not there
-    int lo[TT], hi[TT], range[2];
+    int lo[TT], hi[TT];
+    int range[4];  // frames that some token looks at; those that all of them look at
 };
 
 // Of the widest heads, keys and values of a wavefront's positions and both sums do not fit the registers of two wavefronts a SIMD: the
@@ -147,13 +148,18 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
             }
             if (a.windows) {
                 int lo = some ? row_lo : a.T, hi = some ? row_hi : 0;
+                int all_lo = some || threadIdx.x >= TT ? row_lo : a.T, all_hi = some ? row_hi : (threadIdx.x >= TT ? a.T : 0);
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) {
                     lo = min(lo, __shfl_xor(lo, d));
                     hi = max(hi, __shfl_xor(hi, d));
+                    all_lo = max(all_lo, __shfl_xor(all_lo, d));
+                    all_hi = min(all_hi, __shfl_xor(all_hi, d));
                 }
                 rows.range[0] = lo;  // (the same value from every lane)
                 rows.range[1] = hi;
+                rows.range[2] = all_lo;
+                rows.range[3] = all_hi;
             }
         }
         __syncthreads();
@@ -161,6 +167,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
         if (after < unit_end) load(after);
         if (w0 >= len) continue;
         if (a.windows && (rows.range[0] >= w0 + 32 || rows.range[1] <= w0)) continue;
+        const bool masked = a.windows && (rows.range[2] > w0 || rows.range[3] < w0 + 32);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const unsigned char *qb = buf + n * T::kBlock, *gb = qb + T::kBytes;
@@ -182,7 +189,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
                 s[r] = p;
                 dp[r] = p * (dp[r] - rows.delta[u]);
             }
-            if (a.windows) {
+            if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int u = 32 * n + M::position(r, half);
@@ -254,8 +261,9 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
     int g, u;
     bool exists;
     if (a.head_tiles) {
-        g = ct / a.head_tiles;
-        u = ((ct - g * a.head_tiles) * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        const int gt = ct / a.head_tiles, log = a.head_waves_log;
+        g = (gt << log) + (block & ((1 << log) - 1));
+        u = ((ct - gt * a.head_tiles) * ((SHARED ? NW : 1) >> log) + (block >> log)) * 32 + (lane & 31);
         exists = u < a.U;
     } else {
         const int m = (ct * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
@@ -300,7 +308,9 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         }
         __syncthreads();
     }
-    const int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+    // this workgroup's share of the tiles between them
+    const int t_first = first / TT, t_last = (last + TT - 1) / TT, t_share = (t_last - t_first + a.splits - 1) / a.splits;
+    const int t_begin = t_first + split * t_share, t_end = min(t_last, t_begin + t_share);
 
     // the first tiles and the tokens are loaded together
     T kt, vt;
@@ -318,7 +328,7 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         const S *orow = (const S *)a.o + (size_t)b * a.os + item;
         bool taken = false;
         if constexpr (SHARED) {
-            if (a.head_tiles) {  // (uniform)
+            if (a.head_tiles && a.head_waves_log == 0) {  // (uniform)
                 const int u0 = (ct - g * a.head_tiles) * NW * 32;
                 OwnColumns<S, DP, NW> q_own, g_own, o_own;
                 o_own.load(orow, a.D, a.U, u0);
@@ -329,6 +339,20 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
 #pragma unroll
                 for (int s = 0; s < KS; ++s) delta += M::dot(q[s], go[s]);
                 q_own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
+                taken = true;
+            } else if (a.head_tiles) {
+                const int u0 = __builtin_amdgcn_readfirstlane(exists ? u : a.U);
+                unsigned char *own = smem + wave * DP * M::kRow;
+                WaveColumns<S, DP> q_own, g_own, o_own;
+                o_own.load(orow, a.D, a.U, u0, lane);
+                g_own.load(gr, a.D, a.U, u0, lane);
+                q_own.load(qr, a.D, a.U, u0, lane);
+                o_own.take(own, a.D, a.U, q_len, u0, lane, q);
+                g_own.take(own, a.D, a.U, q_len, u0, lane, go);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) delta += M::dot(q[s], go[s]);
+                q_own.take(own, a.D, a.U, q_len, u0, lane, q);
+                __syncthreads();
                 taken = true;
             }
         }

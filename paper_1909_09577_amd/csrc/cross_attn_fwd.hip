@@ -20,11 +20,11 @@ constexpr float kLag = 8.f;
 
 // Wavefronts of a SIMD that the registers are made to last for: two, and four where a workgroup's eight wavefronts have narrow heads
 // (a tile's groups are then few for each of them).
-template <typename S, int DP, int NW>
-constexpr int kSimdWaves = sizeof(S) * DP > 256 ? NW / 4 : (NW == 8 && sizeof(S) * DP <= 128 ? 4 : 2);
+template <typename S, int DP, int NW, bool SHARED>
+constexpr int kSimdWaves = sizeof(S) * DP > 256 ? NW / 4 : (NW == 8 && SHARED && sizeof(S) * DP <= 128 ? 4 : 2);
 
 template <typename S, int DP, int NB, int NW, bool SHARED>
-__global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW>)) void attn_fwd_kernel(AttnArgs a)
+__global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW, SHARED>)) void attn_fwd_kernel(AttnArgs a)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;
@@ -43,8 +43,9 @@ __global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW>)) void attn_fwd_ker
     int g, u;
     bool exists;
     if (a.head_tiles) {
-        g = ct / a.head_tiles;
-        u = ((ct - g * a.head_tiles) * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
+        const int gt = ct / a.head_tiles, log = a.head_waves_log;
+        g = (gt << log) + (block & ((1 << log) - 1));
+        u = ((ct - gt * a.head_tiles) * ((SHARED ? NW : 1) >> log) + (block >> log)) * 32 + (lane & 31);
         exists = u < a.U;
     } else {
         const int m = (ct * (SHARED ? NW : 1) + block) * 32 + (lane & 31);
@@ -84,7 +85,9 @@ __global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW>)) void attn_fwd_ker
         }
         __syncthreads();
     }
-    const int t_begin = max(first / TT, split * a.tiles_per_split), t_end = min((last + TT - 1) / TT, (split + 1) * a.tiles_per_split);
+    // this workgroup's share of the tiles between them
+    const int t_first = first / TT, t_last = (last + TT - 1) / TT, t_share = (t_last - t_first + a.splits - 1) / a.splits;
+    const int t_begin = t_first + split * t_share, t_end = min(t_last, t_begin + t_share);
 
     // the first tiles and the tokens are loaded together
     T kt, vt;
@@ -100,11 +103,18 @@ __global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW>)) void attn_fwd_ker
         const S *rows = (const S *)a.q + (size_t)b * a.qs + (size_t)head * a.D * a.U;
         bool taken = false;
         if constexpr (SHARED) {
-            if (a.head_tiles) {  // (uniform)
+            if (a.head_tiles && a.head_waves_log == 0) {  // (uniform)
                 const int u0 = (ct - g * a.head_tiles) * NW * 32;
                 OwnColumns<S, DP, NW> own;
                 own.load(rows, a.D, a.U, u0);
                 own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
+                taken = true;
+            } else if (a.head_tiles) {
+                const int u0 = __builtin_amdgcn_readfirstlane(exists ? u : a.U);
+                WaveColumns<S, DP> own;
+                own.load(rows, a.D, a.U, u0, lane);
+                own.take(smem + wave * DP * M::kRow, a.D, a.U, q_len, u0, lane, q);
+                __syncthreads();
                 taken = true;
             }
         }
@@ -342,9 +352,10 @@ hipError_t run(AttnArgs a, hipStream_t s)
 constexpr int kApartColumns = 32;
 // Few columns go apart (but float tiles of wide heads, one per wavefront, do not fit the registers).  Of the others, 256 share keys and
 // values where there are that many: they are then read and written to LDS half as often.
+constexpr int apart_waves(bool bf16, int DP) { return bf16 && DP <= 64 ? 8 : 8; }  // as many as tiles of 32 positions fit LDS and registers for
 AttnForm form_of(bool bf16, int DP, int U, int G)
 {
-    if ((long long)U * G <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, 4, 2};
+    if ((long long)U * G <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, apart_waves(bf16, DP), 1};
     if (bf16 && U > 128) return {256, 64, 1, DP <= 64 ? 2 : 1};
     return {128, bf16 ? 64 : 32, 1, 2};
 }
@@ -355,7 +366,7 @@ hipError_t run_form(const AttnArgs &a, hipStream_t s)
     constexpr bool bf16 = sizeof(S) == 2;
     const AttnForm f = form_of(bf16, DP, a.U, a.G);
     if constexpr (bf16 || DP <= 64) {
-        if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, 4, false>(a, s);
+        if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, apart_waves(bf16, DP), false>(a, s);
     }
     if constexpr (bf16) {
         if (f.columns == 256) return run<S, DP, 2, 8, true>(a, s);

@@ -669,12 +669,14 @@ def _attn_dims(q, k, heads, kv_heads, where):
     return B, heads, kv_heads, HD // heads, U, k.shape[2]
 
 
-def _attn_workspace(op, dims, code, workspace, like):
+def _attn_workspace(op, dims, code, workspace, like, stream):
     if workspace is None:
         need = nm_cross_attn_workspace_bytes(op, *dims, code)
         if not need:
             return None, None, 0
         workspace = like.new_empty(need, dtype=_torch().uint8)
+        if stream is not None:
+            workspace.record_stream(stream)
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -694,7 +696,7 @@ def nm_cross_attn_fwd(q, k, v, *, heads, kv_heads=None, scale=None, lengths=None
     op, os_ = _item_ptr(o, q.dtype, (B, H * D, U), "o")
     if lse is None and want_lse:
         lse = q.new_empty((B, H, U), dtype=torch.float32)
-    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_FWD, dims, code, workspace, q)
+    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_FWD, dims, code, workspace, q, stream)
     st = lib().nm_cross_attn_fwd(
         *dims, qp, qs, kp, ks, vp, vs, _ptr(lengths, torch.int32, (B,), "lengths"),
         _ptr(q_lengths, torch.int32, (B,), "q_lengths"), _ptr(windows, torch.int32, (B, U, 2), "windows"),
@@ -719,7 +721,7 @@ def nm_cross_attn_bwd(do, q, k, v, o, lse, *, heads, kv_heads=None, scale=None, 
            for a in _item_ptr(t, q.dtype, shape, name)]
     outs = [a for t, shape, name in ((dq, q_shape, "dq"), (dk, kv_shape, "dk"), (dv, kv_shape, "dv"))
             for a in _item_ptr(t, q.dtype, shape, name)]
-    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_BWD, dims, code, workspace, q)
+    ws, ws_ptr, ws_bytes = _attn_workspace(NM_OP_ATTN_BWD, dims, code, workspace, q, stream)
     st = lib().nm_cross_attn_bwd(
         *dims, *ins, _ptr(lse, torch.float32, (B, H, U), "lse"), _ptr(lengths, torch.int32, (B,), "lengths"),
         _ptr(q_lengths, torch.int32, (B,), "q_lengths"), _ptr(windows, torch.int32, (B, U, 2), "windows"),
@@ -754,12 +756,12 @@ def nm_residual_norm_fwd(x, f=None, *, gate=None, rscale=None, post_norm=None, p
         n = torch.empty_like(x)
     kind, gp = _gate_kind(gate, x)
     flags = (NM_NORM_POST if post else 0) | (NM_NORM_NEXT if next_norm else 0) | (NM_NORM_LAYER if layer else 0)
-    vec = lambda t, name: _ptr(t, torch.float32, (C,), name)  # noqa: E731
-    act = lambda t, name: _ptr(t, x.dtype, (B, C, T), name)  # noqa: E731
+    dt, f32, all_, c = x.dtype, torch.float32, x.shape, (C,)
     st = lib().nm_residual_norm_fwd(
-        B, C, T, act(x, "x"), act(f, "f"), gp, kind, vec(rscale, "rscale"), vec(post_weight, "post_weight"),
-        vec(post_bias, "post_bias"), vec(next_weight, "next_weight"), vec(next_bias, "next_bias"), eps,
-        _ptr(lengths, torch.int32, (B,), "lengths"), act(y, "y"), act(n, "n"), flags, _dtype_code(x), _stream(stream))
+        B, C, T, _ptr(x, name="x"), _ptr(f, dt, all_, "f"), gp, kind, _ptr(rscale, f32, c, "rscale"),
+        _ptr(post_weight, f32, c, "post_weight"), _ptr(post_bias, f32, c, "post_bias"), _ptr(next_weight, f32, c, "next_weight"),
+        _ptr(next_bias, f32, c, "next_bias"), eps, _ptr(lengths, torch.int32, (B,), "lengths"), _ptr(y, dt, all_, "y"),
+        _ptr(n, dt, all_, "n"), flags, _dtype_code(x), _stream(stream))
     if st != NM_OK:
         raise NmError(st, "nm_residual_norm_fwd")
     return (x if f is None else y), n
@@ -790,12 +792,20 @@ def nm_residual_norm_bwd(dy, dn, y, f=None, *, gate=None, rscale=None, post_norm
             got[name] = None
         elif got.get(name) is None:
             got[name] = torch.empty_like(t)
-    vec = lambda t, name: _ptr(t, torch.float32, (C,), name)  # noqa: E731
-    act = lambda t, name: _ptr(t, like.dtype, (B, C, T), name)  # noqa: E731
+    shape = like.shape
+
+    def vec(t, name):
+        return t if t is None else _ptr(t, torch.float32, (C,), name)
+
+    def act(t, name):
+        return t if t is None else _ptr(t, like.dtype, shape, name)
+
     _, dgp = _gate_kind(got["dgate"], like, "dgate")
     code = _dtype_code(like)
     if workspace is None:
         workspace = like.new_empty(max(nm_residual_norm_bwd_workspace_bytes(B, C, T, code), 256), dtype=torch.uint8)
+        if stream is not None:
+            workspace.record_stream(stream)  # (it is given back when this call returns)
     st = lib().nm_residual_norm_bwd(
         B, C, T, act(dy, "dy"), act(dn, "dn"), act(y, "y"), act(f, "f"), gp, kind, vec(rscale, "rscale"),
         vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), vec(next_weight if dn is not None else None, "next_weight"), eps,

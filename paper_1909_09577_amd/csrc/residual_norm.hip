@@ -470,10 +470,9 @@ __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_k
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 asm volatile("" : "+v"(cl));
-            unpack_again(yr[i]);
+                unpack_again(yr[i]);
                 unpack_again(dnr[i]);
-                asm volatile("" : "+v"(cl));
-            unpack_again(fr[i]);
+                unpack_again(fr[i]);
                 float v[V], d[V], u[V];
                 const float there = in(i) ? 1.f : 0.f, w = next_w[channel(i)] * there;
                 Group<S>::unpack(yr[i], v);
@@ -501,7 +500,6 @@ __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_k
             asm volatile("" : "+v"(cl));
             unpack_again(yr[i]);
             unpack_again(dnr[i]);
-            asm volatile("" : "+v"(cl));
             unpack_again(fr[i]);
             float v[V], d[V], u[V];
             const float there = in(i) ? 1.f : 0.f, w = next_w[channel(i)];

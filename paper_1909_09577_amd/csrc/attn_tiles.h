@@ -396,6 +396,22 @@ struct OwnColumns {
         for (int s = 0; s < KS; ++s) f[s] = M::across(smem + wave * Own::kBlock, off, s);
         __syncthreads();
     }
+    // the same, and the operands of a second tensor's blocks, which were written behind these
+    template <int KS>
+    __device__ __forceinline__ void take(unsigned char *smem, int D, int len, int valid, int t0, int wave, int lane, typename M::Frag (&f)[KS],
+                                         typename M::Frag (&second)[KS])
+    {
+        int off[2];
+        M::template across_offsets<false>(lane, off);
+        own.write(smem, D, len, valid, t0, threadIdx.x);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            f[s] = M::across(smem + wave * Own::kBlock, off, s);
+            second[s] = M::across(smem + Own::kBytes + wave * Own::kBlock, off, s);
+        }
+        __syncthreads();
+    }
 };
 
 // The same for a wavefront with a block of its own, through LDS of its own.  (Rows of a group at least: shorter ones have no tiles

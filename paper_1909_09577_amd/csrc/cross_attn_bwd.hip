@@ -122,11 +122,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     int i = next_from(part * a.units_per_part), turn = 0;
     if (i < unit_end) load(i);
     if (t_first < len) {
-        k_own.take(smem, a.D, a.T, len, t_first, wave, lane, kf);
-        if constexpr (kValuesInLds)
+        if constexpr (kValuesInLds) {
             v_own.own.write(values, a.D, a.T, len, t_first, threadIdx.x);  // (read behind the barrier of the first unit)
-        else
-            v_own.take(smem, a.D, a.T, len, t_first, wave, lane, vf);
+            k_own.take(smem, a.D, a.T, len, t_first, wave, lane, kf);
+        } else {
+            v_own.own.write(smem + OwnColumns<S, DP, NW>::Own::kBytes, a.D, a.T, len, t_first, threadIdx.x);
+            k_own.take(smem, a.D, a.T, len, t_first, wave, lane, kf, vf);
+        }
     }
     values += wave * OwnColumns<S, DP, NW>::Own::kBlock;
     int off[2], own_off[2];
@@ -216,10 +218,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
         store_block<float, DP>(block, dv, 1.f, a.kv_part + all + to, a.D, a.T, w0, len, lane);
         return;
     }
-    unsigned char *block = smem + wave * DP * M::kRow;
+    unsigned char *block = smem + wave * 2 * DP * M::kRow;
     store_block<S, DP>(block, dk, a.scale, (S *)a.dk + (size_t)b * a.dks + item, a.D, a.T, w0, len, lane);
-    wave_fence();
-    store_block<S, DP>(block, dv, 1.f, (S *)a.dv + (size_t)b * a.dvs + item, a.D, a.T, w0, len, lane);
+    store_block<S, DP>(block + DP * M::kRow, dv, 1.f, (S *)a.dv + (size_t)b * a.dvs + item, a.D, a.T, w0, len, lane);
 }
 
 // Adds the parts of dk and dv, in order.
@@ -499,11 +500,11 @@ hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
     constexpr int NB = token_blocks(sizeof(S) == 2, DP);
-    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes;
+    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, owns = values_in_lds(sizeof(S) == 2, DP) ? own : 2 * own;
     constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16)) +
                           (values_in_lds(sizeof(S) == 2, DP) ? own : 0);
-    constexpr int out = kWaves * DP * 128;
-    constexpr int bytes = tiles > own ? (tiles > out ? tiles : out) : (own > out ? own : out);
+    constexpr int out = kWaves * DP * (sizeof(S) == 2 ? 128 : 256);
+    constexpr int bytes = tiles > owns ? (tiles > out ? tiles : out) : (owns > out ? owns : out);
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);

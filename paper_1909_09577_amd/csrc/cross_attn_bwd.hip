@@ -28,7 +28,6 @@ template <int TT>
 struct TokenRows {  // of a tile of tokens
     float lse[TT], delta[TT];  // log-sum-exp in halves of powers of two, infinite where a token is not there
     int lo[TT], hi[TT];
-    int range[4];  // frames that some token looks at; those that all of them look at
 };
 
 // Of the widest heads, keys and values of a wavefront's positions and both sums do not fit the registers of two wavefronts a SIMD: the
@@ -65,27 +64,33 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
-    // Frames that the tokens of a tile look at, so that tiles which look elsewhere are left out (as many as there is room for;
-    // tiles behind those are taken).
-    __shared__ int reach[2][kReach];
+    // Frames that some token of a tile looks at, so that tiles which look elsewhere are left out, and frames that all of them look at,
+    // which need no masks (of as many tiles as there is room for; those behind are taken, with masks).
+    __shared__ int reach[4][kReach];
     const int tiles = (q_len + TT - 1) / TT;
     if (a.windows) {
         for (int u0 = wave * 64; u0 < min(tiles * TT, kReach * TT); u0 += NT) {
             const int u = u0 + lane;
-            int lo = a.T, hi = 0;
-            if (u < q_len) frames_of(a, b, u, len, lo, hi);
-            if (lo >= hi) {
-                lo = a.T;
-                hi = 0;
+            int lo = a.T, hi = 0, all_lo = 0, all_hi = a.T;
+            if (u < q_len) {
+                frames_of(a, b, u, len, all_lo, all_hi);
+                if (all_lo < all_hi) {
+                    lo = all_lo;
+                    hi = all_hi;
+                }
             }
 #pragma unroll
             for (int d = 1; d < TT; d <<= 1) {
                 lo = min(lo, __shfl_xor(lo, d));
                 hi = max(hi, __shfl_xor(hi, d));
+                all_lo = max(all_lo, __shfl_xor(all_lo, d));
+                all_hi = min(all_hi, __shfl_xor(all_hi, d));
             }
             if (lane % TT == 0 && u / TT < kReach) {
                 reach[0][u / TT] = lo;
                 reach[1][u / TT] = hi;
+                reach[2][u / TT] = all_lo;
+                reach[3][u / TT] = all_hi;
             }
         }
         __syncthreads();
@@ -140,36 +145,23 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
         const int u0 = (i % tiles) * TT;
         qt.write(buf, a.D, a.U, q_len, u0, threadIdx.x);
         gt.write(buf + T::kBytes, a.D, a.U, q_len, u0, threadIdx.x);
-        if (threadIdx.x < 64) {
-            const bool some = threadIdx.x < TT && row_lo < row_hi;
-            if (threadIdx.x < TT) {
-                rows.lse[threadIdx.x] = some && row_lse != -INFINITY ? row_lse * (0.5f * kLog2e) : INFINITY;
-                rows.delta[threadIdx.x] = some ? row_delta : 0.f;
-                rows.lo[threadIdx.x] = row_lo;
-                rows.hi[threadIdx.x] = row_hi;
-            }
-            if (a.windows) {
-                int lo = some ? row_lo : a.T, hi = some ? row_hi : 0;
-                int all_lo = some || threadIdx.x >= TT ? row_lo : a.T, all_hi = some ? row_hi : (threadIdx.x >= TT ? a.T : 0);
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    lo = min(lo, __shfl_xor(lo, d));
-                    hi = max(hi, __shfl_xor(hi, d));
-                    all_lo = max(all_lo, __shfl_xor(all_lo, d));
-                    all_hi = min(all_hi, __shfl_xor(all_hi, d));
-                }
-                rows.range[0] = lo;  // (the same value from every lane)
-                rows.range[1] = hi;
-                rows.range[2] = all_lo;
-                rows.range[3] = all_hi;
-            }
+        if (threadIdx.x < TT) {
+            const bool some = row_lo < row_hi;
+            rows.lse[threadIdx.x] = some && row_lse != -INFINITY ? row_lse * (0.5f * kLog2e) : INFINITY;
+            rows.delta[threadIdx.x] = some ? row_delta : 0.f;
+            rows.lo[threadIdx.x] = row_lo;
+            rows.hi[threadIdx.x] = row_hi;
         }
         __syncthreads();
         after = next_from(i + 1);
         if (after < unit_end) load(after);
         if (w0 >= len) continue;
-        if (a.windows && (rows.range[0] >= w0 + 32 || rows.range[1] <= w0)) continue;
-        const bool masked = a.windows && (rows.range[2] > w0 || rows.range[3] < w0 + 32);
+        const int at_tile = u0 / TT;
+        bool masked = a.windows;
+        if (a.windows && at_tile < kReach) {
+            if (reach[0][at_tile] >= w0 + 32 || reach[1][at_tile] <= w0) continue;
+            masked = reach[2][at_tile] > w0 || reach[3][at_tile] < w0 + 32;
+        }
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const unsigned char *qb = buf + n * T::kBlock, *gb = qb + T::kBytes;

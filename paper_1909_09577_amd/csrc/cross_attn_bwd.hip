@@ -478,6 +478,7 @@ __global__ __launch_bounds__(256) void attn_dq_join_kernel(AttnArgs a)
     const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (e >= all) return;
     float v = 0.f;
+#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) v += a.part[s * all + e];
     const size_t b = e / item;
     store_from_f32((S *)a.dq, b * a.dqs + (e - b * item), v * a.scale);

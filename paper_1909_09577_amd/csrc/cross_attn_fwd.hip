@@ -292,36 +292,45 @@ __global__ __launch_bounds__(NW * 64, (kSimdWaves<S, DP, NW, SHARED>)) void attn
     }
 }
 
-// Joins the sums of `splits` workgroups, in order: a workgroup takes 64 tokens of a head, whose weights lie in LDS, and 32 channels.
+// Joins the sums of `splits` workgroups, in order: a workgroup takes 64 tokens of a head, whose weights lie in LDS, and 32 channels.  The
+// wavefronts fetch the maxima and sums of different splits (one after the other, 22 splits took 17 us).
 template <typename S>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    __shared__ float weight[kMaxSplits][64];
+    __shared__ float top_of[kMaxSplits][64], sum_of[kMaxSplits][64];
     const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
     const int tiles = (a.U + 63) / 64, bh = blockIdx.x / tiles, u = (blockIdx.x - bh * tiles) * 64 + lane;
     const int b = bh / a.H, h = bh - b * a.H;
     const size_t rows = (size_t)a.B * a.H * a.U, all = rows * a.D, row = (size_t)bh * a.U + min(u, a.U - 1);
-    if (share == 0) {
-        float top = -INFINITY, total = 0.f;
-        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[(s * rows + row) * 2]);
-        const float base = top == -INFINITY ? 0.f : top;
-        for (int s = 0; s < a.splits; ++s) {
-            const float w = __builtin_amdgcn_exp2f(a.part_ml[(s * rows + row) * 2] - base);
-            weight[s][lane] = w;
-            total += w * a.part_ml[(s * rows + row) * 2 + 1];
-        }
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        for (int s = 0; s < a.splits; ++s) weight[s][lane] *= inv;
-        if (a.lse && u < a.U && blockIdx.y == 0) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f : -INFINITY;
+#pragma unroll 4
+    for (int s = share; s < a.splits; s += 4) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (s * rows + row) * 2);
+        top_of[s][lane] = ml.x;
+        sum_of[s][lane] = ml.y;
     }
     __syncthreads();
+    float top = -INFINITY, total = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, top_of[s][lane]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) total += __builtin_amdgcn_exp2f(top_of[s][lane] - base) * sum_of[s][lane];
     if (u >= a.U) return;
-    for (int d = blockIdx.y * 32 + share; d < min(a.D, (int)blockIdx.y * 32 + 32); d += 4) {
-        const size_t e = ((size_t)bh * a.D + d) * a.U + u;
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s) v += weight[s][lane] * a.part[s * all + e];
-        store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)h * a.D + d) * a.U + u, v);
+    if (a.lse && share == 0 && blockIdx.y == 0) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f : -INFINITY;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int d0 = blockIdx.y * 32 + share;
+    const float *part = a.part + (size_t)bh * a.D * a.U + u;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    for (int s = 0; s < a.splits; ++s) {  // (eight channels' loads at a time)
+        const float w = __builtin_amdgcn_exp2f(top_of[s][lane] - base) * inv;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += w * part[s * all + (size_t)min(d0 + 4 * i, a.D - 1) * a.U];
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (d0 + 4 * i < a.D) store_from_f32((S *)a.out, (size_t)b * a.os + ((size_t)h * a.D + d0 + 4 * i) * a.U + u, v[i]);
 }
 
 // ---- which form, and its sizes --------------------------------------------------------------------------------

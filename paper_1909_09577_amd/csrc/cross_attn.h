@@ -17,7 +17,9 @@ struct AttnPlan {
 struct AttnForm {
     int columns, tile, waves;  // of a workgroup: tokens, positions of a tile, tiles that it takes at a time
     int per_cu;                // workgroups that run on a CU at a time
+    int work;                  // of a position, in those of bfloat16: float matrix instructions make an eighth as many products a cycle
 };
+constexpr int attn_work(bool bf16) { return bf16 ? 1 : 4; }  // (the rest of a round is no slower)
 // Rounds of a workgroup, of `rounds`, where `groups` workgroups may each be shared among several: as many as are fastest by an
 // estimate of round_us a round, and of writing and reading join_bytes for every share.
 int attn_share(long long groups, int rounds, double round_us, double join_bytes, int per_cu);

@@ -42,7 +42,7 @@ AttnPlan attn_plan(const AttnForm &f, int B, int H, int Hkv, int D, int U, int T
     p.head_waves_log = p.head_tiles ? log : 0;
     p.col_tiles = p.head_tiles ? (G >> log) * head_tiles : (int)(((long long)G * U + columns - 1) / columns);
     const int tiles = (T + f.tile - 1) / f.tile, rounds = (tiles + f.waves - 1) / f.waves;
-    const int per = attn_share((long long)B * Hkv * p.col_tiles, rounds, kRoundUs * D / 64 * f.tile / 64, 2.0 * 4 * B * H * U * D, f.per_cu);
+    const int per = attn_share((long long)B * Hkv * p.col_tiles, rounds, kRoundUs * f.work * D / 64 * f.tile / 64, 2.0 * 4 * B * H * U * D, f.per_cu);
     p.splits = (rounds + per - 1) / per;
     const size_t rows = (size_t)B * H * U;
     p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * rows * D * sizeof(float), 256) : 0;

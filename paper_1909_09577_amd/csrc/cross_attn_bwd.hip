@@ -512,7 +512,7 @@ bool is_shared(bool bf16, int DP, long long columns) { return columns > 32 || (!
 AttnForm form_of(bool bf16, int DP, long long columns)
 {
     const bool shared = is_shared(bf16, DP, columns);
-    return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves, 2};
+    return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves, bf16 || DP <= 64 ? 2 : 1, attn_work(bf16)};
 }
 template <typename S, int DP, bool SHARED>
 hipError_t run_dq(const AttnArgs &a, hipStream_t s)
@@ -566,7 +566,8 @@ AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
     // dk and dv: units of a tile of tokens of a head
     const int per = kWaves * 32, tokens = 32 * token_blocks(bf16, DP), units = (U + tokens - 1) / tokens * (H / Hkv);
     p.pos_tiles = (T + per - 1) / per;
-    p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D, 2);
+    p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * attn_work(bf16) * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D,
+                                  bf16 || DP <= 64 ? 2 : 1);
     p.parts = (units + p.units_per_part - 1) / p.units_per_part;
     p.kv_part_bytes = p.parts > 1 ? (size_t)p.parts * 2 * B * Hkv * D * T * sizeof(float) : 0;
     return p;

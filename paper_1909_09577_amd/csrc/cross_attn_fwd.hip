@@ -358,15 +358,14 @@ hipError_t run(AttnArgs a, hipStream_t s)
     return hipGetLastError();
 }
 
-constexpr int kApartColumns = 32;
+constexpr int kApartColumns = 32, kApartWaves = 8;  // (one token, 600 frames: 4 wavefronts 12.5 us, 8 11.1, 16 with half tiles 13.9)
 // Few columns go apart (but float tiles of wide heads, one per wavefront, do not fit the registers).  Of the others, 256 share keys and
 // values where there are that many: they are then read and written to LDS half as often.
-constexpr int apart_waves(bool bf16, int DP) { return bf16 && DP <= 64 ? 8 : 8; }  // as many as tiles of 32 positions fit LDS and registers for
 AttnForm form_of(bool bf16, int DP, int U, int G)
 {
-    if ((long long)U * G <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, apart_waves(bf16, DP), 1};
-    if (bf16 && U > 128) return {256, 64, 1, DP <= 64 ? 2 : 1};
-    return {128, bf16 ? 64 : 32, 1, 2};
+    if ((long long)U * G <= kApartColumns && (bf16 || DP <= 64)) return {32, bf16 && DP <= 64 ? 64 : 32, kApartWaves, 1, attn_work(bf16)};
+    if (bf16 && U > 128) return {256, 64, 1, DP <= 64 ? 2 : 1, 1};
+    return {128, bf16 ? 64 : 32, 1, bf16 || DP <= 64 ? 2 : 1, attn_work(bf16)};
 }
 
 template <typename S, int DP>
@@ -375,7 +374,7 @@ hipError_t run_form(const AttnArgs &a, hipStream_t s)
     constexpr bool bf16 = sizeof(S) == 2;
     const AttnForm f = form_of(bf16, DP, a.U, a.G);
     if constexpr (bf16 || DP <= 64) {
-        if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, apart_waves(bf16, DP), false>(a, s);
+        if (f.columns == 32) return run<S, DP, bf16 && DP <= 64 ? 2 : 1, kApartWaves, false>(a, s);
     }
     if constexpr (bf16) {
         if (f.columns == 256) return run<S, DP, 2, 8, true>(a, s);

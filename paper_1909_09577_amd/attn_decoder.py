@@ -261,7 +261,7 @@ def main():
     dec = AttentionDecoder(vocab, 256, 4, 2, 256, kv_heads=2, seed=1)
     for i in range(400):
         batch = spelled(32, room, 96, vocab, 256, dec.dtype, seed=i)
-        loss, _ = dec.step(*batch, lr=2e-3 * min(1.0, (i + 1) / 50))
+        loss, _ = dec.step(*batch, lr=2e-3 * min((i + 1) / 50, (400 - i) / 350))
         if i % 50 == 0 or i == 399:
             print(f"step {i}: loss {loss.item():.3f}", flush=True)
     ins, targets, states, n, frames = spelled(8, room, 96, vocab, 256, dec.dtype, seed=10 ** 6)

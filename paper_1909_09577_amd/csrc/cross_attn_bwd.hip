@@ -6,6 +6,12 @@
 // log-sum-exp: two of seven products, against writing and reading them.  In each kernel the result of the first products (scores
 // and dp) is the second operand of the next ones, in the registers it was made in (attn_tiles.h).  Where either has too few
 // workgroups, several share one's positions or tokens, and their sums are joined by another kernel, in order.
+//
+// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: dq 57 us, dk and dv 76 (215 MB that have to move: 1.6 TB/s);
+// 4 x 333 tokens with windows of a quarter of 3001 frames, 8 heads of 128 over 2: dq 37 and 8 for the join, dk and dv 55 and 12.  Of
+// the cycles of the former's dk and dv the matrix pipes are busy in 14 %, the vector units in 33 %, with 1.4 of two possible wavefronts a
+// SIMD on average: a workgroup has two or three tiles of tokens between its first loads and its stores.  Three wavefronts a SIMD send 44
+// registers to scratch memory (95 us); loads two tiles ahead changed nothing.
 #include "cross_attn.h"
 
 namespace nm {

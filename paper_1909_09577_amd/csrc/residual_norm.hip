@@ -9,6 +9,11 @@
 // Rows of any length: the last group of a row is read from where the row's last whole group begins, so that some of its
 // positions are there twice.  Both copies hold the same values and are stored over each other; sums over time leave one out.
 // Rows shorter than a group go to kernels that work by elements.
+//
+// Bound by memory, and by the phases of a workgroup that loads, sums, stores: forward, 32 x 1024 x 800, bfloat16: 58 us when inputs come
+// from the Infinity Cache, 74 from memory (2.8 TB/s); backward, 16 x 768 x up to 777 with a gate per element: 60 and 4 for the sums over
+// time (78 from memory, 1.7 TB/s): 300 tiles that are not padding on 256 CUs, one a CU.  Backward with 1024 threads a tile: 69 us (scratch
+// memory); without the selections between summands in whole tiles: no change.
 #include "../../include/nm_norm.h"
 #include "../../include/nm_conv1d.h"
 #include "nm_common.h"

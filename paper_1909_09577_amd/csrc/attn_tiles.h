@@ -370,6 +370,7 @@ struct AttnArgs {
     int head_waves_log;  // log2 of the heads whose tokens a workgroup's wavefronts take side by side
     float *kv_part;  // [parts][2][B][Hkv][D][T]: sums of the workgroups that share positions
     int pos_tiles, parts, units_per_part;
+    int dq_first;  // the workgroups of dq come before those of dk and dv
 };
 
 // A workgroup's NW blocks of a head's tokens or positions as operands of its wavefronts, through LDS (`smem`).  All that a kernel wants

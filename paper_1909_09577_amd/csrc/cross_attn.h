@@ -12,6 +12,7 @@ constexpr int kMaxSplits = 64;
 struct AttnPlan {
     int col_tiles, head_tiles, head_waves_log, splits;   // of the forward pass or of dq
     int pos_tiles, parts, units_per_part;     // of dk and dv
+    bool dq_first;                            // workgroups of dq take longer
     size_t part_bytes, ml_bytes, kv_part_bytes;  // of workspace
 };
 struct AttnForm {

@@ -198,7 +198,7 @@ int nm_cross_attn_bwd(int B, int heads, int kv_heads, int D, int U, int T, const
     a.delta = (float *)workspace;
     a.part = (float *)((char *)workspace + delta_bytes);
     a.kv_part = (float *)((char *)workspace + delta_bytes + p.part_bytes);
-    a.pos_tiles = p.pos_tiles; a.parts = p.parts; a.units_per_part = p.units_per_part;
+    a.pos_tiles = p.pos_tiles; a.parts = p.parts; a.units_per_part = p.units_per_part; a.dq_first = p.dq_first;
     a.col_tiles = p.col_tiles; a.head_tiles = p.head_tiles; a.head_waves_log = p.head_waves_log; a.splits = p.splits;
     return dev(launch_attn_bwd(dtype == NM_BF16, a, (hipStream_t)hip_stream));
 }

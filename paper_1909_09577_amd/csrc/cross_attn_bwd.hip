@@ -1,17 +1,18 @@
 // Cross attention, backward (definition: include/nm_attention.h).
 //
-// Two kernels after one another: dq, whose workgroups own tokens and go over the positions, in the two forms of the forward pass,
-// and which leaves delta, the sums over channels of o * dout of its tokens, in the workspace; dk and dv, whose workgroups own positions
-// and go over the tokens of all heads that share them.  Scores and probabilities are made again in both from the saved
-// log-sum-exp: two of seven products, against writing and reading them.  In each kernel the result of the first products (scores
-// and dp) is the second operand of the next ones, in the registers it was made in (attn_tiles.h).  Where either has too few
-// workgroups, several share one's positions or tokens, and their sums are joined by another kernel, in order.
+// A small kernel makes delta, the sums over channels of o * dout.  Then one launch makes all three gradients: workgroups of dq own tokens
+// and go over the positions, in the two forms of the forward pass; workgroups of dk and dv own positions and go over the tokens of all
+// heads that share them.  Scores and probabilities are made again in both from the saved log-sum-exp: two of seven products,
+// against writing and reading them.  In each the result of the first products (scores and dp) is the second operand of the next ones,
+// in the registers it was made in (attn_tiles.h).  Where either has too few workgroups, several share one's positions or tokens,
+// and their sums are joined by another kernel, in order.
 //
-// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: dq 57 us, dk and dv 76 (215 MB that have to move: 1.6 TB/s);
-// 4 x 333 tokens with windows of a quarter of 3001 frames, 8 heads of 128 over 2: dq 37 and 8 for the join, dk and dv 55 and 12.  Of
-// the cycles of the former's dk and dv the matrix pipes are busy in 14 %, the vector units in 33 %, with 1.4 of two possible wavefronts a
-// SIMD on average: a workgroup has two or three tiles of tokens between its first loads and its stores.  Three wavefronts a SIMD send 44
-// registers to scratch memory (95 us); loads two tiles ahead changed nothing.
+// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: delta 7 us, gradients 114 (215 MB that have to move: 1.8 TB/s);
+// 4 x 333 tokens with windows of a quarter of 3001 frames, 8 heads of 128 over 2: 5, 70 and 19 for the join.  In launches of their own, with
+// delta made by dq, they took 57 + 76 us and 37 + 55 + 8 + 12: neither fills the chip to its end.  The former's dk and dv alone kept the matrix
+// pipes busy in 14 % of the cycles and the vector units in 33 %, with 1.4 of two possible wavefronts a SIMD on average: a
+// workgroup has two or three tiles of tokens between its first loads and its stores.  Three wavefronts a SIMD sent 44 registers to
+// scratch memory (76 -> 95 us); loads two tiles ahead changed nothing.
 #include "cross_attn.h"
 
 namespace nm {
@@ -41,7 +42,7 @@ struct TokenRows {  // of a tile of tokens
 constexpr bool values_in_lds(bool bf16, int DP) { return bf16 && DP > 96; }
 
 template <typename S, int DP, int NB, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_dkv(const AttnArgs &a, const int id)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = NW * 64, KS = DP / M::kSteps;
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
     constexpr bool kValuesInLds = values_in_lds(sizeof(S) == 2, DP);
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int bh = id % (a.B * a.Hkv), rest = id / (a.B * a.Hkv);
     const int tile = rest % a.pos_tiles, part = rest / a.pos_tiles;
     const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
     const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
@@ -223,10 +224,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= 256 ? 2 : 1) void attn_d
 
 // Adds the parts of dk and dv, in order.
 template <typename S>
-__global__ __launch_bounds__(256) void attn_dkv_join_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_dkv_join(const AttnArgs &a, unsigned id)
 {
     const size_t item = (size_t)a.Hkv * a.D * a.T, all = item * a.B;
-    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t e = (size_t)id * 256 + threadIdx.x;
     if (e >= all) return;
     float k = 0.f, v = 0.f;
 #pragma unroll 4
@@ -241,14 +242,14 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(AttnArgs a)
 
 // ---- dq: a wavefront's columns are tokens, rows are positions; shared and apart as in the forward pass ---------------------
 template <typename S, int DP, int NB, int NW, bool SHARED>
-__global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192) ? 2 : 1) void attn_dq_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_dq(const AttnArgs &a, const int id)
 {
     typedef Mma<S> M;
     constexpr int TT = NB * 32, NT = SHARED ? NW * 64 : 64, KS = DP / M::kSteps;
     typedef Tile<S, DP, NB, NT> T;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int bh = id % (a.B * a.Hkv), rest = id / (a.B * a.Hkv);
     const int ct = rest % a.col_tiles, split = rest / a.col_tiles;
     const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
     const int len = a.len ? clipped(a.len[b], a.T) : a.T, q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
@@ -281,7 +282,9 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
         first = lo;
         last = hi;
         if (lo < hi) {
-            lse = a.lse[((size_t)b * a.H + head) * a.U + u] * (0.5f * kLog2e);
+            const size_t row = ((size_t)b * a.H + head) * a.U + u;
+            lse = a.lse[row] * (0.5f * kLog2e);
+            delta = a.delta[row];
             if (lse == -INFINITY) lse = INFINITY;
         }
     }
@@ -324,32 +327,23 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
     {
         const size_t item = (size_t)head * a.D * a.U;
         const S *qr = (const S *)a.q + (size_t)b * a.qs + item, *gr = (const S *)a.dout + (size_t)b * a.dos + item;
-        const S *orow = (const S *)a.o + (size_t)b * a.os + item;
         bool taken = false;
         if constexpr (SHARED) {
             if (a.head_tiles && a.head_waves_log == 0) {  // (uniform)
                 const int u0 = (ct - g * a.head_tiles) * NW * 32;
-                OwnColumns<S, DP, NW> q_own, g_own, o_own;
-                o_own.load(orow, a.D, a.U, u0);
+                OwnColumns<S, DP, NW> q_own, g_own;
                 g_own.load(gr, a.D, a.U, u0);
                 q_own.load(qr, a.D, a.U, u0);
-                o_own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
                 g_own.take(smem, a.D, a.U, q_len, u0, wave, lane, go);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) delta += M::dot(q[s], go[s]);
                 q_own.take(smem, a.D, a.U, q_len, u0, wave, lane, q);
                 taken = true;
             } else if (a.head_tiles) {
                 const int u0 = __builtin_amdgcn_readfirstlane(exists ? u : a.U);
                 unsigned char *own = smem + wave * DP * M::kRow;
-                WaveColumns<S, DP> q_own, g_own, o_own;
-                o_own.load(orow, a.D, a.U, u0, lane);
+                WaveColumns<S, DP> q_own, g_own;
                 g_own.load(gr, a.D, a.U, u0, lane);
                 q_own.load(qr, a.D, a.U, u0, lane);
-                o_own.take(own, a.D, a.U, q_len, u0, lane, q);
                 g_own.take(own, a.D, a.U, q_len, u0, lane, go);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) delta += M::dot(q[s], go[s]);
                 q_own.take(own, a.D, a.U, q_len, u0, lane, q);
                 __syncthreads();
                 taken = true;
@@ -360,13 +354,10 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
             for (int s = 0; s < KS; ++s) {
                 q[s] = M::column(qr + u, s, half, a.D, a.U, there);
                 go[s] = M::column(gr + u, s, half, a.D, a.U, there);
-                delta += M::dot(M::column(orow + u, s, half, a.D, a.U, there), go[s]);
             }
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = M::flipped(q[s], a.flip);
-        delta = half_sum(delta);
-        if (exists && half == 0 && split == 0 && (SHARED || wave == 0)) a.delta[((size_t)b * a.H + head) * a.U + u] = delta;
     }
     f32x16_t acc[DP / 32];
 #pragma unroll
@@ -478,10 +469,10 @@ __global__ __launch_bounds__(NW * 64, (int)sizeof(S) * DP <= (SHARED ? 256 : 192
 
 // Adds the parts of dq of `splits` workgroups, in order.
 template <typename S>
-__global__ __launch_bounds__(256) void attn_dq_join_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_dq_join(const AttnArgs &a, unsigned id)
 {
     const size_t item = (size_t)a.H * a.D * a.U, all = item * a.B;
-    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t e = (size_t)id * 256 + threadIdx.x;
     if (e >= all) return;
     float v = 0.f;
 #pragma unroll 8
@@ -490,26 +481,60 @@ __global__ __launch_bounds__(256) void attn_dq_join_kernel(AttnArgs a)
     store_from_f32((S *)a.dq, b * a.dqs + (e - b * item), v * a.scale);
 }
 
+// Both joins in one launch, as far as there are parts.
+template <typename S>
+__global__ __launch_bounds__(256) void attn_bwd_join_kernel(AttnArgs a, unsigned dq_groups)
+{
+    if (blockIdx.x < dq_groups)
+        attn_dq_join<S>(a, blockIdx.x);
+    else
+        attn_dkv_join<S>(a, blockIdx.x - dq_groups);
+}
+
+// ---- delta: the sums over channels of o * dout of every token, 64 tokens of a head and four shares of the channels a workgroup ------
+template <typename S>
+__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a)
+{
+    __shared__ float parts[4][64];
+    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
+    const int tiles = (a.U + 63) / 64, bh = blockIdx.x / tiles, u = (blockIdx.x - bh * tiles) * 64 + lane;
+    const int b = bh / a.H, h = bh - b * a.H;
+    const int q_len = a.q_len ? clipped(a.q_len[b], a.U) : a.U;
+    float v = 0.f;
+    if (u < q_len) {
+        const S *o = (const S *)a.o + (size_t)b * a.os + (size_t)h * a.D * a.U + u, *g = (const S *)a.dout + (size_t)b * a.dos + (size_t)h * a.D * a.U + u;
+#pragma unroll 8
+        for (int d = share; d < a.D; d += 4) v += load_as_f32(o, (size_t)d * a.U) * load_as_f32(g, (size_t)d * a.U);
+    }
+    parts[share][lane] = v;
+    __syncthreads();
+    if (share == 0 && u < a.U) a.delta[(size_t)bh * a.U + u] = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
+}
+
+// All three gradients in one launch: few workgroups of either leave the chip half empty.  Those that take longer come first.
+template <typename S, int DP, int NBQ, int NBKV, int NW, bool SHARED>
+__global__ __launch_bounds__(NW * 64, sizeof(S) * DP <= (SHARED ? 256 : 192) ? 2 : 1) void attn_bwd_kernel(AttnArgs a, int dq_groups, int dkv_groups)
+{
+    const int id = a.dq_first ? (int)blockIdx.x - dq_groups : (int)blockIdx.x;
+    if (id >= 0 && id < dkv_groups)
+        attn_dkv<S, DP, NBKV, NW>(a, id);
+    else
+        attn_dq<S, DP, NBQ, NW, SHARED>(a, a.dq_first ? (int)blockIdx.x : (int)blockIdx.x - dkv_groups);
+}
+
 // ---- sizes ------------------------------------------------------------------------------------------------------
 constexpr int kWaves = 4;
 constexpr int token_blocks(bool bf16, int DP) { return bf16 && DP <= 96 ? 2 : 1; }  // of a tile of the kernel of dk and dv
 
 template <typename S, int DP>
-hipError_t run_dkv(const AttnArgs &a, hipStream_t s)
+constexpr int dkv_lds()
 {
-    static LdsOptIn opt;
     constexpr int NB = token_blocks(sizeof(S) == 2, DP);
     constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, owns = values_in_lds(sizeof(S) == 2, DP) ? own : 2 * own;
     constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16)) +
                           (values_in_lds(sizeof(S) == 2, DP) ? own : 0);
     constexpr int out = kWaves * DP * (sizeof(S) == 2 ? 128 : 256);
-    constexpr int bytes = tiles > owns ? (tiles > out ? tiles : out) : (owns > out ? owns : out);
-    static_assert(bytes <= 160 * 1024, "LDS of a CU");
-    auto *fn = attn_dkv_kernel<S, DP, NB, kWaves>;
-    const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
-    if (e != hipSuccess) return e;
-    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.pos_tiles * a.parts), dim3(kWaves * 64), bytes, s>>>(a);
-    return hipGetLastError();
+    return tiles > owns ? (tiles > out ? tiles : out) : (owns > out ? owns : out);
 }
 
 constexpr bool two_blocks(bool bf16, int DP, bool shared) { return bf16 && (shared || DP <= 64); }
@@ -521,29 +546,29 @@ AttnForm form_of(bool bf16, int DP, long long columns)
     return {shared ? 128 : 32, two_blocks(bf16, DP, shared) ? 64 : 32, shared ? 1 : kWaves, bf16 || DP <= 64 ? 2 : 1, attn_work(bf16)};
 }
 template <typename S, int DP, bool SHARED>
-hipError_t run_dq(const AttnArgs &a, hipStream_t s)
+hipError_t run(const AttnArgs &a, hipStream_t s)
 {
     static LdsOptIn opt;
     constexpr int NB = two_blocks(sizeof(S) == 2, DP, SHARED) ? 2 : 1, NT = SHARED ? kWaves * 64 : 64;
     constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? kWaves * DP * 128 : kWaves * DP / 32 * 16 * 64 * 4;
-    constexpr int bytes = tiles > join ? tiles : join;  // (a workgroup's tokens fit the room of its results)
-    static_assert(bytes <= 160 * 1024, "LDS of a CU");
-    auto *fn = attn_dq_kernel<S, DP, NB, kWaves, SHARED>;
+    constexpr int dq = tiles > join ? tiles : join, dkv = dkv_lds<S, DP>();  // (a workgroup's tokens fit the room of its results)
+    constexpr int bytes = dq > dkv ? dq : dkv;
+    static_assert(bytes + 4 * kReach * 4 <= 160 * 1024, "LDS of a CU");
+    auto *fn = attn_bwd_kernel<S, DP, NB, token_blocks(sizeof(S) == 2, DP), kWaves, SHARED>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
     if (e != hipSuccess) return e;
-    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.col_tiles * a.splits), dim3(kWaves * 64), bytes, s>>>(a);
+    attn_delta_kernel<S><<<dim3((unsigned)(a.B * a.H) * ((a.U + 63) / 64)), dim3(256), 0, s>>>(a);
+    const int dkv_groups = a.B * a.Hkv * a.pos_tiles * a.parts, dq_groups = a.B * a.Hkv * a.col_tiles * a.splits;
+    fn<<<dim3((unsigned)dkv_groups + dq_groups), dim3(kWaves * 64), bytes, s>>>(a, dq_groups, dkv_groups);
     return hipGetLastError();
 }
 template <typename S, int DP>
 hipError_t run_both(const AttnArgs &a, hipStream_t s)
 {
-    hipError_t e = hipSuccess;
-    if (is_shared(sizeof(S) == 2, DP, (long long)a.G * a.U)) {
-        e = run_dq<S, DP, true>(a, s);
-    } else {
-        if constexpr (sizeof(S) == 2 || DP <= 64) e = run_dq<S, DP, false>(a, s);
+    if constexpr (sizeof(S) == 2 || DP <= 64) {
+        if (!is_shared(sizeof(S) == 2, DP, (long long)a.G * a.U)) return run<S, DP, false>(a, s);
     }
-    return e == hipSuccess ? run_dkv<S, DP>(a, s) : e;
+    return run<S, DP, true>(a, s);
 }
 template <typename S>
 hipError_t run_any(const AttnArgs &a, hipStream_t s)
@@ -554,15 +579,16 @@ hipError_t run_any(const AttnArgs &a, hipStream_t s)
     else if (a.D <= 96) e = run_both<S, 96>(a, s);
     else e = run_both<S, 128>(a, s);
     if (e != hipSuccess) return e;
-    if (a.splits > 1) attn_dq_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
-    if (a.parts > 1) attn_dkv_join_kernel<S><<<dim3((unsigned)(((size_t)a.B * a.Hkv * a.T * a.D + 255) / 256)), dim3(256), 0, s>>>(a);
+    const unsigned dq_groups = a.splits > 1 ? (unsigned)(((size_t)a.B * a.H * a.U * a.D + 255) / 256) : 0;
+    const unsigned dkv_groups = a.parts > 1 ? (unsigned)(((size_t)a.B * a.Hkv * a.T * a.D + 255) / 256) : 0;
+    if (dq_groups + dkv_groups) attn_bwd_join_kernel<S><<<dim3(dq_groups + dkv_groups), dim3(256), 0, s>>>(a, dq_groups);
     return hipGetLastError();
 }
 
 }  // namespace
 
 // a unit of the kernel of dk and dv, in microseconds at 64 tokens and channels
-constexpr double kUnitUs = 2.0;
+constexpr double kUnitUs = 2.0, kDqRoundUs = 1.5;  // (and a tile of dq)
 
 AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
 {
@@ -575,6 +601,9 @@ AttnPlan attn_bwd_plan(bool bf16, int B, int H, int Hkv, int D, int U, int T)
     p.units_per_part = attn_share((long long)B * Hkv * p.pos_tiles, units, kUnitUs * attn_work(bf16) * DP / 64 * tokens / 64, 2.0 * 2 * 4 * B * Hkv * T * D,
                                   bf16 || DP <= 64 ? 2 : 1);
     p.parts = (units + p.units_per_part - 1) / p.units_per_part;
+    const AttnForm f = form_of(bf16, DP, columns);
+    const int rounds = ((T + f.tile - 1) / f.tile + f.waves * p.splits - 1) / (f.waves * p.splits);
+    p.dq_first = rounds * kDqRoundUs * f.tile > p.units_per_part * kUnitUs * tokens;  // (both at 64 positions or tokens, of as many channels)
     p.kv_part_bytes = p.parts > 1 ? (size_t)p.parts * 2 * B * Hkv * D * T * sizeof(float) : 0;
     return p;
 }

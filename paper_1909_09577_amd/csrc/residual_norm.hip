@@ -7,7 +7,8 @@
 // over the wavefronts through LDS, always in the same order.
 //
 // Rows of any length: the last group of a row is read from where the row's last whole group begins, so that some of its
-// positions are there twice.  Both copies hold the same values and are stored over each other; sums over time leave one out.
+// positions are there twice, in one workgroup or in two neighbouring ones.  Both copies are made in full from the same inputs and
+// stored over each other; sums over time leave one out.
 // Rows shorter than a group go to kernels that work by elements.
 //
 // Bound by memory, and by the phases of a workgroup that loads, sums, stores: forward, 32 x 1024 x 800, bfloat16: 58 us when inputs come
@@ -182,7 +183,8 @@ __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(NormFwd p)
     const S *x = (const S *)p.x + item, *f = p.f ? (const S *)p.f + item : nullptr;
     S *y = (S *)p.y + item, *n = (S *)p.n + item;
     auto at = [&](int i) { return (uint32_t)(min(cl + i * CL, p.C - 1) * p.T + t0) * (uint32_t)sizeof(S); };
-    const bool any = tile * TW < len;  // (uniform) some position is no padding
+    // (uniform) some position that the tile stores is no padding: a last tile of less than a group stores positions of the one before
+    const bool any = min(tile * TW, p.T - V) < len;
 
     u32x4_t xr[NR], fr[NR];
     if (any) {

@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_k
         auto put = [&](S *to, int i, u32x4_t v) {
             if (store && in(i)) store_group<S>(to, at(i), first_positions<S>(v, len - t0));
         };
-        if (tile * TW >= len) {  // (uniform) padding
+        if (min(tile * TW, p.T - V) >= len) {  // (uniform) all that the tile stores is padding
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 put(dx, i, zero);

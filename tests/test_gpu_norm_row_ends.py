@@ -46,3 +46,26 @@ def test_forward(case, dtype, gate, layer):
         check(y, ry, STEP[dtype] * np.abs(ry) + slack * size, "y")
         _, rn = orc.norm_fwd(y, layer=layer, lengths=left, next_weight=a["next_weight"], next_bias=a["next_bias"])
         check(host(n)[:, :, at:], rn, STEP[dtype] * np.abs(rn) + slack * (4 + np.abs(rn).max()), "n")
+
+
+@pytest.mark.parametrize("gate,layer", [(None, False), ("element", True), ("item", False)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_backward(case, dtype, gate, layer):
+    C, T, B, whole = case
+    a, dev, lengths, ln = make(C, T, B, dtype, gate, layer)
+    kw = {k: dev[k] for k in VECTORS + ("gate",)}
+    at, cut, left = ends(a, lengths, T, whole)
+    names = ("rscale", "post_weight", "post_bias", "next_weight", "gate")
+    r = orc.norm_bwd(cut["dy"], cut["dn"], cut["y"], cut["f"], post=True, layer=layer, lengths=left, **{k: cut[k] for k in names})
+    worst = (C + 64) * 2.0 ** -24 * 30
+    for _ in range(3):
+        got = nm.nm_residual_norm_bwd(dev["dy"], dev["dn"], dev["y"], dev["f"], layer=layer, lengths=ln, **kw)
+        for name, of in (("dx", "dx"), ("df", "df")) + ((("dgate", "dgate_element"),) if gate == "element" else ()):
+            check(host(got[name])[:, :, at:], r[of], STEP[dtype] * np.abs(r[of]) + worst * (1 + np.abs(r[of]).max()), name)
+        if not whole:
+            continue
+        if gate == "item":
+            check(host(got["dgate"]), r["dgate_item"], (worst + (T + 8) * 2.0 ** -24) * (1 + r["abs_dgate_item"]), "dgate")
+        for name in ("drscale", "dpost_weight", "dnext_weight") + (("dpost_bias", "dnext_bias") if layer else ()):
+            check(host(got[name]), r[name], (worst + (B * T + 8) * 2.0 ** -24) * (1 + r["abs_" + name]), name)

@@ -3,11 +3,20 @@
 
 #include "attn_tiles.h"
 
+#include <initializer_list>
 #include <math.h>
 
 namespace nm {
 
 constexpr int kMaxSplits = 64;
+
+// Bytes of LDS of a workgroup whose phases want these
+constexpr int most(std::initializer_list<int> phases)
+{
+    int bytes = 0;
+    for (const int b : phases) bytes = b > bytes ? b : bytes;
+    return bytes;
+}
 
 struct AttnPlan {
     int col_tiles, head_tiles, head_waves_log, splits;   // of the forward pass or of dq

@@ -530,11 +530,14 @@ template <typename S, int DP>
 constexpr int dkv_lds()
 {
     constexpr int NB = token_blocks(sizeof(S) == 2, DP);
-    constexpr int own = Tile<S, DP, kWaves, kWaves * 64>::kBytes, owns = values_in_lds(sizeof(S) == 2, DP) ? own : 2 * own;
-    constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16)) +
-                          (values_in_lds(sizeof(S) == 2, DP) ? own : 0);
+    constexpr int own = OwnColumns<S, DP, kWaves>::Own::kBytes;
+    constexpr int tiles = 2 * (2 * Tile<S, DP, NB, kWaves * 64>::kBytes + (int)((sizeof(TokenRows<NB * 32>) + 15) / 16 * 16));
     constexpr int out = kWaves * DP * (sizeof(S) == 2 ? 128 : 256);
-    return tiles > owns ? (tiles > out ? tiles : out) : (owns > out ? owns : out);
+    if (values_in_lds(sizeof(S) == 2, DP)) {  // the values lie behind the tiles, whose place the keys take before
+        static_assert(!values_in_lds(sizeof(S) == 2, DP) || own <= tiles, "keys in front of the values");
+        return most({tiles + own, out});
+    }
+    return most({tiles, 2 * own, out});
 }
 
 constexpr bool two_blocks(bool bf16, int DP, bool shared) { return bf16 && (shared || DP <= 64); }
@@ -551,8 +554,8 @@ hipError_t run(const AttnArgs &a, hipStream_t s)
     static LdsOptIn opt;
     constexpr int NB = two_blocks(sizeof(S) == 2, DP, SHARED) ? 2 : 1, NT = SHARED ? kWaves * 64 : 64;
     constexpr int tiles = (SHARED ? 4 : kWaves * 2) * Tile<S, DP, NB, NT>::kBytes, join = SHARED ? kWaves * DP * 128 : kWaves * DP / 32 * 16 * 64 * 4;
-    constexpr int dq = tiles > join ? tiles : join, dkv = dkv_lds<S, DP>();  // (a workgroup's tokens fit the room of its results)
-    constexpr int bytes = dq > dkv ? dq : dkv;
+    constexpr int own = SHARED ? most({OwnColumns<S, DP, kWaves>::Own::kBytes, kWaves * WaveColumns<S, DP>::Own::kBytes}) : 0;  // of dq's tokens
+    constexpr int bytes = most({tiles, join, own, dkv_lds<S, DP>()});
     static_assert(bytes + 4 * kReach * 4 <= 160 * 1024, "LDS of a CU");
     auto *fn = attn_bwd_kernel<S, DP, NB, token_blocks(sizeof(S) == 2, DP), kWaves, SHARED>;
     const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);

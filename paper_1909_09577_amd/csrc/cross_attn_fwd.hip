@@ -344,12 +344,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 template <typename S, int DP, int NB, int NW, bool SHARED>
 constexpr int lds_bytes()
 {
-    if constexpr (SHARED) {
-        constexpr int tiles = 4 * Tile<S, DP, NB, NW * 64>::kBytes, out = NW * DP * 128;  // (room for results as float blocks)
-        return tiles > out ? tiles : out;
+    if constexpr (SHARED) {  // two tiles of keys and of values in turn; before them the workgroup's tokens, after them its results as float blocks
+        return most({4 * Tile<S, DP, NB, NW * 64>::kBytes, OwnColumns<S, DP, NW>::Own::kBytes, NW * WaveColumns<S, DP>::Own::kBytes, NW * DP * 128});
     }
-    constexpr int tiles = NW * 2 * Tile<S, DP, NB, 64>::kBytes, join = NW * 128 * 4 + NW * (DP / 32 * 16) * 64 * 4;
-    return tiles > join ? tiles : join;
+    return most({NW * 2 * Tile<S, DP, NB, 64>::kBytes, NW * 128 * 4 + NW * (DP / 32 * 16) * 64 * 4});
 }
 
 template <typename S, int DP, int NB, int NW, bool SHARED>

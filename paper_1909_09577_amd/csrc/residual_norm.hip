@@ -552,9 +552,9 @@ __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_k
             for (int j = 0; j < V; ++j) {
                 hat[j] = (hat[j] - ym[j]) * yrs[j];
                 g[i][j] += yrs[j] * (d[j] * w - hat[j] * ya[j] - yb[j]);
-                const float dj = j >= first && j < last ? d[j] : 0.f;
-                sw += dj * hat[j];
-                sb += dj;
+                const bool counts = j >= first && j < last;  // (hat is NaN in the padding where eps is 0)
+                sw += counts ? d[j] * hat[j] : 0.f;
+                sb += counts ? d[j] : 0.f;
             }
             keep(kDnw, i, sw);
             keep(kDnb, i, sb);

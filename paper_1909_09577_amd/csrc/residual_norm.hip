@@ -529,12 +529,12 @@ __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_k
         sum_columns(lds, s);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            yrs[j] = 1.f / sqrtf(s[0][j] * per_c + p.eps);
+            yrs[j] = p.next ? 1.f / sqrtf(s[0][j] * per_c + p.eps) : 0.f;  // (infinite without an eps, as y is zero there)
             ya[j] = s[1][j] * yrs[j] * per_c;
             frs[j] = p.post ? 1.f / sqrtf(s[2][j] * per_c + p.eps) : 1.f;
         }
-        // g, in the place of dy and dn; dx and the sums over time of the norm of y.  (Without that norm dn = 0, and all of this
-        // adds nothing to dy.)
+        // g, in the place of dy and dn; dx and the sums over time of the norm of y.  (Without that norm y, dn and yrs are zero, and
+        // all of this adds nothing to dy.)
         float g[NR][V];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {

@@ -34,3 +34,18 @@ def test_padding(shape, dtype, layer):
                                   lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"), **{k: dev[k] for k in names})
     r = orc.norm_bwd(a["dy"], a["dn"], a["y"], a["f"], post=True, layer=layer, eps=0.0, lengths=lengths, **{k: a[k] for k in names})
     compare(got, r, dtype, B, C, T, ("drscale", "dpost_weight", "dnext_weight") + (("dpost_bias", "dnext_bias") if layer else ()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_no_next_norm(shape, dtype):
+    B, C, T = shape
+    a = arrays(B, C, T, dtype, None, False)
+    dev = on_device(a, dtype)
+    got = nm.nm_residual_norm_bwd(dev["dy"], None, None, dev["f"], rscale=dev["rscale"], post_weight=dev["post_weight"], eps=0.0)
+    r = orc.norm_bwd(a["dy"], None, None, a["f"], rscale=a["rscale"], post=True, post_weight=a["post_weight"], eps=0.0)
+    assert (host(got["dx"]) == a["dy"]).all()
+    compare(got, r, dtype, B, C, T, ("drscale", "dpost_weight"))
+    got = nm.nm_residual_norm_bwd(dev["dy"], None, None, dev["f"], rscale=dev["rscale"], eps=0.0)
+    r = orc.norm_bwd(a["dy"], None, None, a["f"], rscale=a["rscale"], eps=0.0)
+    compare(got, r, dtype, B, C, T, ("drscale",))

@@ -21,7 +21,8 @@
  *
  * Conventions are those of nm_conv1d.h.  The tensors of a step are described once, in a plan: nm_adamw_plan writes it into
  * host memory, the caller copies those bytes to the device and hands both copies to every step.  A plan holds addresses: the
- * tensors stay where they are while it is in use.  No tensor of a plan overlaps another.
+ * tensors stay where they are while it is in use.  No tensor of a plan overlaps another, and together
+ * they have less than 2^24 runs of 4096 elements (a tensor's last run may be shorter).
  */
 #ifndef NM_ADAMW_H
 #define NM_ADAMW_H

@@ -23,7 +23,9 @@
  *    probabilities are float32; in NM_BF16 mode p is rounded to bfloat16 as an operand of the second product, ds to two such terms.
  *  - a tensor is [batch][channels][positions] with dense rows; *_stride is the distance of its batch items in elements
  *    (at least channels * positions, so that keys and values may be the halves of one projection's output).
- *  - D is at most 128; kv_heads divides heads; a tensor spans fewer than 2^40 elements, an item of it fewer than 2^31.
+ *  - D is at most 128; kv_heads divides heads; a tensor spans fewer than 2^40 elements, an item of it fewer than 2^31.  Larger batches
+ *    than a launch can have work items for (from B * kv_heads = 2^23, B * heads * ceil(U/32) or B * kv_heads * ceil(T/32) = 2^24 on) are
+ *    unsupported.
  *  - lengths, q_lengths [B] int32 and windows [B][U][2] int32 are optional (NULL); any values are taken, clipped to the
  *    sequence.  Keys and values at t >= lengths[b] are not used, whatever they hold (NaN included); dk and dv are 0 there.
  *    Those below it that are outside a token's window count for other tokens: they have to be finite.

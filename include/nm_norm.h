@@ -22,7 +22,9 @@
  * Conventions are those of nm_conv1d.h.  dtype is the storage type of x, f, y, n, an element gate and their gradients;
  * rscale, weights, biases, an item gate and their gradients are float; all arithmetic is float32.  lengths [B] int32 (NULL:
  * none): positions at or beyond an item's length are not read; y, n, dx, df and an element gate's gradient are zero there,
- * and they add nothing to the sums.  C is at most 8192, B at most 65000.
+ * and they add nothing to the sums.  C is at most 8192, B at most 65000, and
+ * B*C*T below 2^31; the forward pass takes no more than some 2^28 positions in bfloat16, 2^27 in float (which calls of 16 channels
+ * or fewer can reach).
  */
 #ifndef NM_NORM_H
 #define NM_NORM_H

@@ -257,7 +257,7 @@ bool check_tensors(const nm_adamw_tensor *t, int count, int bits, long long *blo
         *blocks += b;
         *chunks += (b + kChunkBlocks - 1) / kChunkBlocks;
     }
-    return *chunks < (1LL << 31);
+    return *chunks < (1LL << 24);  // workgroups of 256: a launch has less than 2^32 work items
 }
 size_t plan_size(int count, long long chunks)
 {

@@ -786,11 +786,17 @@ int bwd_splits(int B, int C, int T, int dtype)
     return tiles < want ? tiles : want;
 }
 
+// Workgroups of the forward pass
+size_t fwd_groups(int B, int C, int T, size_t element)
+{
+    const int width = in_registers(C, T, element) ? kFwdTG * (int)(16 / element) : plain_positions(T);
+    return (size_t)B * ((T + width - 1) / width);
+}
+
 template <typename S, int NR>
 hipError_t fwd_rows(const NormFwd &p, hipStream_t s)
 {
-    constexpr int TW = kFwdTG * Group<S>::V;
-    const dim3 grid = eights((size_t)p.B * ((p.T + TW - 1) / TW));
+    const dim3 grid = eights(fwd_groups(p.B, p.C, p.T, sizeof(S)));
     if (p.layer)
         residual_norm_fwd_kernel<S, kFwdTG, NR, true><<<grid, dim3(kThreads), 0, s>>>(p);
     else
@@ -801,8 +807,7 @@ template <typename S>
 hipError_t fwd_any(const NormFwd &p, hipStream_t s)
 {
     if (!in_registers(p.C, p.T, sizeof(S))) {
-        const int positions = plain_positions(p.T);
-        residual_norm_fwd_plain_kernel<S><<<dim3((unsigned)p.B * ((p.T + positions - 1) / positions)), dim3(kPlainThreads), 0, s>>>(p, positions);
+        residual_norm_fwd_plain_kernel<S><<<dim3((unsigned)fwd_groups(p.B, p.C, p.T, sizeof(S))), dim3(kPlainThreads), 0, s>>>(p, plain_positions(p.T));
         return hipGetLastError();
     }
     return p.C <= 4 * kFwdLanes ? fwd_rows<S, 4>(p, s) : fwd_rows<S, 8>(p, s);
@@ -881,6 +886,8 @@ int nm_residual_norm_fwd(int B, int C, int T, const void *x, const void *f, cons
     if ((gate_kind != NM_GATE_NONE) != (gate != nullptr) || (f != nullptr) != (y != nullptr) || next != (n != nullptr)) return NM_ERR_BAD_ARG;
     if (!f && (!next || post || gate || rscale)) return NM_ERR_BAD_ARG;
     if ((!post && (post_weight || post_bias)) || (!next && (next_weight || next_bias)) || (!layer && (post_bias || next_bias))) return NM_ERR_BAD_ARG;
+    static_assert(kThreads == 512 && kPlainThreads == 512, "the limit below");
+    if (fwd_groups(B, C, T, dtype == NM_BF16 ? 2 : 4) > (1u << 23) - 8) return NM_ERR_UNSUPPORTED;  // a launch has less than 2^32 work items
     const size_t bytes = (size_t)B * C * T * (dtype == NM_BF16 ? 2 : 4), gate_bytes = gate_kind == NM_GATE_ITEM ? (size_t)B * C * 4 : bytes;
     if (overlap(y, bytes, x, bytes) || overlap(y, bytes, f, bytes) || overlap(y, bytes, gate, gate_bytes) || overlap(n, bytes, x, bytes) ||
         overlap(n, bytes, f, bytes) || overlap(n, bytes, gate, gate_bytes) || overlap(n, bytes, y, bytes))

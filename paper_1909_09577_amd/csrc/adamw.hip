@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
             bool plain = true;  // all of the lane's v have a float root
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const double gj = g[j] * gs;
+                const double gj = (double)g[j] * (double)gs;
                 m[j] = a.beta1_d * ((double)mf[j] * ms) + a.one_minus_beta1_d * gj;
                 const double rj = (double)rf[j] * rs;
                 v[j] = a.beta2_d * (rj * rj) + a.one_minus_beta2_d * (gj * gj);

@@ -871,6 +871,8 @@ def nm_adamw_plan(params, grads, m, v, *, m_scales=None, v_scales=None, copies=N
 def nm_adamw_step(plan: AdamWPlan, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, step, grad_scale=None, seed=0, stream=None) -> None:
     """One step over the tensors of the plan; step counts from 1.  grad_scale: float32 device tensor of one element that multiplies
     the gradients.  seed: of the rounding of 8-bit states, another one each step."""
+    if grad_scale is not None and grad_scale.numel() != 1:
+        raise ValueError(f"grad_scale must have one element, got {grad_scale.numel()}")
     st = lib().nm_adamw_step(plan.host.data_ptr(), plan.device.data_ptr(), plan.host.numel(), lr, beta1, beta2, eps, step,
                              _ptr(grad_scale, _torch().float32, None, "grad_scale"), seed & 0xFFFFFFFF, _stream(stream))
     if st != NM_OK:

@@ -780,6 +780,8 @@ def nm_residual_norm_bwd(dy, dn, y, f=None, *, gate=None, rscale=None, post_norm
     returned it.  Gradients of vectors are made for those that are given (float32); out: a dict of tensors to write them to."""
     torch = _torch()
     like = dn if dy is None else dy
+    if like is None:
+        raise NmError(NM_ERR_BAD_ARG, "nm_residual_norm_bwd")
     B, C, T = like.shape
     post = (post_weight is not None) if post_norm is None else bool(post_norm)
     kind, gp = _gate_kind(gate, like)

@@ -15,7 +15,7 @@
  * the high (r) half of 32 bits mixed from `seed` and the element's number (below).  Rounded to nearest, a moment that
  * changes by less than half a step per call, as v with its beta2 always does, would never move.  An r above zero does not
  * become zero (it becomes 2^-9 of the scale: m/r stays bounded).  All of this is decided in 64-bit arithmetic.  Moments
- * that are infinite or NaN are stored as NaN and left out of the block's maximum.
+ * that are infinite, NaN or larger than 448 times the largest float are stored as NaN and left out of the block's maximum.
  *   bits of element e: 256*(blocks of the plan in front of its tensor) + (its index in the tensor), mod 2^32;
  *   h = e*0x9E3779B9 ^ seed;  h = (h ^ h>>16)*0x6A09E667;  h = (h ^ h>>13)*0xBB67AE85;  h ^ h>>16        (mod 2^32)
  *

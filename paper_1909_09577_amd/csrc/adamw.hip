@@ -90,6 +90,8 @@ __device__ __forceinline__ uint32_t mixed(uint32_t times_element, uint32_t seed)
     return h ^ (h >> 16);
 }
 
+constexpr double kLargest = 448.0 * 0x1.fffffep127;  // moment whose scale is a float; larger ones count as infinite
+
 // The scale of a block from each lane's largest finite magnitude: rounding to float and the division keep the order, so the
 // lanes' own scales are reduced.
 __device__ __forceinline__ float block_scale(double amax)
@@ -200,10 +202,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 update[j] = (float)m[j] * __builtin_amdgcn_rcpf((float)r[j] * a.root_correction + a.eps);  // (an ulp or two; the denominator is no subnormal)
-                // (a comparison with infinity is false for a NaN)
+                // (comparisons are false for a NaN)
                 const double ma = fabs(m[j]);
-                if (ma < INFINITY) m_max = fmax(m_max, ma);
-                if (r[j] < INFINITY) r_max = fmax(r_max, r[j]);
+                if (ma <= kLargest) m_max = fmax(m_max, ma);
+                if (r[j] <= kLargest) r_max = fmax(r_max, r[j]);
             }
             const float m_scale = block_scale(m_max), r_scale = block_scale(r_max);
             const double per_m = reciprocal(m_scale), per_r = reciprocal(r_scale);
@@ -215,8 +217,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Record *__restrict__ r
                 uint32_t cm = e4m3_steps(ma * per_m, u & 0xffffu) | (m[j] < 0.0 ? 0x80u : 0u);
                 uint32_t cr = e4m3_steps(r[j] * per_r, u >> 16);
                 if (cr == 0 && r[j] > 0.0) cr = 1;
-                if (!(ma < INFINITY)) cm = 0x7fu;
-                if (!(r[j] < INFINITY)) cr = 0x7fu;
+                if (!(ma <= kLargest)) cm = 0x7fu;
+                if (!(r[j] <= kLargest)) cr = 0x7fu;
                 mc[j] = (unsigned char)cm;
                 rc[j] = (unsigned char)cr;
             }

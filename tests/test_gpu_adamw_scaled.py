@@ -43,3 +43,22 @@ def test_a_product_beyond_float():
     got = step(host, 1e9)[0]
     assert np.isfinite(got[3]).all() and np.isfinite(got[5]).all()
     assert not (got[2] & 127 == 127).any() and not (got[4] == 127).any() and (got[4][:300] > 0).all()
+
+
+def test_moments_that_no_scale_reaches():
+    """They are stored as NaN, each by itself: the rest of their block keeps its values."""
+    host = [draw8(600, 5)]
+    p, g, mc, ms, rc, rs = (a.copy() for a in host[0])
+    g *= 1e-20
+    g[[7, 300]] = 1e30, -1e35
+    scale = float(np.float32(1e20))
+    got = step([(p, g, mc, ms, rc, rs)], scale)[0]
+    assert np.flatnonzero(got[2] & 127 == 127).tolist() == [7, 300] == np.flatnonzero(got[4] == 127).tolist()
+    rest = np.ones(600, bool)
+    rest[[7, 300]] = False
+    h = g.copy()
+    h[~rest], mc[~rest], rc[~rest] = 0, 0, 0  # the oracle without them
+    _, rmc, rms, rrc, rrs = orc.adamw8(p, h, mc, ms, rc, rs, 0, 77, 3, weight_decay=0.02, grad_scale=scale, **HYPER)
+    assert (got[3] == rms.astype(np.float32)).all() and (got[5] == rrs.astype(np.float32)).all()
+    assert (got[2] & 127 == rmc & 127)[rest].all() and (got[4] == rrc)[rest].all()
+    assert np.isfinite(got[0][rest]).all()

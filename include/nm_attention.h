@@ -20,7 +20,8 @@
  * Conventions are those of nm_conv1d.h (device pointers the caller owns, one stream, enqueue only, argument errors before
  * any device call, deterministic results), with these additions:
  *  - dtype (NM_BF16 or NM_F32) is the storage type of q, k, v, o and their gradients; lse is float.  Sums, maxima and
- *    probabilities are float32; in NM_BF16 mode p is rounded to bfloat16 as an operand of the second product, ds to two such terms.
+ *    probabilities are float32; in NM_BF16 mode p is rounded to bfloat16 as an operand of the second product, ds to two such terms
+ *    (outputs and gradients differ from 64 bits by 1.1 to 1.4 times what rounding the results alone would make; NM_F32 has no such rounding).
  *  - a tensor is [batch][channels][positions] with dense rows; *_stride is the distance of its batch items in elements
  *    (at least channels * positions, so that keys and values may be the halves of one projection's output).
  *  - D is at most 128; kv_heads divides heads; a tensor spans fewer than 2^40 elements, an item of it fewer than 2^31.  Larger batches
@@ -28,7 +29,8 @@
  *    unsupported.
  *  - lengths, q_lengths [B] int32 and windows [B][U][2] int32 are optional (NULL); any values are taken, clipped to the
  *    sequence.  Keys and values at t >= lengths[b] are not used, whatever they hold (NaN included); dk and dv are 0 there.
- *    Those below it that are outside a token's window count for other tokens: they have to be finite.
+ *    Those below it that are outside a token's window count for other tokens: they have to be finite.  So have q and dout at
+ *    u < q_lengths[b], also of tokens whose window leaves them nothing.
  *  - U = 1 is the form for single tokens; hypotheses of a beam search that share an utterance are its U tokens.
  *  - workspace: nm_cross_attn_workspace_bytes bytes, 256-byte aligned (NULL where that is 0).
  */

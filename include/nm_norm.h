@@ -22,7 +22,8 @@
  * Conventions are those of nm_conv1d.h.  dtype is the storage type of x, f, y, n, an element gate and their gradients;
  * rscale, weights, biases, an item gate and their gradients are float; all arithmetic is float32.  lengths [B] int32 (NULL:
  * none): positions at or beyond an item's length are not read; y, n, dx, df and an element gate's gradient are zero there,
- * and they add nothing to the sums.  C is at most 8192, B at most 65000, and
+ * and they add nothing to the sums.  Up to 1024 channels (rows of 16 bytes or more) are held in registers, wider rows are read again for
+ * every sum, many times as long.  Without an eps the norm of a position of zeros is NaN.  C is at most 8192, B at most 65000, and
  * B*C*T below 2^31; the forward pass takes no more than some 2^28 positions in bfloat16, 2^27 in float (which calls of 16 channels
  * or fewer can reach).
  */

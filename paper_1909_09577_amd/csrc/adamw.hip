@@ -2,8 +2,8 @@
 //
 // Bound by memory: 30 bytes an element with float states (parameter, both moments in and out, gradient in, bfloat16 copy
 // out), 18 with 8-bit states, whose 64-bit arithmetic takes about as long: roots and reciprocals come from the float instructions
-// and steps of Newton's iteration (library roots and divisions: 1530 us instead of 1190 over 322 million weights; with float
-// states 1590 to 1840 us, 5.3 to 6.1 TB/s).  A wavefront owns a block of 256 elements, four neighbours per lane, so that every access is
+// and steps of Newton's iteration (library roots and divisions: 1530 us instead of 1190 to 1205 over 322 million weights; with
+// float states 1590 to 1845 us, 5.2 to 6.1 TB/s).  A wavefront owns a block of 256 elements, four neighbours per lane, so that every access is
 // 16 bytes (float), 8 (copy) or 4 (codes) per lane and contiguous over the wavefront, and so that the maximum of a block of
 // 8-bit states needs no LDS.  A workgroup takes kChunkBlocks blocks of one tensor; the plan names the tensor of every chunk.
 #include "../../include/nm_adamw.h"

@@ -102,7 +102,9 @@ struct Mma<bf16_t> {
         return t;
     }
 
-    static __device__ __forceinline__ Probs probs(const f32x16_t &p)  // rounds to bfloat16
+    // Rounds to bfloat16, which is what the matrix instruction takes.  Outputs are then off from 64 bits by 0.0018 to 0.0024 of their rms, against
+    // 0.0017 of the rounding of the stored result alone; two terms of p would be half as many matrix instructions again in the forward pass.
+    static __device__ __forceinline__ Probs probs(const f32x16_t &p)
     {
         Probs out;
 #pragma unroll

@@ -7,12 +7,12 @@
 // in the registers it was made in (attn_tiles.h).  Where either has too few workgroups, several share one's positions or tokens,
 // and their sums are joined by another kernel, in order.
 //
-// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: delta 7 us, gradients 114 (215 MB that have to move: 1.8 TB/s);
-// 4 x 333 tokens with windows of a quarter of 3001 frames, 8 heads of 128 over 2: 5, 70 and 19 for the join.  In launches of their own, with
+// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: delta 7 us, gradients 116 (215 MB that have to move: 1.8 TB/s);
+// 4 x 333 tokens with windows of a quarter of 3001 frames, 8 heads of 128 over 2: 5, 71 and 19 for the join.  In launches of their own, with
 // delta made by dq, they took 57 + 76 us and 37 + 55 + 8 + 12: neither fills the chip to its end.  The former's dk and dv alone kept the matrix
 // pipes busy in 14 % of the cycles and the vector units in 33 %, with 1.4 of two possible wavefronts a SIMD on average: a
 // workgroup has two or three tiles of tokens between its first loads and its stores.  Three wavefronts a SIMD sent 44 registers to
-// scratch memory (76 -> 95 us); loads two tiles ahead changed nothing.
+// scratch memory (76 -> 95 us); loads two tiles ahead changed nothing.  Heads of 65 to 96 channels in bfloat16 keep 8 bytes a lane in scratch memory.
 #include "cross_attn.h"
 
 namespace nm {

@@ -12,8 +12,8 @@
 //            for another wavefront.
 // Calls with too few workgroups for the chip share a token's positions among several, whose sums are joined by a second kernel.
 //
-// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: 34 us (96 MB that have to move: 2.8 TB/s; the longest
-// utterance's 13 tiles one after the other); 4 x 700 tokens, 7501 frames, 8 heads of 128: 126 us and 17 for the join (0.68 PFLOP/s in the
+// Measured in bfloat16: 32 x 150 tokens, up to 800 frames, 16 heads of 64: 35 us (96 MB that have to move: 2.7 TB/s; the longest
+// utterance's 13 tiles one after the other); 4 x 700 tokens, 7501 frames, 8 heads of 128: 127 us and 17 for the join (0.68 PFLOP/s in the
 // first).  Nothing is busy all the time there: matrix pipes 30 % of the cycles, vector units 28 % and as much again for
 // exponentials, LDS 26 %; a wavefront's products, exponentials and reads of LDS follow one another, and the registers hold two wavefronts
 // a SIMD.  Scores of the next block written beside the exponentials of this one (5 % slower), loads two tiles ahead and a higher priority

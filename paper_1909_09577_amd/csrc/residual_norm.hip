@@ -14,7 +14,9 @@
 // Bound by memory, and by the phases of a workgroup that loads, sums, stores: forward, 32 x 1024 x 800, bfloat16: 58 us when inputs come
 // from the Infinity Cache, 74 from memory (2.8 TB/s); backward, 16 x 768 x up to 777 with a gate per element: 60 and 4 for the sums over
 // time (78 from memory, 1.7 TB/s): 300 tiles that are not padding on 256 CUs, one a CU.  Backward with 1024 threads a tile: 69 us (scratch
-// memory); without the selections between summands in whole tiles: no change.
+// memory); without the selections between summands in whole tiles: no change.  In bfloat16 some backward instances keep a few registers
+// in scratch memory: 28 to 72 bytes a lane at 129 to 192 and 257 to 384 channels, 20 to 124 at 769 to 896 with LayerNorm and 897 to 1024.
+// 16 x 800 positions without a gate, from the Infinity Cache: 384 channels 31 us, 768 (no scratch) 57, 1024 76, with LayerNorm 98.
 #include "../../include/nm_norm.h"
 #include "../../include/nm_conv1d.h"
 #include "nm_common.h"
@@ -283,7 +285,8 @@ __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(NormFwd p)
 
 // Any number of channels, rows of any length: `positions` (a power of two up to 64) threads side by side along a row, the others
 // share the channels, and the tensors are read again for every sum.  A wavefront's threads of one position add by exchanges, the
-// wavefronts through LDS.
+// wavefronts through LDS.  Made for few positions (a decoding step), not for wide rows of many: 16 x 2048 x 800 in bfloat16 takes 598 us
+// forward and 1590 backward, 1024 channels in registers 26 and 76.
 constexpr int kPlainThreads = 512, kPlainWaves = kPlainThreads / 64;
 struct PlainSums {
     float of[kPlainWaves][64];
@@ -368,7 +371,8 @@ struct NormBwdLds {
 // Few channels have many positions in a tile (TG), so that a thread has groups enough for the work around them.
 // The per-channel vectors lie in LDS, ones and zeros for those that are not given, so that nothing branches between the rows.
 // The groups of f and of an element gate wait in LDS, each thread's its own, until g is made: five tensors' groups and all that is
-// made of them do not fit the registers.  NR = ceil(C / 128): only the last row of a thread can lie beyond the channels.
+// made of them do not fit the registers.  NR = ceil(C / CL), the channels side by side (128 with four lanes along a row, 64 with eight): only
+// the last row of a thread can lie beyond the channels.
 template <typename S, int TG, int NR, bool LAYER>
 __global__ __launch_bounds__(kThreads, NR >= 4 ? 2 : 4) void residual_norm_bwd_kernel(NormBwd p)
 {

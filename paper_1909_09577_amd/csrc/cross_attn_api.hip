@@ -62,8 +62,9 @@ int check(int B, int H, int Hkv, int D, int U, int T, int dtype)
     if ((long long)D * element > ((1LL << 32) - 1) / U || (long long)D * element > ((1LL << 32) - 1) / T) return NM_ERR_UNSUPPORTED;  // a head's rows
     if (D > kMaxD || (long long)H * D > most / U || (long long)Hkv * D > most / T || (long long)B * H > (1 << 24)) return NM_ERR_UNSUPPORTED;
     if ((long long)B * H * U > most / 2) return NM_ERR_UNSUPPORTED;
-    // The grids, with as many column tiles, position tiles and parts as there can be: below 2^32 work items.  (Workgroups of 512 take few
-    // tokens, and then all heads that share keys and values; those of 256 at least 128 tokens or positions, or one head's.)
+    // The grids, with as many column tiles, position tiles and parts as there can be: below 2^32 work items.  (Workgroups of 512 take
+    // 256 tokens, or few tokens and then those of all heads that share keys and values; those of 256 take 128 tokens or positions, or one
+    // head's if it has fewer.)
     if ((long long)B * Hkv >= 1LL << 23 || (long long)B * H * ((U + 31) / 32) >= 1LL << 24 || (long long)B * Hkv * ((T + 31) / 32) >= 1LL << 24 ||
         (long long)B * H * D > ((1LL << 31) * 256 - 1) / U)
         return NM_ERR_UNSUPPORTED;

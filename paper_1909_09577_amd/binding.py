@@ -24,6 +24,8 @@ NM_OP_FWD, NM_OP_BWD_DATA, NM_OP_BWD_WEIGHT, NM_OP_BWD, NM_OP_BN_FWD, NM_OP_BN_B
 NM_OP_ATTN_FWD, NM_OP_ATTN_BWD = 16, 17
 NM_NORM_POST, NM_NORM_NEXT, NM_NORM_LAYER = 1, 2, 4
 NM_GATE_NONE, NM_GATE_ITEM, NM_GATE_ELEMENT = 0, 1, 2
+NM_HEADS_NORM, NM_HEADS_PAIRS = 1, 2
+NM_MOST_ALTERNATIVES = 16
 
 EXPORTS = ("nm_conv1d_out_len", "nm_conv1d_workspace_bytes", "nm_strerror", "nm_conv1d_block_fwd",
            "nm_conv1d_bwd_data", "nm_conv1d_bwd_weight", "nm_conv1d_bwd", "nm_conv1d_block_fwd_masked", "nm_conv1d_bwd_data_masked",
@@ -35,7 +37,11 @@ EXPORTS = ("nm_conv1d_out_len", "nm_conv1d_workspace_bytes", "nm_strerror", "nm_
            "nm_conv1d_bwd_fp8", "nm_conv1d_fp8_bwd_workspace_bytes",
            "nm_cross_attn_workspace_bytes", "nm_cross_attn_fwd", "nm_cross_attn_bwd",
            "nm_residual_norm_fwd", "nm_residual_norm_bwd", "nm_residual_norm_bwd_workspace_bytes",
-           "nm_adamw_plan_bytes", "nm_adamw_plan", "nm_adamw_step")
+           "nm_adamw_plan_bytes", "nm_adamw_plan", "nm_adamw_step",
+           "nm_embedding_fwd", "nm_embedding_bwd_workspace_bytes", "nm_embedding_bwd",
+           "nm_head_norm_fwd", "nm_head_norm_bwd_workspace_bytes", "nm_head_norm_bwd", "nm_head_norm_cache",
+           "nm_paged_attn_workspace_bytes", "nm_paged_attn_fwd",
+           "nm_token_scores_workspace_bytes", "nm_token_scores_fwd", "nm_token_scores_bwd")
 
 _lib = None
 
@@ -141,6 +147,30 @@ def lib() -> ctypes.CDLL:
         L.nm_adamw_plan.restype = i
         L.nm_adamw_step.argtypes = [vp, vp, sz, d, d, d, d, ll, vp, u, vp]
         L.nm_adamw_step.restype = i
+        L.nm_embedding_fwd.argtypes = [i] * 4 + [vp, i, vp, f, vp, vp, i, vp]
+        L.nm_embedding_fwd.restype = i
+        L.nm_embedding_bwd_workspace_bytes.argtypes = [i] * 5
+        L.nm_embedding_bwd_workspace_bytes.restype = sz
+        L.nm_embedding_bwd.argtypes = [i] * 4 + [vp, vp, i, f, vp, vp, u, i, vp, sz, vp]
+        L.nm_embedding_bwd.restype = i
+        L.nm_head_norm_fwd.argtypes = [i] * 5 + [vp, ll, vp, vp, f, vp, i, vp, vp, vp, ll, u, i, vp]
+        L.nm_head_norm_fwd.restype = i
+        L.nm_head_norm_bwd_workspace_bytes.argtypes = [i] * 6
+        L.nm_head_norm_bwd_workspace_bytes.restype = sz
+        L.nm_head_norm_bwd.argtypes = [i] * 5 + [vp, ll, vp, ll, vp, vp, f, vp, i, vp, vp, vp, ll, vp, vp, u, i, vp, sz, vp]
+        L.nm_head_norm_bwd.restype = i
+        L.nm_head_norm_cache.argtypes = [i] * 5 + [vp, ll, vp, vp, f, vp, i, i, i, vp, i, vp, vp, vp, vp, vp, ll, u, i, vp]
+        L.nm_head_norm_cache.restype = i
+        L.nm_paged_attn_workspace_bytes.argtypes = [i] * 8
+        L.nm_paged_attn_workspace_bytes.restype = sz
+        L.nm_paged_attn_fwd.argtypes = [i] * 5 + [vp, ll, vp, vp, i, i, vp, i, vp, vp, i, f, vp, ll, vp, i, vp, sz, vp]
+        L.nm_paged_attn_fwd.restype = i
+        L.nm_token_scores_workspace_bytes.argtypes = [i] * 5
+        L.nm_token_scores_workspace_bytes.restype = sz
+        L.nm_token_scores_fwd.argtypes = [i] * 3 + [vp, vp, i, vp, i] + [vp] * 5 + [i, vp, sz, vp]
+        L.nm_token_scores_fwd.restype = i
+        L.nm_token_scores_bwd.argtypes = [i] * 3 + [vp, vp, i, vp] + [vp] * 5 + [i, i, vp]
+        L.nm_token_scores_bwd.restype = i
         _lib = L
     return _lib
 
@@ -879,3 +909,277 @@ def nm_adamw_step(plan: AdamWPlan, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, step
                              _ptr(grad_scale, _torch().float32, None, "grad_scale"), seed & 0xFFFFFFFF, _stream(stream))
     if st != NM_OK:
         raise NmError(st, "nm_adamw_step")
+
+
+# ---- what the operators on tokens share -----------------------------------------------------------
+def _on_current(t, name):
+    """Launches go to the current device: a tensor of another one is an error."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != _torch()._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _token_ptr(t, shape, name):
+    """(pointer, bytes of an element) of token numbers."""
+    torch = _torch()
+    if t.dtype == torch.int64:
+        return _ptr(t, None, shape, name), 8
+    return _ptr(t, torch.int32, shape, name), 4
+
+
+def _workspace_of(need, workspace, like, stream):
+    """(tensor to keep, pointer, bytes)"""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = like.new_empty(need, dtype=_torch().uint8)
+        if stream is not None:
+            workspace.record_stream(stream)  # (it is given back when the call returns)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+# ---- embeddings of tokens (include/nm_embedding.h) ------------------------------------------------
+def nm_embedding_fwd(ids, table, *, scale=1.0, lengths=None, out=None, stream=None):
+    """out [B, C, U]: scale * the rows of table [V, C] that ids [B, U] (int32 or int64) name; zeros for ids outside the table and behind
+    lengths (int32 [B])."""
+    torch = _torch()
+    _on_current(table, "table")
+    if ids.dim() != 2 or table.dim() != 2:
+        raise NmError(NM_ERR_BAD_ARG, "nm_embedding_fwd")
+    B, U = ids.shape
+    V, C = table.shape
+    code = _dtype_code(table)
+    ip, size = _token_ptr(ids, (B, U), "ids")
+    if out is None:
+        out = table.new_empty((B, C, U))
+    st = lib().nm_embedding_fwd(B, V, C, U, ip, size, _ptr(table, name="table"), scale, _ptr(lengths, torch.int32, (B,), "lengths"),
+                                _ptr(out, table.dtype, (B, C, U), "out"), code, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_embedding_fwd")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def nm_embedding_bwd_workspace_bytes(B, V, C, U, dtype=NM_BF16) -> int:
+    return int(lib().nm_embedding_bwd_workspace_bytes(B, V, C, U, dtype))
+
+
+def nm_embedding_bwd(dout, ids, vocab, *, scale=1.0, lengths=None, dtable=None, accumulate=False, workspace=None, stream=None):
+    """Gradient [vocab, C] float32 of the table from dout [B, C, U]; accumulate: added to dtable."""
+    torch = _torch()
+    _on_current(dout, "dout")
+    if dout.dim() != 3:
+        raise NmError(NM_ERR_BAD_ARG, "nm_embedding_bwd")
+    B, C, U = dout.shape
+    code = _dtype_code(dout)
+    ip, size = _token_ptr(ids, (B, U), "ids")
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs an existing dtable")
+        dtable = dout.new_empty((vocab, C), dtype=torch.float32)
+    ws, ws_ptr, ws_bytes = _workspace_of(nm_embedding_bwd_workspace_bytes(B, vocab, C, U, code), workspace, dout, stream)
+    st = lib().nm_embedding_bwd(B, vocab, C, U, _ptr(dout, name="dout"), ip, size, scale, _ptr(lengths, torch.int32, (B,), "lengths"),
+                                _ptr(dtable, torch.float32, (vocab, C), "dtable"), NM_ACCUM_DW if accumulate else 0, code, ws_ptr, ws_bytes,
+                                _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_embedding_bwd")
+    return dtable
+
+
+# ---- norms and rotation of queries and keys (include/nm_head_norm.h) -------------------------------
+def _head_args(x, heads, kv_heads, groups, norm, pairs, q_weight, k_weight, freqs, where):
+    """(D, flags, pointers of the weights, pointer of freqs, rot); groups: heads side by side in x."""
+    torch = _torch()
+    _on_current(x, "x")
+    if x.dim() != 3 or heads <= 0 or kv_heads < 0 or x.shape[1] % groups:
+        raise NmError(NM_ERR_BAD_ARG, where)
+    D = x.shape[1] // groups
+    rot = 0
+    if freqs is not None:
+        if freqs.dim() != 1:
+            raise ValueError("freqs must be a vector")
+        rot = 2 * freqs.shape[0]
+    return (D, (NM_HEADS_NORM if norm else 0) | (NM_HEADS_PAIRS if pairs else 0), _ptr(q_weight, torch.float32, (D,), "q_weight"),
+            _ptr(k_weight, torch.float32, (D,), "k_weight"), _ptr(freqs, torch.float64, None, "freqs") if rot else None, rot)
+
+
+def nm_head_norm_fwd(x, *, heads, kv_heads, norm=True, q_weight=None, k_weight=None, eps=1e-5, freqs=None, pairs=False, positions=None,
+                     lengths=None, out=None, stream=None):
+    """x [B, (heads + kv_heads)*D, U], queries and then keys, head by head over its rms (norm) times q_weight or k_weight [D], its first
+    2*len(freqs) channels turned by position*freqs (float64): in halves, or neighbours with pairs.  positions int32 [B, U] (None: 0, 1, ...);
+    lengths int32 [B]: zeros beyond."""
+    torch = _torch()
+    D, flags, qw, kw, fp, rot = _head_args(x, heads, kv_heads, heads + kv_heads, norm, pairs, q_weight, k_weight, freqs, "nm_head_norm_fwd")
+    B, C, U = x.shape
+    code = _dtype_code(x)
+    xp, xs = _item_ptr(x, x.dtype, (B, C, U), "x")
+    if out is None:
+        out = x.new_empty((B, C, U))
+    op, os_ = _item_ptr(out, x.dtype, (B, C, U), "out")
+    st = lib().nm_head_norm_fwd(B, heads, kv_heads, D, U, xp, xs, qw, kw, eps, fp, rot, _ptr(positions, torch.int32, (B, U), "positions"),
+                                _ptr(lengths, torch.int32, (B,), "lengths"), op, os_, flags, code, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_head_norm_fwd")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def nm_head_norm_bwd_workspace_bytes(B, heads, kv_heads, D, U, dtype=NM_BF16) -> int:
+    return int(lib().nm_head_norm_bwd_workspace_bytes(B, heads, kv_heads, D, U, dtype))
+
+
+def nm_head_norm_bwd(dout, x, *, heads, kv_heads, norm=True, q_weight=None, k_weight=None, eps=1e-5, freqs=None, pairs=False, positions=None,
+                     lengths=None, dx=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """Gradients (dx, dq_weight, dk_weight) of nm_head_norm_fwd from that of its output; the weights' float32, None without the weight."""
+    torch = _torch()
+    D, flags, qw, kw, fp, rot = _head_args(x, heads, kv_heads, heads + kv_heads, norm, pairs, q_weight, k_weight, freqs, "nm_head_norm_bwd")
+    B, C, U = x.shape
+    code = _dtype_code(x)
+    xp, xs = _item_ptr(x, x.dtype, (B, C, U), "x")
+    gp, gs = _item_ptr(dout, x.dtype, (B, C, U), "dout")
+    if dx is None:
+        dx = x.new_empty((B, C, U))
+    dp, ds = _item_ptr(dx, x.dtype, (B, C, U), "dx")
+    if q_weight is None:
+        dq_weight = None
+    elif dq_weight is None:
+        dq_weight = torch.empty_like(q_weight)
+    if k_weight is None:
+        dk_weight = None
+    elif dk_weight is None:
+        dk_weight = torch.empty_like(k_weight)
+    need = 0 if q_weight is None and k_weight is None else nm_head_norm_bwd_workspace_bytes(B, heads, kv_heads, D, U, code)
+    ws, ws_ptr, ws_bytes = _workspace_of(need, workspace, x, stream)
+    st = lib().nm_head_norm_bwd(B, heads, kv_heads, D, U, gp, gs, xp, xs, qw, kw, eps, fp, rot, _ptr(positions, torch.int32, (B, U), "positions"),
+                                _ptr(lengths, torch.int32, (B,), "lengths"), dp, ds, _ptr(dq_weight, torch.float32, (D,), "dq_weight"),
+                                _ptr(dk_weight, torch.float32, (D,), "dk_weight"), flags, code, ws_ptr, ws_bytes, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_head_norm_bwd")
+    return dx, dq_weight, dk_weight
+
+
+def _cache_ptrs(k_cache, v_cache, page_table, lengths, q_lengths, like, B, kv_heads, D, where):
+    """(pages, page_size, max_pages, pointers of k_cache, v_cache, page_table, lengths, q_lengths)"""
+    torch = _torch()
+    if k_cache.dim() != 4 or page_table.dim() != 2:
+        raise NmError(NM_ERR_BAD_ARG, where)
+    pages, page, most = k_cache.shape[0], k_cache.shape[2], page_table.shape[1]
+    return (pages, page, most, _ptr(k_cache, like.dtype, (pages, kv_heads, page, D), "k_cache"),
+            _ptr(v_cache, like.dtype, (pages, kv_heads, D, page), "v_cache"), _ptr(page_table, torch.int32, (B, most), "page_table"),
+            _ptr(lengths, torch.int32, (B,), "lengths"), _ptr(q_lengths, torch.int32, (B,), "q_lengths"))
+
+
+def nm_head_norm_cache(x, k_cache, v_cache, page_table, lengths, *, heads, kv_heads, q_lengths=None, norm=True, q_weight=None, k_weight=None,
+                       eps=1e-5, freqs=None, pairs=False, q=None, stream=None):
+    """x [B, (heads + 2*kv_heads)*D, U]: the queries [B, heads*D, U] come back normalised and turned, keys (so too) and values go to their places
+    in k_cache [pages, kv_heads, page_size, D] and v_cache [pages, kv_heads, D, page_size].  page_table int32 [B, max_pages]; lengths int32 [B]:
+    tokens of every sequence with the new ones, q_lengths (None: U) of which are new."""
+    D, flags, qw, kw, fp, rot = _head_args(x, heads, kv_heads, heads + 2 * kv_heads, norm, pairs, q_weight, k_weight, freqs, "nm_head_norm_cache")
+    B, C, U = x.shape
+    code = _dtype_code(x)
+    xp, xs = _item_ptr(x, x.dtype, (B, C, U), "x")
+    pages, page, most, kp, vp, tp, lp, nq = _cache_ptrs(k_cache, v_cache, page_table, lengths, q_lengths, x, B, kv_heads, D, "nm_head_norm_cache")
+    if q is None:
+        q = x.new_empty((B, heads * D, U))
+    qp, qs = _item_ptr(q, x.dtype, (B, heads * D, U), "q")
+    st = lib().nm_head_norm_cache(B, heads, kv_heads, D, U, xp, xs, qw, kw, eps, fp, rot, pages, page, tp, most, lp, nq, kp, vp, qp, qs, flags,
+                                  code, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_head_norm_cache")
+    return q
+
+
+# ---- attention over a paged cache (include/nm_paged_attention.h) -----------------------------------
+@functools.lru_cache(maxsize=1024)
+def nm_paged_attn_workspace_bytes(B, heads, kv_heads, D, U, page_size, max_pages, dtype=NM_BF16) -> int:
+    return int(lib().nm_paged_attn_workspace_bytes(B, heads, kv_heads, D, U, page_size, max_pages, dtype))
+
+
+def nm_paged_attn_fwd(q, k_cache, v_cache, page_table, lengths, *, heads, kv_heads, q_lengths=None, window=0, scale=None, o=None, lse=None,
+                      want_lse=False, workspace=None, stream=None):
+    """Attention of the new tokens q [B, heads*D, U] to what the cache holds of their sequences, themselves included (cache, table and lengths
+    as nm_head_norm_cache takes them); returns (o, lse), lse None unless given or wanted.  window: how many tokens a token looks
+    back on, itself included (0: all); scale: 1/sqrt(D) if None."""
+    torch = _torch()
+    _on_current(q, "q")
+    if q.dim() != 3 or heads <= 0 or kv_heads <= 0 or q.shape[1] % heads:
+        raise NmError(NM_ERR_BAD_ARG, "nm_paged_attn_fwd")
+    B, HD, U = q.shape
+    D = HD // heads
+    code = _dtype_code(q)
+    qp, qs = _item_ptr(q, q.dtype, (B, HD, U), "q")
+    pages, page, most, kp, vp, tp, lp, nq = _cache_ptrs(k_cache, v_cache, page_table, lengths, q_lengths, q, B, kv_heads, D, "nm_paged_attn_fwd")
+    if o is None:
+        o = q.new_empty((B, HD, U))
+    op, os_ = _item_ptr(o, q.dtype, (B, HD, U), "o")
+    if lse is None and want_lse:
+        lse = q.new_empty((B, heads, U), dtype=torch.float32)
+    ws, ws_ptr, ws_bytes = _workspace_of(nm_paged_attn_workspace_bytes(B, heads, kv_heads, D, U, page, most, code), workspace, q, stream)
+    st = lib().nm_paged_attn_fwd(B, heads, kv_heads, D, U, qp, qs, kp, vp, pages, page, tp, most, lp, nq, window, D ** -0.5 if scale is None else scale,
+                                 op, os_, _ptr(lse, torch.float32, (B, heads, U), "lse"), code, ws_ptr, ws_bytes, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_paged_attn_fwd")
+    return o, lse
+
+
+# ---- what scores say about tokens (include/nm_token_scores.h) --------------------------------------
+@functools.lru_cache(maxsize=1024)
+def nm_token_scores_workspace_bytes(B, V, U, top=0, dtype=NM_BF16) -> int:
+    return int(lib().nm_token_scores_workspace_bytes(B, V, U, top, dtype))
+
+
+def nm_token_scores_fwd(scores, targets=None, *, top=0, lengths=None, out=None, workspace=None, stream=None):
+    """A dict of float32 tensors from the scores [B, V, U]: "logp" [B, U], log-probabilities of the targets [B, U] (int32 or int64; only with
+    targets), "entropy" and "lse" [B, U], and with top "top_ids" (int32) and "top_logp" [B, top, U], the likeliest classes in order.
+    lengths int32 [B]: places behind them are zeros, ids -1.  out: a dict of tensors to write them to."""
+    torch = _torch()
+    _on_current(scores, "scores")
+    if scores.dim() != 3:
+        raise NmError(NM_ERR_BAD_ARG, "nm_token_scores_fwd")
+    B, V, U = scores.shape
+    code = _dtype_code(scores)
+    tp, size = (None, 0) if targets is None else _token_ptr(targets, (B, U), "targets")
+    given, got = out or {}, {}
+    f32 = torch.float32
+    for name in ("logp", "entropy", "lse") if targets is not None else ("entropy", "lse"):
+        t = given.get(name)
+        got[name] = scores.new_empty((B, U), dtype=f32) if t is None else t
+    if top > 0:
+        for name, dtype in (("top_ids", torch.int32), ("top_logp", f32)):
+            t = given.get(name)
+            got[name] = scores.new_empty((B, top, U), dtype=dtype) if t is None else t
+    ws, ws_ptr, ws_bytes = _workspace_of(nm_token_scores_workspace_bytes(B, V, U, top, code), workspace, scores, stream)
+    st = lib().nm_token_scores_fwd(
+        B, V, U, _ptr(scores, name="scores"), tp, size, _ptr(lengths, torch.int32, (B,), "lengths"), top,
+        _ptr(got.get("logp"), f32, (B, U), "logp"), _ptr(got["entropy"], f32, (B, U), "entropy"), _ptr(got["lse"], f32, (B, U), "lse"),
+        _ptr(got.get("top_ids"), torch.int32, (B, top, U), "top_ids"), _ptr(got.get("top_logp"), f32, (B, top, U), "top_logp"), code, ws_ptr,
+        ws_bytes, _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_token_scores_fwd")
+    return got
+
+
+def nm_token_scores_bwd(scores, targets, lse, entropy, dlogp, dentropy=None, *, lengths=None, dscores=None, dtype=None, stream=None):
+    """Gradient [B, V, U] with respect to the scores, in `dtype` (None: theirs), from dlogp (None: none, then no targets either) and dentropy
+    [B, U]; lse and entropy (needed with dentropy) as nm_token_scores_fwd gave them."""
+    torch = _torch()
+    _on_current(scores, "scores")
+    if scores.dim() != 3:
+        raise NmError(NM_ERR_BAD_ARG, "nm_token_scores_bwd")
+    B, V, U = scores.shape
+    code, f32, place = _dtype_code(scores), torch.float32, (B, U)
+    tp, size = (None, 0) if targets is None else _token_ptr(targets, place, "targets")
+    if dscores is None:
+        dscores = scores.new_empty((B, V, U), dtype=scores.dtype if dtype is None else dtype)
+    elif dtype is not None and dscores.dtype != dtype:
+        raise TypeError(f"dscores must have dtype {dtype}, got {dscores.dtype}")
+    st = lib().nm_token_scores_bwd(
+        B, V, U, _ptr(scores, name="scores"), tp, size, _ptr(lengths, torch.int32, (B,), "lengths"), _ptr(lse, f32, place, "lse"),
+        _ptr(entropy, f32, place, "entropy"), _ptr(dlogp, f32, place, "dlogp"), _ptr(dentropy, f32, place, "dentropy"),
+        _ptr(dscores, None, (B, V, U), "dscores"), code, _dtype_code(dscores), _stream(stream))
+    if st != NM_OK:
+        raise NmError(st, "nm_token_scores_bwd")
+    return dscores

@@ -1,0 +1,507 @@
+// Attention of new tokens over a paged cache (definition: include/nm_paged_attention.h).
+//
+// The cache is laid out for the matrix instructions: a key is a row of channels, so that its 16 bytes are operands of the scores as they lie in
+// memory; values are rows of tokens, so that theirs are operands of the second product.  Scores have places as rows and tokens as columns
+// (the new tokens of all heads that share keys and values), and the places are dealt to the rows such that a lane ends up with
+// those eight neighbouring places of its column that the second product wants from it: probabilities stay in the registers that they were
+// made in.  One pass with a running maximum and sum for each column.
+#include "../../include/nm_paged_attention.h"
+#include "token_ops.h"
+
+namespace nm {
+namespace {
+
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kLag = 8.f;      // powers of two that the base of the sums may lie below the maximum
+constexpr int kMaxSplits = 64;
+constexpr int kTile = 32;        // places that a wavefront looks at at a time
+constexpr int kWaves = 4;
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+struct Paged {
+    int B, H, Hkv, G, D, U;
+    const void *q, *k, *v;
+    long long qs, os;
+    int pages, log_page, max_pages;
+    const int *table, *len, *q_len;
+    int window;
+    float c;  // scale * log2(e)
+    void *out;
+    float *lse, *part, *part_ml;  // [splits][B*H*U][D], [splits][B*H*U][2]
+    int col_tiles, splits;
+};
+
+// Products of blocks of 16 x 16, a tile of 32 places being two of them: `Mma<S>::place(m, i)` is the place of row i of block m.
+template <typename S>
+struct Mma;
+template <>
+struct Mma<bf16_t> {
+    static constexpr int kChannels = 32;  // of a step of the scores
+    typedef bf16x8_t Frag;
+    // row i = 4*a + c of block m is place 8*a + 4*m + c: a lane's results of both blocks are eight neighbouring places
+    static __device__ __forceinline__ int place(int m, int i) { return 8 * (i >> 2) + 4 * m + (i & 3); }
+    static __device__ __forceinline__ int first_channel(int step, int quarter) { return 32 * step + 8 * quarter; }
+    static __device__ __forceinline__ f32x4_t mul(Frag a, Frag b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mma<float> {
+    static constexpr int kChannels = 16;
+    typedef f32x4_t Frag;  // four steps of four channels: step j takes element j of every quarter's
+    static __device__ __forceinline__ int place(int m, int i) { return 16 * m + i; }
+    static __device__ __forceinline__ int first_channel(int step, int quarter) { return 16 * step + 4 * quarter; }
+    static __device__ __forceinline__ f32x4_t mul(Frag a, Frag b, f32x4_t c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// The new tokens' places that a column may look at, [lo, hi)
+struct Column {
+    int g, u, lo, hi;
+    bool exists, there;
+};
+__device__ __forceinline__ Column column_of(const Paged &a, int b, int m, int n, int len)
+{
+    Column c;
+    c.exists = m < a.G * a.U;
+    c.u = c.exists ? m / a.G : 0;
+    c.g = m - c.u * a.G;
+    if (!c.exists) c.g = 0;
+    c.there = c.exists && c.u < n;
+    const int at = len - n + c.u;
+    c.hi = c.there ? max(0, min(at + 1, a.max_pages << a.log_page)) : 0;
+    c.lo = c.there && a.window ? max(0, at + 1 - a.window) : 0;
+    if (c.hi <= c.lo) c.there = false;
+    return c;
+}
+
+// NC blocks of 16 columns; DB blocks of 16 channels
+template <typename S, int DB, int NC>
+__global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
+{
+    typedef Mma<S> M;
+    typedef typename M::Frag Frag;
+    constexpr bool kBf16 = sizeof(S) == 2;
+    constexpr int KS = (DB * 16 + M::kChannels - 1) / M::kChannels;  // steps of the scores
+    constexpr int VB = kBf16 ? 1 : 2;                                // value operands of 16 channels and a tile
+    constexpr int kPer = 16 / sizeof(S);                             // elements of an operand's 16 bytes
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, i = lane & 15;
+    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int ct = rest % a.col_tiles, split = rest / a.col_tiles, b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const int n_new = length_in(a.q_len, b, a.U), len = max(a.len[b], 0);
+
+    Column col[NC];
+    int first = 0x7fffffff, last = 0;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        col[n] = column_of(a, b, (ct * NC + n) * 16 + i, n_new, len);
+        if (col[n].there) {
+            first = min(first, col[n].lo);
+            last = max(last, col[n].hi);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        first = min(first, __shfl_xor(first, d));
+        last = max(last, __shfl_xor(last, d));
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    const int t_first = last ? first / kTile : 0, t_last = (last + kTile - 1) / kTile, share = (t_last - t_first + a.splits - 1) / a.splits;
+    const int t_begin = t_first + split * share, t_end = min(t_last, t_begin + share);
+
+    // the tokens' channels
+    Frag q[NC][KS];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        const S *p = (const S *)a.q + (size_t)b * a.qs + (size_t)(kvh * a.G + col[n].g) * a.D * a.U + col[n].u;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            S e[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int d = M::first_channel(s, quarter) + j;
+                e[j] = p[(size_t)min(d, a.D - 1) * a.U];
+                if (!col[n].there || d >= a.D) e[j] = S(0);
+            }
+            __builtin_memcpy(&q[n][s], e, 16);
+        }
+    }
+
+    // a tile's operands; a page that does not exist is read as page 0, and masked
+    const int size = 1 << a.log_page;
+    auto page_of = [&](int t, int part) {
+        const int at = min((t * kTile + 16 * part) >> a.log_page, a.max_pages - 1);
+        return a.table[(size_t)b * a.max_pages + at];
+    };
+    Frag kf[2][KS], vf[DB][VB];
+    auto load_k = [&](int t, int pg0, int pg1) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int place = M::place(m, i), pg = place < 16 ? pg0 : pg1, row = (t * kTile + place) & (size - 1);
+            const S *p = (const S *)a.k + (((size_t)pg * a.Hkv + kvh) * size + row) * a.D;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int d = M::first_channel(s, quarter);
+                kf[m][s] = *reinterpret_cast<const Frag *>(p + min(d, a.D - kPer));
+                if (DB * 16 % M::kChannels && s == KS - 1 && d >= a.D) kf[m][s] = Frag{};
+            }
+        }
+    };
+    auto load_v = [&](int t, int pg0, int pg1) {
+#pragma unroll
+        for (int h = 0; h < VB; ++h) {
+            const int place = kBf16 ? 8 * quarter : 16 * h + 4 * quarter, pg = place < 16 ? pg0 : pg1, row = (t * kTile + place) & (size - 1);
+            const S *p = (const S *)a.v + (((size_t)pg * a.Hkv + kvh) * a.D + i) * size + row;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) vf[d][h] = *reinterpret_cast<const Frag *>(p + (size_t)d * 16 * size);
+        }
+    };
+
+    float mx[NC], sum[NC];
+    f32x4_t acc[NC][DB];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        mx[n] = -INFINITY;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    auto there = [&](int pg) { return (unsigned)pg < (unsigned)a.pages; };
+    auto usable = [&](int pg) { return there(pg) ? pg : 0; };
+
+    int t = t_begin + wave, pg0 = 0, pg1 = 0, next0 = 0, next1 = 0;
+    if (t < t_end) {
+        pg0 = page_of(t, 0);
+        pg1 = page_of(t, 1);
+        load_k(t, usable(pg0), usable(pg1));
+        load_v(t, usable(pg0), usable(pg1));
+        next0 = page_of(t + kWaves, 0);
+        next1 = page_of(t + kWaves, 1);
+    }
+    for (; t < t_end; t += kWaves) {
+        const int t0 = t * kTile;
+        f32x4_t s[NC][2];
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                s[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < KS; ++st) s[n][m] = M::mul(kf[m][st], q[n][st], s[n][m]);
+            }
+        const bool more = t + kWaves < t_end;
+        if (more) load_k(t + kWaves, usable(next0), usable(next1));
+        const bool whole = there(pg0) && there(pg1);
+        bool inside = whole;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) inside = inside && (!col[n].there || (col[n].lo <= t0 && t0 + kTile <= col[n].hi));
+        const bool edge = !__all(inside);
+        Frag p[NC][2];  // bfloat16: the probabilities and what their rounding leaves; float: of the two blocks
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            // (as plain floats: elements of a matrix result that are changed under a branch come out wrong from this compiler)
+            float z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = s[n][j >> 2][j & 3] * a.c;
+            if (edge) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int place = M::place(j >> 2, 4 * quarter + (j & 3)), pos = t0 + place;
+                    const bool seen = (pos >= col[n].lo) & (pos < col[n].hi) & there(place < 16 ? pg0 : pg1);
+                    z[j] = seen ? z[j] : -INFINITY;
+                }
+            }
+            float top = z[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) top = fmaxf(top, z[j]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any(top > mx[n] + kLag)) {
+                top = fmaxf(top, mx[n]);
+                const float shrink = __builtin_amdgcn_exp2f(mx[n] - (top == -INFINITY ? 0.f : top));
+                sum[n] *= shrink;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[n][d] *= shrink;
+                mx[n] = top;
+            }
+            const float base = mx[n] == -INFINITY ? 0.f : mx[n];
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(z[j] - base);
+                sum[n] += e[j];
+            }
+            if constexpr (kBf16) {
+                u32x4_t hi, lo;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    hi[j] = pack_bf16x2(e[2 * j], e[2 * j + 1]);
+                    lo[j] = pack_bf16x2(e[2 * j] - __uint_as_float(hi[j] << 16), e[2 * j + 1] - __uint_as_float(hi[j] & 0xffff0000u));
+                }
+                p[n][0] = __builtin_bit_cast(Frag, hi);
+                p[n][1] = __builtin_bit_cast(Frag, lo);
+            } else {
+                __builtin_memcpy(&p[n][0], e, 16);
+                __builtin_memcpy(&p[n][1], e + 4, 16);
+            }
+        }
+        if (t0 < first || t0 + kTile > last || !whole) {  // (uniform) values that no token looks at may hold anything
+#pragma unroll
+            for (int h = 0; h < VB; ++h) {
+                const int place = kBf16 ? 8 * quarter : 16 * h + 4 * quarter, from = first - t0 - place, to = last - t0 - place;
+                const bool exists = there(place < 16 ? pg0 : pg1);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    S e[kPer];
+                    __builtin_memcpy(e, &vf[d][h], 16);
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (!exists || j < from || j >= to) e[j] = S(0);
+                    __builtin_memcpy(&vf[d][h], e, 16);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                if constexpr (kBf16) {
+                    acc[n][d] = M::mul(vf[d][0], p[n][1], acc[n][d]);
+                    acc[n][d] = M::mul(vf[d][0], p[n][0], acc[n][d]);
+                } else {
+                    acc[n][d] = M::mul(vf[d][0], p[n][0], acc[n][d]);
+                    acc[n][d] = M::mul(vf[d][VB - 1], p[n][1], acc[n][d]);
+                }
+            }
+        if (more) {
+            load_v(t + kWaves, usable(next0), usable(next1));
+            pg0 = next0;
+            pg1 = next1;
+            next0 = page_of(t + 2 * kWaves, 0);
+            next1 = page_of(t + 2 * kWaves, 1);
+        }
+    }
+
+    // the wavefronts' maxima, sums and products are joined through LDS
+    float *sums = reinterpret_cast<float *>(smem);          // [kWaves][NC][2][16]
+    float *prod = sums + kWaves * NC * 32;                  // [kWaves][NC][DB][64][4]
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        float all = sum[n];
+        all += __shfl_xor(all, 16);
+        all += __shfl_xor(all, 32);
+        if (quarter == 0) {
+            sums[(wave * NC + n) * 32 + i] = mx[n];
+            sums[(wave * NC + n) * 32 + 16 + i] = all;
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4_t *>(prod + (((wave * NC + n) * DB + d) * 64 + lane) * 4) = acc[n][d];
+    }
+    __syncthreads();
+    const size_t rows = (size_t)a.B * a.H * a.U;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        float top = -INFINITY, total = 0.f, weight[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sums[(w * NC + n) * 32 + i]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            weight[w] = __builtin_amdgcn_exp2f(sums[(w * NC + n) * 32 + i] - (top == -INFINITY ? 0.f : top));
+            total += weight[w] * sums[(w * NC + n) * 32 + 16 + i];
+        }
+        if (!col[n].exists) continue;
+        const int head = kvh * a.G + col[n].g;
+        const size_t row = ((size_t)b * a.H + head) * a.U + col[n].u;
+        const bool some = col[n].there && total != 0.f;
+        if (wave == 0 && quarter == 0) {
+            if (a.splits > 1) {
+                float *ml = a.part_ml + ((size_t)split * rows + row) * 2;
+                ml[0] = some ? top : -INFINITY;
+                ml[1] = some ? total : 0.f;
+            } else if (a.lse) {
+                a.lse[row] = some ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+            }
+        }
+        const float inv = some ? (a.splits > 1 ? 1.f : 1.f / total) : 0.f;
+        for (int d = wave; d < DB; d += kWaves) {
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += weight[w] * *reinterpret_cast<const f32x4_t *>(prod + (((w * NC + n) * DB + d) * 64 + lane) * 4);
+            const int ch = 16 * d + 4 * quarter;
+            if (!some) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (a.splits > 1) {
+                *reinterpret_cast<f32x4_t *>(a.part + ((size_t)split * rows + row) * a.D + ch) = v;
+            } else {
+                S *o = (S *)a.out + (size_t)b * a.os + ((size_t)head * a.D + ch) * a.U + col[n].u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) store_from_f32(o, (size_t)r * a.U, v[r] * inv);
+            }
+        }
+    }
+}
+
+// Joins the sums of `splits` workgroups in order: 16 rows (tokens of heads) a workgroup, a thread eight channels of one
+template <typename S>
+__global__ __launch_bounds__(256) void paged_join_kernel(Paged a)
+{
+    __shared__ float tile[16][128 + 1];
+    const size_t rows = (size_t)a.B * a.H * a.U;
+    const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
+    const size_t row0 = (size_t)blockIdx.x * 16, row = min(row0 + r, rows - 1);
+    float top = -INFINITY, total = 0.f;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[((size_t)s * rows + row) * 2]);
+    const float base = top == -INFINITY ? 0.f : top;
+    const int d0 = part * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + ((size_t)s * rows + row) * 2);
+        const float w = __builtin_amdgcn_exp2f(ml.x - base);
+        total += w * ml.y;
+        if (d0 < a.D) {
+            float p[8];
+            load8(a.part + ((size_t)s * rows + row) * a.D + d0, 8, p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w * p[j];
+        }
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    if (a.lse && part == 0 && row0 + r < rows) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[r][d0 + j] = v[j] * inv;
+    __syncthreads();
+    // neighbouring lanes store neighbouring tokens, or channels where there is one token
+    for (int e = threadIdx.x; e < 16 * a.D; e += 256) {
+        const int er = a.U >= 8 ? e & 15 : e / a.D, d = a.U >= 8 ? e >> 4 : e - er * a.D;
+        const size_t to = row0 + er;
+        if (to >= rows) continue;
+        const size_t bh = to / a.U, u = to - bh * a.U, b = bh / a.H, h = bh - b * a.H;
+        store_from_f32((S *)a.out, b * a.os + (h * a.D + d) * a.U + u, tile[er][d]);
+    }
+}
+
+struct Plan {
+    int blocks, col_tiles, splits;  // blocks: of 16 columns of a workgroup
+    size_t part_bytes, ml_bytes;
+};
+Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, int)
+{
+    Plan p = {};
+    const long long columns = (long long)(H / Hkv) * U;
+    p.blocks = columns > 16 ? 2 : 1;
+    p.col_tiles = (int)((columns + 16 * p.blocks - 1) / (16 * p.blocks));
+    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = ((long long)max_pages * page_size + kTile * kWaves - 1) / (kTile * kWaves);
+    long long splits = (1024 + groups - 1) / groups;
+    if (splits > rounds / 2) splits = rounds / 2;
+    if (splits > kMaxSplits) splits = kMaxSplits;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    const size_t rows = (size_t)B * H * U;
+    p.part_bytes = p.splits > 1 ? align_up(p.splits * rows * D * 4, 256) : 0;
+    p.ml_bytes = p.splits > 1 ? align_up(p.splits * rows * 2 * 4, 256) : 0;
+    return p;
+}
+
+template <typename S, int DB, int NC>
+hipError_t run_few(const Paged &a, hipStream_t s)
+{
+    static LdsOptIn opt;
+    constexpr int bytes = kWaves * NC * (32 + DB * 256) * 4;
+    auto *fn = paged_few_kernel<S, DB, NC>;
+    const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, bytes);
+    if (e != hipSuccess) return e;
+    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.col_tiles * a.splits), dim3(kWaves * 64), bytes, s>>>(a);
+    return hipGetLastError();
+}
+template <typename S, int DB>
+hipError_t run_blocks(const Paged &a, int blocks, hipStream_t s)
+{
+    return blocks == 1 ? run_few<S, DB, 1>(a, s) : run_few<S, DB, 2>(a, s);
+}
+template <typename S>
+hipError_t run(const Paged &a, int blocks, hipStream_t s)
+{
+    hipError_t e;
+    switch (a.D / 16) {
+    case 1: e = run_blocks<S, 1>(a, blocks, s); break;
+    case 2: e = run_blocks<S, 2>(a, blocks, s); break;
+    case 3: e = run_blocks<S, 3>(a, blocks, s); break;
+    case 4: e = run_blocks<S, 4>(a, blocks, s); break;
+    case 5: e = run_blocks<S, 5>(a, blocks, s); break;
+    case 6: e = run_blocks<S, 6>(a, blocks, s); break;
+    case 7: e = run_blocks<S, 7>(a, blocks, s); break;
+    default: e = run_blocks<S, 8>(a, blocks, s); break;
+    }
+    if (e != hipSuccess || a.splits == 1) return e;
+    const size_t rows = (size_t)a.B * a.H * a.U;
+    paged_join_kernel<S><<<dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+int check(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, int dtype)
+{
+    if (B <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || U <= 0 || page_size <= 0 || max_pages <= 0 || H % Hkv || !known_dtype(dtype)) return NM_ERR_BAD_ARG;
+    const long long most = (1LL << 31) - 1;
+    if (D % 16 || D > 128 || page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return NM_ERR_UNSUPPORTED;
+    if ((long long)max_pages * page_size > most - 512 || (long long)B * max_pages > most) return NM_ERR_UNSUPPORTED;
+    if ((long long)H * D > most / U || (long long)B * H > most / 2 / U) return NM_ERR_UNSUPPORTED;
+    // the grid, of 256 work items for 16 or 32 columns and a split: below 2^32 (from 2^10 workgroups on nothing is split)
+    if ((long long)B * Hkv >= 1LL << 23 || (long long)B * Hkv * (((long long)H / Hkv * U + 15) / 16) >= 1LL << 23) return NM_ERR_UNSUPPORTED;
+    return NM_OK;
+}
+
+}  // namespace
+}  // namespace nm
+
+using namespace nm;
+
+extern "C" {
+
+size_t nm_paged_attn_workspace_bytes(int B, int heads, int kv_heads, int D, int U, int page_size, int max_pages, int dtype)
+{
+    if (check(B, heads, kv_heads, D, U, page_size, max_pages, dtype) != NM_OK) return 0;
+    const Plan p = plan_of(B, heads, kv_heads, D, U, page_size, max_pages, dtype);
+    return p.part_bytes + p.ml_bytes;
+}
+
+int nm_paged_attn_fwd(int B, int heads, int kv_heads, int D, int U, const void *q, long long q_stride, const void *k_cache,
+                      const void *v_cache, int pages, int page_size, const int *page_table, int max_pages, const int *lengths,
+                      const int *q_lengths, int window, float scale, void *o, long long o_stride, float *lse, int dtype, void *workspace,
+                      size_t workspace_bytes, void *hip_stream)
+{
+    const int st = check(B, heads, kv_heads, D, U, page_size, max_pages, dtype);
+    if (st != NM_OK) return st;
+    const long long item = (long long)heads * D * U;
+    if (!q || !k_cache || !v_cache || !page_table || !lengths || !o || pages <= 0 || window < 0 || !finite_float(scale) || !stride_ok(q_stride, item) ||
+        !stride_ok(o_stride, item) || (uintptr_t)k_cache % 16 || (uintptr_t)v_cache % 16)
+        return NM_ERR_BAD_ARG;
+    const int size = (int)element(dtype);
+    if ((long long)pages * kv_heads > (1LL << 40) / (page_size * D)) return NM_ERR_UNSUPPORTED;
+    const size_t cache = (size_t)pages * kv_heads * page_size * D * size;
+    const Items to = {o, o_stride, item, B, size}, from = {q, q_stride, item, B, size};
+    const Region l = {lse, (size_t)B * heads * U * 4};
+    const Region in[5] = {{k_cache, cache}, {v_cache, cache}, {page_table, (size_t)B * max_pages * 4}, {lengths, (size_t)B * 4}, {q_lengths, (size_t)B * 4}};
+    if (meet(to, from) || meets(to.region(), in) || meets(l, in) || meet(l, from.region()) || meet(l, to.region())) return NM_ERR_BAD_ARG;
+    const Plan p = plan_of(B, heads, kv_heads, D, U, page_size, max_pages, dtype);
+    if (workspace_missing(workspace, workspace_bytes, p.part_bytes + p.ml_bytes)) return NM_ERR_WORKSPACE;
+    Paged a = {};
+    a.B = B; a.H = heads; a.Hkv = kv_heads; a.G = heads / kv_heads; a.D = D; a.U = U;
+    a.q = q; a.k = k_cache; a.v = v_cache; a.qs = q_stride; a.os = o_stride;
+    a.pages = pages; a.max_pages = max_pages;
+    while (1 << a.log_page < page_size) ++a.log_page;
+    a.table = page_table; a.len = lengths; a.q_len = q_lengths;
+    a.window = window;
+    a.c = scale * 1.4426950408889634f;
+    a.out = o; a.lse = lse;
+    a.part = (float *)workspace;
+    a.part_ml = (float *)((char *)workspace + p.part_bytes);
+    a.col_tiles = p.col_tiles; a.splits = p.splits;
+    hipStream_t s = (hipStream_t)hip_stream;
+    return status_of(dtype == NM_BF16 ? run<bf16_t>(a, p.blocks, s) : run<float>(a, p.blocks, s));
+}
+
+}  // extern "C"

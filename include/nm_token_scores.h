@@ -22,7 +22,7 @@
  *    scores are not read at u >= lengths[b], whatever they hold.
  *  - top is at most 16 and at most V.
  *  - workspace: nm_token_scores_workspace_bytes bytes, 256-byte aligned (NULL where that is 0).
- *  - B * V * U must be below 2^31, V at most 2^31 - 2^16 - 1.
+ *  - B * V * U must be below 2^31, V at most 2^31 - 2^16 - 1, U at most 2^29.
  */
 #ifndef NM_TOKEN_SCORES_H
 #define NM_TOKEN_SCORES_H

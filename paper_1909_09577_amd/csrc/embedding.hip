@@ -6,10 +6,9 @@
 // Gradient: a sum over the places of each token, which has to come out the same every time, so the places are sorted by token, without
 // atomics on sums.  Three launches:
 //   order  one workgroup for each range of tokens reads all token numbers, counts those of its range and of the ranges below,
-//          and writes its places in order behind them (counts of a thread's own stretch of the places, summed over the threads, are where the
-//          thread writes: a stable counting sort).  Beside them other workgroups turn dout into rows of channels and fill dtable
-//          with zeros.
-//   sums   a wavefront adds a run of 32 sorted places, a lane eight channels of them; a token whose places lie in one run is finished there.
+//          packs the places of its range into a list in their order, and writes each to where its token's next one goes: a stable counting
+//          sort.  Beside them other workgroups turn dout into rows of channels and fill dtable with zeros.
+//   sums   a wavefront adds a run of eight sorted places, a lane eight channels of them; a token whose places lie in one run is finished there.
 //          A frequent token's runs leave parts.
 //   join   adds the parts of such a token in order.
 #include "../../include/nm_embedding.h"
@@ -100,11 +99,17 @@ hipError_t run_fwd(EmbedFwd a, hipStream_t s)
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
-constexpr int kRange = 32;    // tokens of a sorting workgroup at most
-constexpr int kChunk = 8192;  // places that it looks at at a time
-constexpr int kMine = kChunk / 256;  // of a thread
-constexpr int kRun = 32;      // sorted places of a wavefront
-constexpr int kFill = 16384;  // floats that a workgroup fills
+constexpr int kThreads = 512, kWaves = kThreads / 64;  // of the workgroups that sort, turn and fill
+constexpr int kMine = 16;                              // places of a thread that sorts
+constexpr int kChunk = kThreads * kMine;               // places that a sorting workgroup looks at at a time
+constexpr int kRange = 1024;                           // tokens of a sorting workgroup at most
+constexpr int kRun = 8;                                // sorted places of a wavefront
+constexpr int kFill = 32768;                           // floats that a workgroup fills
+
+// A sorted place: where it is, its token, and where the token's places begin and end in the order.
+struct __align__(16) Entry {
+    int place, token, from, to;
+};
 
 struct EmbedBwd {
     int B, V, C, U, N;
@@ -115,22 +120,11 @@ struct EmbedBwd {
     float scale;
     float *dtable;
     bool add;
-    int *order, *token, *starts;  // places sorted by token [N], their tokens [N], where a token's begin [V+1]
-    float *parts;                 // [runs][2][C]: sums of a run's first and last token
+    Entry *order;             // [N]
+    int *total;               // places that have a token
+    float *parts;             // [runs][2][C]: sums of a run's first and last token
     int range, sorters, u_tiles, c_tiles, turners;
 };
-
-// the token at place p, -1 where there is none
-__device__ __forceinline__ int token_at(const EmbedBwd &a, int p)
-{
-    if (p >= a.N) return -1;
-    int id = a.ids.at(p, a.V);
-    if (a.len) {
-        const int b = p / a.U;
-        if (p - b * a.U >= a.len[b]) id = -1;
-    }
-    return id;
-}
 
 __device__ __forceinline__ int wave_scan(int v, int lane)  // sum of the lanes up to this one
 {
@@ -142,128 +136,177 @@ __device__ __forceinline__ int wave_scan(int v, int lane)  // sum of the lanes u
     return v;
 }
 
-__device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
+// The tokens of kMine places from p0 on, -1 where there is none
+__device__ __forceinline__ void tokens_at(const EmbedBwd &a, int p0, int (&id)[kMine])
 {
-    uint8_t *local = smem;                                                // [kChunk]: token in the range, or 255
-    uint16_t *count = reinterpret_cast<uint16_t *>(smem + kChunk);        // [range][256]
-    int *cursor = reinterpret_cast<int *>(smem + kChunk + kRange * 512);  // [kRange]: where a token's next place goes
-    int *found = cursor + kRange;                                         // [kRange]: places of a token in the chunk
-    int *below = found + kRange;                                          // [4]
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int v0 = blockIdx.x * a.range, bins = min(a.range, a.V - v0);
-    if (t < kRange) cursor[t] = 0;
-    __syncthreads();
-    int less = 0;
-    const int chunks = (a.N + kChunk - 1) / kChunk;
-    auto stage = [&](int p0, bool counting) {
-#pragma unroll 8
-        for (int i = 0; i < kMine; ++i) {
-            const int id = token_at(a, p0 + i * 256 + t), r = id - v0;
-            const bool mine = id >= 0 && r >= 0 && r < bins;
-            local[i * 256 + t] = mine ? (uint8_t)r : (uint8_t)255;
-            if (counting) {
-                less += id >= 0 && r < 0;
-                if (mine) atomicAdd(&cursor[r], 1);  // (whole numbers: any order gives the same)
-            }
-        }
-    };
-    for (int k = 0; k < chunks; ++k) stage(k * kChunk, true);
+    if (p0 + kMine <= a.N) {
+        if (a.ids.wide) {
+            long long w[kMine];
+            __builtin_memcpy(w, reinterpret_cast<const long long *>(a.ids.p) + p0, sizeof(w));
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) less += __shfl_xor(less, d);
-    if (lane == 0) below[wave] = less;
-    __syncthreads();
-    if (wave == 0) {
-        const int n = lane < bins ? cursor[lane] : 0, base = below[0] + below[1] + below[2] + below[3];
-        const int upto = wave_scan(n, lane);
-        if (lane < bins) {
-            cursor[lane] = base + upto - n;
-            a.starts[v0 + lane] = base + upto - n;
-            if (v0 + lane == a.V - 1) a.starts[a.V] = base + upto;
+            for (int i = 0; i < kMine; ++i) id[i] = w[i] < 0 || w[i] >= a.V ? -1 : (int)w[i];
+        } else {
+            __builtin_memcpy(id, reinterpret_cast<const int *>(a.ids.p) + p0, sizeof(id));
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) id[i] = id[i] < 0 || id[i] >= a.V ? -1 : id[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) id[i] = p0 + i < a.N ? a.ids.at(p0 + i, a.V) : -1;
+    }
+    if (a.len && p0 < a.N) {
+        int b = p0 / a.U, u = p0 - b * a.U, len = a.len[b];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (u >= len) id[i] = -1;
+            if (++u == a.U) {
+                u = 0;
+                b = min(b + 1, a.B - 1);
+                len = a.len[b];
+            }
         }
     }
+}
+
+// One range of tokens: which places have them, in order of the tokens and of the places.  A thread has kMine neighbouring places of a chunk;
+// those of the range are packed into a list in their order, and each wavefront picks its tokens' out of it.
+__device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
+{
+    uint32_t *list = reinterpret_cast<uint32_t *>(smem);           // [kChunk]: token in the range, place in the chunk
+    int *count = reinterpret_cast<int *>(smem + kChunk * 4);       // [kRange]
+    int *begin = count + kRange;                                   // [kRange]
+    int *next = begin + kRange;                                    // [kRange]: where the next place goes
+    int *sums = next + kRange;                                     // [2][kWaves]
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int v0 = blockIdx.x * a.range, bins = min(a.range, a.V - v0);
+    for (int r = t; r < bins; r += kThreads) count[r] = 0;
     __syncthreads();
+    int less = 0, id[kMine];
+    const int chunks = (a.N + kChunk - 1) / kChunk;
     for (int k = 0; k < chunks; ++k) {
-        if (chunks > 1) stage(k * kChunk, false);
-        for (int r = 0; r < bins; ++r) count[r * 256 + t] = 0;
-        __syncthreads();
-        u32x4_t w[kMine / 16];
-        bool any = false;
+        tokens_at(a, k * kChunk + t * kMine, id);
 #pragma unroll
-        for (int i = 0; i < kMine / 16; ++i) {
-            w[i] = *reinterpret_cast<const u32x4_t *>(local + t * kMine + 16 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) any |= w[i][j] != 0xffffffffu;
+        for (int i = 0; i < kMine; ++i) {
+            const int r = id[i] - v0;
+            less += id[i] >= 0 && r < 0;
+            if (r >= 0 && r < bins && id[i] >= 0) atomicAdd(&count[r], 1);  // (whole numbers: any order gives the same)
         }
-        if (any) {
+    }
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const int r = (w[i / 16][i / 4 % 4] >> (8 * (i % 4))) & 255;
-                if (r != 255) ++count[r * 256 + t];
-            }
+    for (int d = 1; d < 64; d <<= 1) less += __shfl_xor(less, d);
+    if (lane == 0) sums[wave] = less;
+    __syncthreads();
+    if (wave == 0) {  // where every token's places begin
+        int base = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) base += sums[w];
+        for (int r0 = 0; r0 < bins; r0 += 64) {
+            const int n = r0 + lane < bins ? count[r0 + lane] : 0, upto = wave_scan(n, lane);
+            if (r0 + lane < bins) begin[r0 + lane] = next[r0 + lane] = base + upto - n;
+            base += __shfl(upto, 63);
+        }
+        if (lane == 0 && v0 + bins == a.V) *a.total = base;
+    }
+    for (int k = 0; k < chunks; ++k) {
+        if (chunks > 1) tokens_at(a, k * kChunk + t * kMine, id);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) n += id[i] >= v0 && id[i] < v0 + bins;
+        const int upto = wave_scan(n, lane);
+        if (lane == 63) sums[kWaves + wave] = upto;
+        __syncthreads();  // (and `begin` is there; the list's last readers are through)
+        int at = upto - n, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) at += sums[kWaves + w];
+            all += sums[kWaves + w];
+        }
+        if (n) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i)
+                if (id[i] >= v0 && id[i] < v0 + bins) list[at++] = (uint32_t)(id[i] - v0) << 16 | (uint32_t)(t * kMine + i);
         }
         __syncthreads();
-        for (int r = wave; r < bins; r += 4) {  // counts become what lies before a thread's own
-            uint16_t *c = count + r * 256 + lane * 4;
-            const int n0 = c[0], n1 = c[1], n2 = c[2], n3 = c[3], sum = n0 + n1 + n2 + n3;
-            const int upto = wave_scan(sum, lane), from = upto - sum;
-            c[0] = (uint16_t)from;
-            c[1] = (uint16_t)(from + n0);
-            c[2] = (uint16_t)(from + n0 + n1);
-            c[3] = (uint16_t)(from + n0 + n1 + n2);
-            if (lane == 63) found[r] = upto;
-        }
-        __syncthreads();
-        if (any) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const int r = (w[i / 16][i / 4 % 4] >> (8 * (i % 4))) & 255;
-                if (r != 255) {
-                    const int at = cursor[r] + count[r * 256 + t]++;
-                    a.order[at] = k * kChunk + t * kMine + i;
-                    a.token[at] = v0 + r;
+        // A wavefront's tokens are every kWaves-th.  Of 64 listed places it finds those of one of its tokens at a time.
+        for (int j = 0; j < all; j += 64) {
+            const uint32_t e = j + lane < all ? list[j + lane] : 0xffffffffu;
+            const int r = (int)(e >> 16);
+            uint64_t open = __ballot(j + lane < all && r % kWaves == wave);
+            while (open) {
+                const int token = __builtin_amdgcn_readlane(r, __builtin_ctzll(open));
+                const uint64_t same = __ballot(j + lane < all && r == token);
+                const int from = begin[token], at = next[token];
+                if ((same >> lane) & 1) {
+                    const int before = __builtin_popcountll(same & ((1ull << lane) - 1));
+                    a.order[at + before] = Entry{k * kChunk + (int)(e & 0xffff), v0 + token, from, from + count[token]};
                 }
+                if (lane == 0) next[token] = at + __builtin_popcountll(same);  // (this wavefront's alone)
+                open &= ~same;
             }
         }
-        __syncthreads();
-        if (t < bins) cursor[t] += found[t];
         __syncthreads();
     }
 }
 
-// 64 tokens x 64 channels of dout as rows of channels
+// 64 tokens x `kChannels` channels of dout as rows of channels
+template <typename S>
+struct Turn {
+    static constexpr int kChannels = sizeof(S) == 2 ? 128 : 64, kPitch = sizeof(S) == 2 ? 66 : 65, kSteps = kChannels * 8 / kThreads;
+    static constexpr int kBytes = kChannels * kPitch * sizeof(S);
+};
+__device__ __forceinline__ void load8_bits(const bf16_t *p, int n, bf16_t (&e)[8])
+{
+    const u32x4_t v = load8_any(p, n);
+    __builtin_memcpy(e, &v, 16);
+}
+__device__ __forceinline__ void load8_bits(const float *p, int n, float (&e)[8]) { load8(p, n, e); }
+__device__ __forceinline__ void store8_bits(bf16_t *p, int n, const bf16_t (&e)[8])
+{
+    u32x4_t v;
+    __builtin_memcpy(&v, e, 16);
+    store8_any(p, v, n);
+}
+__device__ __forceinline__ void store8_bits(float *p, int n, const float (&e)[8]) { store8(p, n, e); }
+
 template <typename S>
 __device__ void turn_tile(const EmbedBwd &a, int tile, unsigned char *smem)
 {
-    constexpr int kPitch = 64 + (sizeof(S) == 2 ? 2 : 1);
-    S *lds = reinterpret_cast<S *>(smem);  // [64 channels][kPitch]
+    typedef Turn<S> T;
+    S *lds = reinterpret_cast<S *>(smem);  // [kChannels][kPitch]
     const int t = threadIdx.x, ct = tile % a.c_tiles, rest = tile / a.c_tiles;
-    const int b = rest / a.u_tiles, u0 = (rest - b * a.u_tiles) * 64, c0 = ct * 64;
+    const int b = rest / a.u_tiles, u0 = (rest - b * a.u_tiles) * 64, c0 = ct * T::kChannels;
     const int len = length_in(a.len, b, a.U);
     if (u0 >= len) return;
+    S e[T::kSteps][8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = (t >> 3) + 32 * i, u = (t & 7) * 8;
-        float v[8];
-        load8((const S *)a.dout + ((size_t)b * a.C + min(c0 + c, a.C - 1)) * a.U + u0 + u, len - u0 - u, v);
+    for (int i = 0; i < T::kSteps; ++i) {
+        const int c = (t >> 3) + kThreads / 8 * i, u = (t & 7) * 8;
+        load8_bits((const S *)a.dout + ((size_t)b * a.C + min(c0 + c, a.C - 1)) * a.U + u0 + u, len - u0 - u, e[i]);
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) store_from_f32(lds + c * kPitch + u, j, v[j]);
+    for (int i = 0; i < T::kSteps; ++i) {
+        const int c = (t >> 3) + kThreads / 8 * i, u = (t & 7) * 8;
+        __builtin_memcpy(__builtin_assume_aligned(lds + c * T::kPitch + u, 4), e[i], sizeof(e[i]));
     }
     __syncthreads();
+    constexpr int kGroups = T::kChannels / 8;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int u = (t >> 3) + 32 * i, c = (t & 7) * 8;
+    for (int i = 0; i < T::kSteps; ++i) {
+        const int u = t / kGroups + kThreads / kGroups * i, c = t % kGroups * 8;
         if (u0 + u >= len) continue;
-        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = load_as_f32(lds, (c + j) * kPitch + u);
-        store8((S *)a.turned + ((size_t)b * a.U + u0 + u) * a.C + c0 + c, a.C - c0 - c, v);
+        for (int j = 0; j < 8; ++j) e[i][j] = lds[(c + j) * T::kPitch + u];
+        store8_bits((S *)a.turned + ((size_t)b * a.U + u0 + u) * a.C + c0 + c, a.C - c0 - c, e[i]);
     }
 }
 
+constexpr int kSortBytes = kChunk * 4 + 3 * kRange * 4 + 2 * kWaves * 4;
+
 template <typename S>
-__global__ __launch_bounds__(256) void embed_order_kernel(EmbedBwd a)
+__global__ __launch_bounds__(kThreads) void embed_order_kernel(EmbedBwd a)
 {
-    __shared__ __align__(16) unsigned char smem[kChunk + kRange * 512 + (2 * kRange + 4) * 4];
+    __shared__ __align__(16) unsigned char smem[kSortBytes];
+    static_assert(Turn<S>::kBytes <= kSortBytes, "");
     int w = blockIdx.x;
     if (w < a.sorters) {
         sort_range(a, smem);
@@ -277,8 +320,8 @@ __global__ __launch_bounds__(256) void embed_order_kernel(EmbedBwd a)
     const size_t all = (size_t)a.V * a.C, from = (size_t)(w - a.turners) * kFill;
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kFill / 2048; ++i) {
-        const size_t at = from + i * 2048 + threadIdx.x * 8;
+    for (int i = 0; i < kFill / (kThreads * 8); ++i) {
+        const size_t at = from + (i * kThreads + threadIdx.x) * 8;
         if (at < all) store8(a.dtable + at, (int)min(all - at, (size_t)8), zero);
     }
 }
@@ -298,66 +341,57 @@ template <typename S>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a, int c_waves)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int unit = blockIdx.x * 4 + wave, run = unit / c_waves, c = (unit - run * c_waves) * 512 + lane * 8;
-    const int total = a.starts[a.V], i0 = run * kRun, cnt = min(kRun, total - i0);
+    const int unit = blockIdx.x * 4 + wave, run = unit / c_waves, c = (unit - run * c_waves) * 512 + lane * 8, i0 = run * kRun;
+    if (i0 >= a.N) return;
+    const Entry mine = a.order[min(i0 + (lane & (kRun - 1)), a.N - 1)];  // (those behind the last that there is are not used)
+    const int cnt = min(kRun, *a.total - i0);
     if (cnt <= 0) return;
-    const int mine = lane < cnt ? lane : cnt - 1;
-    const int place = a.order[i0 + mine], token = a.token[i0 + mine];
     const int n = a.C - c;
     const bool whole = a.C % 8 == 0;  // lanes behind the row read its last group and store nothing: no branch around a load
     const int from_c = whole ? min(c, a.C - 8) : c;
+    float v[kRun][8];
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+        const size_t row = (size_t)__builtin_amdgcn_readlane(mine.place, min(k, cnt - 1)) * a.C;
+        if (whole) load8((const S *)a.rows + row + from_c, 8, v[k]);
+        else load8((const S *)a.rows + row + c, n, v[k]);
+    }
     float acc[8];
-    auto leave = [&](int v) {
-        if (n <= 0) return;
-        const int from = a.starts[v], to = a.starts[v + 1];
-        if (from >= i0 && to <= i0 + kRun) {
-            finish_row(a, v, c, acc, n);
-        } else {  // (where the token began in an earlier run, it is this run's first)
-            store8(a.parts + ((size_t)run * 2 + (from < i0 ? 0 : 1)) * a.C + c, n, acc);
-        }
-    };
-    int current = __builtin_amdgcn_readfirstlane(token);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    for (int i = 0; i < cnt; i += 8) {
-        float v[8][8];
+    for (int j = 0; j < 8; ++j) acc[j] = v[0][j];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int p = __builtin_amdgcn_readlane(place, min(i + k, cnt - 1));
-            if (whole) load8((const S *)a.rows + (size_t)p * a.C + from_c, 8, v[k]);
-            else load8((const S *)a.rows + (size_t)p * a.C + c, n, v[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (i + k >= cnt) break;
-            const int id = __builtin_amdgcn_readlane(token, i + k);
-            if (id != current) {
-                leave(current);
-                current = id;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    for (int k = 0; k < kRun; ++k) {
+        if (k >= cnt) break;
+        const int token = __builtin_amdgcn_readlane(mine.token, k);
+        if (k + 1 == cnt || __builtin_amdgcn_readlane(mine.token, k + 1 < kRun ? k + 1 : k) != token) {
+            const int from = __builtin_amdgcn_readlane(mine.from, k), to = __builtin_amdgcn_readlane(mine.to, k);
+            if (n > 0) {
+                if (from >= i0 && to <= i0 + kRun) finish_row(a, token, c, acc, n);
+                else store8(a.parts + ((size_t)run * 2 + (from < i0 ? 0 : 1)) * a.C + c, n, acc);  // (begun in an earlier run: this one's first)
             }
+            if (k + 1 < kRun) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += v[k][j];
+                for (int j = 0; j < 8; ++j) acc[j] = v[k + 1 < kRun ? k + 1 : k][j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += v[k + 1 < kRun ? k + 1 : k][j];
         }
     }
-    leave(current);
 }
 
-// The token that begins in a run and goes beyond it: its parts in order, a wavefront every fourth of them
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a, int c_waves)
+// The token that begins in a run and goes beyond it: its parts in order, a wavefront every eighth of them
+__global__ __launch_bounds__(512) void embed_join_kernel(EmbedBwd a, int c_waves)
 {
-    __shared__ float sums[3][64][8];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int run = blockIdx.x / c_waves, c = (blockIdx.x - run * c_waves) * 512 + lane * 8, n = a.C - c;
-    const int total = a.starts[a.V], i0 = run * kRun;
-    if (i0 + kRun >= total) return;  // (the last run: nothing goes beyond it)
-    const int v = a.token[i0 + kRun - 1], from = a.starts[v], to = a.starts[v + 1];
-    if (from < i0 || to <= i0 + kRun) return;
-    const int last = (to - 1) / kRun;
+    __shared__ float sums[7][8][64];
+    const int run = blockIdx.x / c_waves, i0 = run * kRun;
+    const Entry e = a.order[i0 + kRun - 1];
+    if (i0 + kRun >= *a.total || e.from < i0 || e.to <= i0 + kRun) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.x - run * c_waves) * 512 + lane * 8, n = a.C - c;
+    const int last = (e.to - 1) / kRun;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int r = run + wave; r <= last; r += 4) {
+#pragma unroll 8
+    for (int r = run + wave; r <= last; r += 8) {
         float p[8];
         load8(a.parts + ((size_t)r * 2 + (r == run ? 1 : 0)) * a.C + c, n, p);
 #pragma unroll
@@ -365,20 +399,20 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a, int c_waves
     }
     if (wave) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[wave - 1][lane][j] = acc[j];
+        for (int j = 0; j < 8; ++j) sums[wave - 1][j][lane] = acc[j];
     }
     __syncthreads();
     if (wave || n <= 0) return;
 #pragma unroll
-    for (int w = 0; w < 3; ++w)
+    for (int w = 0; w < 7; ++w)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += sums[w][lane][j];
-    finish_row(a, v, c, acc, n);
+        for (int j = 0; j < 8; ++j) acc[j] += sums[w][j][lane];
+    finish_row(a, e.token, c, acc, n);
 }
 
 // What a call of these sizes keeps in its workspace
 struct Plan {
-    size_t rows, order, token, starts, parts, all;  // offsets, and the whole
+    size_t order, total, parts, all;  // offsets, and the whole
     int runs;
 };
 Plan plan_of(int B, int V, int C, int U, int dtype)
@@ -387,9 +421,8 @@ Plan plan_of(int B, int V, int C, int U, int dtype)
     const size_t N = (size_t)B * U;
     p.runs = (int)((N + kRun - 1) / kRun);
     p.order = U > 1 ? align_up(N * C * element(dtype), 256) : 0;  // (single tokens lie as rows already)
-    p.token = p.order + align_up(N * 4, 256);
-    p.starts = p.token + align_up(N * 4, 256);
-    p.parts = p.starts + align_up(((size_t)V + 1) * 4, 256);
+    p.total = p.order + align_up(N * sizeof(Entry), 256);
+    p.parts = p.total + 256;
     p.all = p.parts + align_up((size_t)p.runs * 2 * C * 4, 256);
     return p;
 }
@@ -398,14 +431,14 @@ template <typename S>
 hipError_t run_bwd(EmbedBwd a, int runs, hipStream_t s)
 {
     const size_t fillers = a.add ? 0 : ((size_t)a.V * a.C + kFill - 1) / kFill;
-    embed_order_kernel<S><<<dim3((unsigned)(a.sorters + a.turners + fillers)), dim3(256), 0, s>>>(a);
+    embed_order_kernel<S><<<dim3((unsigned)(a.sorters + a.turners + fillers)), dim3(kThreads), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int c_waves = (a.C + 511) / 512;
     embed_sum_kernel<S><<<dim3((unsigned)(((long long)runs * c_waves + 3) / 4)), dim3(256), 0, s>>>(a, c_waves);
     e = hipGetLastError();
     if (e != hipSuccess || runs == 1) return e;
-    embed_join_kernel<<<dim3((unsigned)(runs - 1) * c_waves), dim3(256), 0, s>>>(a, c_waves);
+    embed_join_kernel<<<dim3((unsigned)(runs - 1) * c_waves), dim3(512), 0, s>>>(a, c_waves);
     return hipGetLastError();
 }
 
@@ -466,15 +499,15 @@ int nm_embedding_bwd(int B, int V, int C, int U, const void *dout, const void *i
     a.scale = scale;
     a.dtable = dtable;
     a.add = (flags & NM_ACCUM_DW) != 0;
-    a.order = (int *)(ws + p.order);
-    a.token = (int *)(ws + p.token);
-    a.starts = (int *)(ws + p.starts);
+    a.order = (Entry *)(ws + p.order);
+    a.total = (int *)(ws + p.total);
     a.parts = (float *)(ws + p.parts);
     // as many ranges as there are CUs, where that leaves a range no more tokens than a workgroup has counters for
-    a.range = (V + 255) / 256 < kRange ? (V + 255) / 256 : kRange;
-    a.sorters = (V + a.range - 1) / a.range;
+    a.range = V > 256 * kRange ? kRange : (V + 255) / 256;
+    a.sorters = (V - 1) / a.range + 1;
     a.u_tiles = (U + 63) / 64;
-    a.c_tiles = (C + 63) / 64;
+    const int turn = dtype == NM_BF16 ? Turn<bf16_t>::kChannels : Turn<float>::kChannels;
+    a.c_tiles = (C + turn - 1) / turn;
     a.turners = U > 1 ? B * a.u_tiles * a.c_tiles : 0;
     hipStream_t s = (hipStream_t)hip_stream;
     return status_of(dtype == NM_BF16 ? run_bwd<bf16_t>(a, p.runs, s) : run_bwd<float>(a, p.runs, s));

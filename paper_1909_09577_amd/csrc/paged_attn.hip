@@ -346,38 +346,58 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
     }
 }
 
-// Joins the sums of `splits` workgroups in order: 16 rows (tokens of heads) a workgroup, a thread eight channels of one
-template <typename S>
-__global__ __launch_bounds__(256) void paged_join_kernel(Paged a)
+// Joins the sums of `splits` workgroups in order: a wavefront takes a row (a token of a head), a lane one split's maximum and sum, and then
+// eight channels of every fourth split.  (One thread for a row's maxima, split after split, took 17 us for 512 rows of 16 splits.)
+template <typename S, int ROWS>
+__global__ __launch_bounds__(ROWS * 64) void paged_join_kernel(Paged a)
 {
-    __shared__ float tile[16][128 + 1];
-    const size_t rows = (size_t)a.B * a.H * a.U;
-    const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
-    const size_t row0 = (size_t)blockIdx.x * 16, row = min(row0 + r, rows - 1);
-    float top = -INFINITY, total = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[((size_t)s * rows + row) * 2]);
-    const float base = top == -INFINITY ? 0.f : top;
-    const int d0 = part * 8;
+    __shared__ float tile[ROWS][128 + 1];
+    const size_t rows = (size_t)a.B * a.H * a.U, row0 = (size_t)blockIdx.x * ROWS;
+    const int lane = threadIdx.x & 63, r = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = lane >> 4, d0 = (lane & 15) * 8;
+    const size_t row = min(row0 + r, rows - 1);
+    float2 ml = {-INFINITY, 0.f};
+    if (lane < a.splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + ((size_t)lane * rows + row) * 2);
+    const float *part = a.part + row * a.D + min(d0, a.D - 8);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + ((size_t)s * rows + row) * 2);
-        const float w = __builtin_amdgcn_exp2f(ml.x - base);
-        total += w * ml.y;
-        if (d0 < a.D) {
-            float p[8];
-            load8(a.part + ((size_t)s * rows + row) * a.D + d0, 8, p);
+    float top = ml.x;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += w * p[j];
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float w = __builtin_amdgcn_exp2f(ml.x - (top == -INFINITY ? 0.f : top));
+    float total = w * ml.y;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    for (int s0 = 0; s0 < a.splits; s0 += 16) {  // (four splits' loads of a lane at a time)
+        float p[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load8(part + (size_t)min(s0 + 4 * k + slice, a.splits - 1) * rows * a.D, 8, p[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int s = s0 + 4 * k + slice;
+            const float ws = __shfl(w, min(s, 63));  // (0 from the last split on)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += s < a.splits ? ws * p[k][j] : 0.f;
         }
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    if (a.lse && part == 0 && row0 + r < rows) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tile[r][d0 + j] = v[j] * inv;
+    for (int j = 0; j < 8; ++j) {
+        v[j] += __shfl_xor(v[j], 16);
+        v[j] += __shfl_xor(v[j], 32);
+        v[j] *= inv;
+    }
+    if (a.lse && lane == 0 && row0 + r < rows) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+    if (a.U == 1) {  // a head's channels side by side
+        const size_t b = row / a.H, h = row - b * a.H;
+        if (slice == 0 && d0 < a.D && row0 + r < rows) store8((S *)a.out + b * a.os + h * a.D + d0, 8, v);
+        return;
+    }
+    if (slice == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile[r][d0 + j] = v[j];
+    }
     __syncthreads();
-    // neighbouring lanes store neighbouring tokens, or channels where there is one token
-    for (int e = threadIdx.x; e < 16 * a.D; e += 256) {
-        const int er = a.U >= 8 ? e & 15 : e / a.D, d = a.U >= 8 ? e >> 4 : e - er * a.D;
+    for (int e = threadIdx.x; e < ROWS * a.D; e += ROWS * 64) {  // neighbouring lanes store neighbouring tokens
+        const int er = e % ROWS, d = e / ROWS;
         const size_t to = row0 + er;
         if (to >= rows) continue;
         const size_t bh = to / a.U, u = to - bh * a.U, b = bh / a.H, h = bh - b * a.H;
@@ -438,7 +458,8 @@ hipError_t run(const Paged &a, int blocks, hipStream_t s)
     }
     if (e != hipSuccess || a.splits == 1) return e;
     const size_t rows = (size_t)a.B * a.H * a.U;
-    paged_join_kernel<S><<<dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s>>>(a);
+    if (a.U >= 16) paged_join_kernel<S, 16><<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s>>>(a);
+    else paged_join_kernel<S, 4><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -1,10 +1,13 @@
 // Log-probabilities of given tokens, entropies, the likeliest classes, and the scores' gradient (definition: include/nm_token_scores.h).
 //
 // Forward: one pass over the scores with a running maximum m, s = sum exp(z - m) and t = sum exp(z - m) * (z - m), of which
-// lse = m + log s and entropy = log s - t/s; and with a sorted list of the largest scores and their classes.  Places lie side by side in
-// memory, so lanes are places (64 of them, or fewer places times several classes); wavefronts, workgroups and spare lanes share the
-// classes.  What they found is joined in pairs: of two sorted lists a_i and b_i of K the K largest of all are the larger ones of a_i and
-// b_(K-1-i), which are in order again after log K exchanges.
+// lse = m + log s and entropy = log s - t/s, in powers of two throughout.  Places lie side by side in memory, so lanes are places (64 of
+// them, or fewer places times several classes); wavefronts, workgroups and spare lanes share the classes, and join what they found in pairs.
+//
+// The largest scores in order: a lane takes eight classes at a time and keeps a list of the largest of their maxima.  The K largest scores lie in
+// the eights of the K largest maxima (an eight that is not among them has K scores before all of its own), so that one insertion is
+// made for eight classes at most, and at the end the K eights are read again and sorted.  Of two sorted lists a_i and b_i of K the K largest of
+// all are the larger ones of a_i and b_(K-1-i), which are in order again after log K exchanges.
 //
 // Backward: element by element from the saved lse and entropy, a thread on the same eight places of every so many classes.
 #include "../../include/nm_token_scores.h"
@@ -16,6 +19,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr int kNone = 0x7fffffff;  // class of an empty place in a list: behind all others
 constexpr int kMaxSplits = 64;
+constexpr int kRounds = 32;  // of classes side by side that a wavefront does at least where workgroups share a place's classes
 
 struct ScoresFwd {
     int B, V, U;
@@ -34,25 +38,29 @@ struct ScoresFwd {
 
 template <int K>
 struct State {
-    float m, s, t;
+    float m, s, t;  // in powers of two
     float z[K ? K : 1];
     int id[K ? K : 1];
-    __device__ __forceinline__ void clear()
+    __device__ __forceinline__ void clear_list()
     {
-        m = -INFINITY;
-        s = t = 0.f;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             z[i] = -INFINITY;
             id[i] = kNone;
         }
     }
+    __device__ __forceinline__ void clear()
+    {
+        m = -INFINITY;
+        s = t = 0.f;
+        clear_list();
+    }
     static __device__ __forceinline__ bool before(float za, int ia, float zb, int ib) { return za > zb || (za == zb && ia < ib); }
     // sums are taken to `top` from here on
     __device__ __forceinline__ void rebase(float top)
     {
         if (s != 0.f) {
-            const float d = m - top, f = __builtin_amdgcn_exp2f(d * kLog2e);
+            const float d = m - top, f = __builtin_amdgcn_exp2f(d);
             t = f * (t + d * s);
             s *= f;
         }
@@ -68,17 +76,20 @@ struct State {
             id[i] = here ? (above ? id[i ? i - 1 : 0] : c) : id[i];
         }
     }
-    __device__ __forceinline__ void join(float om, float os, float ot, const float (&oz)[K ? K : 1], const int (&oid)[K ? K : 1])
+    __device__ __forceinline__ void join_sums(float om, float os, float ot)
     {
         const float top = fmaxf(m, om);
         if (m < top) rebase(top);
         if (om < top && os != 0.f) {
-            const float d = om - top, f = __builtin_amdgcn_exp2f(d * kLog2e);
+            const float d = om - top, f = __builtin_amdgcn_exp2f(d);
             ot = f * (ot + d * os);
             os *= f;
         }
         s += os;
         t += ot;
+    }
+    __device__ __forceinline__ void join_list(const float (&oz)[K ? K : 1], const int (&oid)[K ? K : 1])
+    {
         if constexpr (K > 0) {
             float nz[K];
             int ni[K];
@@ -93,9 +104,9 @@ struct State {
 #pragma unroll
                 for (int i = 0; i < K; ++i)
                     if (!(i & d)) {
-                        const bool ok = before(nz[i], ni[i], nz[i + d], ni[i + d]) || ni[i] == ni[i + d];
-                        const float zl = ok ? nz[i] : nz[i + d], zh = ok ? nz[i + d] : nz[i];
-                        const int il = ok ? ni[i] : ni[i + d], ih = ok ? ni[i + d] : ni[i];
+                        const bool swap = before(nz[i + d], ni[i + d], nz[i], ni[i]);
+                        const float zl = swap ? nz[i + d] : nz[i], zh = swap ? nz[i] : nz[i + d];
+                        const int il = swap ? ni[i + d] : ni[i], ih = swap ? ni[i] : ni[i + d];
                         nz[i] = zl;
                         nz[i + d] = zh;
                         ni[i] = il;
@@ -108,7 +119,7 @@ struct State {
             }
         }
     }
-    __device__ __forceinline__ void join_lane(int mask)
+    __device__ __forceinline__ void join_list_of_lane(int mask)
     {
         float oz[K ? K : 1];
         int oi[K ? K : 1];
@@ -117,39 +128,74 @@ struct State {
             oz[i] = __shfl_xor(z[i], mask);
             oi[i] = __shfl_xor(id[i], mask);
         }
-        join(__shfl_xor(m, mask), __shfl_xor(s, mask), __shfl_xor(t, mask), oz, oi);
+        join_list(oz, oi);
+    }
+    __device__ __forceinline__ void join_lane(int mask)
+    {
+        join_sums(__shfl_xor(m, mask), __shfl_xor(s, mask), __shfl_xor(t, mask));
+        join_list_of_lane(mask);
     }
 };
 
-// The results of a place
+// Eights: a wavefront has classes c0 .. c1-1, a lane of it every step-th of them from c0 + (lane's number) on, eight at a time.  The classes of
+// the eight that holds class c, in order.
+struct Eight {
+    int first, step, end;
+    __device__ __forceinline__ Eight(const ScoresFwd &a, int c)
+    {
+        step = 64 >> a.log_lanes;
+        const int c0 = c / a.per * a.per, round = (c - c0) / step;
+        first = c - (round & 7) * step;
+        end = min(a.V, c0 + a.per);
+    }
+};
+// The sorted scores of one of the listed eights are added to `list`
 template <typename S, int K>
-__device__ __forceinline__ void finish(const ScoresFwd &a, int b, int u, bool there, const State<K> &st)
+__device__ __forceinline__ void read_again(const ScoresFwd &a, const S *column, float top, int id, State<K> &list)
+{
+    const Eight e(a, id == kNone ? 0 : id);
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = load_as_f32(column, (size_t)min(e.first + i * e.step, a.V - 1) * a.U);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = e.first + i * e.step;
+        const bool is = id != kNone && c < e.end;
+        const float v = is && z[i] == z[i] ? z[i] : -INFINITY;
+        const int vc = is ? c : kNone;
+        if (__any(State<K>::before(v, vc, list.z[K ? K - 1 : 0], list.id[K ? K - 1 : 0]))) list.insert(v, vc);
+    }
+}
+
+// The results of a place, but for its alternatives; the log-sum-exp
+template <typename S>
+__device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, bool there, float m, float s, float t)
 {
     const size_t at = (size_t)b * a.U + u;
-    const float log_s = __builtin_amdgcn_logf(st.s) * kLn2, lse = (st.m == -INFINITY ? 0.f : st.m) + log_s;
+    const float log_s = __builtin_amdgcn_logf(s), lse = ((m == -INFINITY ? 0.f : m) + log_s) * kLn2;
     if (a.lse) a.lse[at] = there ? lse : 0.f;
-    if (a.entropy) a.entropy[at] = there && st.s != 0.f ? log_s - st.t / st.s : 0.f;
+    if (a.entropy) a.entropy[at] = there && s != 0.f ? (log_s - t / s) * kLn2 : 0.f;
     if (a.logp) {
         const int target = there ? a.targets.at(at, a.V) : -1;
         const float z = target < 0 ? 0.f : load_as_f32((const S *)a.scores, ((size_t)b * a.V + target) * a.U + u);
         a.logp[at] = target < 0 ? 0.f : (lse == -INFINITY ? lse : z - lse);
     }
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < a.top) {
-            const size_t to = ((size_t)b * a.top + i) * a.U + u;
-            a.top_ids[to] = there ? st.id[i] : -1;
-            a.top_logp[to] = there ? (lse == -INFINITY ? lse : st.z[i] - lse) : 0.f;
-        }
+    return lse;
+}
+__device__ __forceinline__ void finish_alternative(const ScoresFwd &a, int b, int u, bool there, int i, float z, int id, float lse)
+{
+    const size_t to = ((size_t)b * a.top + i) * a.U + u;
+    a.top_ids[to] = there ? id : -1;
+    a.top_logp[to] = there ? (lse == -INFINITY ? lse : z - lse) : 0.f;
 }
 
 template <typename S, int K>
-__global__ __launch_bounds__(256) void scores_fwd_kernel(ScoresFwd a)
+__global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFwd a)
 {
     constexpr int kAhead = 16;
-    __shared__ float sums[3][3][64];
-    __shared__ float list_z[K ? 3 : 1][K ? K : 1][64];
-    __shared__ int list_id[K ? 3 : 1][K ? K : 1][64];
+    __shared__ float sums[4][3][64];
+    __shared__ float list_z[K ? 4 : 1][K ? K : 1][64];
+    __shared__ int list_id[K ? 4 : 1][K ? K : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ut = blockIdx.x % a.u_tiles, rest = blockIdx.x / a.u_tiles, split = rest % a.splits, b = rest / a.splits;
     const int lanes = 1 << a.log_lanes, u = ut * lanes + (lane & (lanes - 1)), step = 64 >> a.log_lanes;
@@ -160,50 +206,71 @@ __global__ __launch_bounds__(256) void scores_fwd_kernel(ScoresFwd a)
     st.clear();
     const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + min(u, a.U - 1);
     if (ut * lanes < len) {  // (uniform)
-        const int mine = c0 + (lane >> a.log_lanes);
-        for (int c = mine; c - mine + c0 < c1; c += step * kAhead) {
-            float z[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(column, (size_t)min(c + i * step, a.V - 1) * a.U);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) z[i] = there && c + i * step < c1 ? z[i] : -INFINITY;
+        // rows of `step` classes, kAhead of them at a time; a lane's bytes from a row's first element are of 32 bits
+        const uint32_t mine = ((uint32_t)(lane >> a.log_lanes) * (uint32_t)a.U + (uint32_t)min(u, a.U - 1)) * (uint32_t)sizeof(S);
+        const size_t row = (size_t)step * a.U;
+        auto take = [&](const float (&z)[kAhead], int c) {  // c: this lane's first class
             float top = z[0];
 #pragma unroll
             for (int i = 1; i < kAhead; ++i) top = fmaxf(top, z[i]);
-            if (top > st.m) st.rebase(top);
+            if (top * kLog2e > st.m) st.rebase(top * kLog2e);
             const float base = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const float x = z[i] - base, e = __builtin_amdgcn_exp2f(x * kLog2e);
+                const float y = __builtin_fmaf(z[i], kLog2e, -base), e = __builtin_amdgcn_exp2f(y);
                 st.s += e;
-                st.t = __builtin_fmaf(e, fmaxf(x, -1e30f), st.t);  // (zero times what is barred)
+                st.t = __builtin_fmaf(e, fmaxf(y, -1e30f), st.t);  // (zero times what is barred)
             }
             if constexpr (K > 0) {
-                if (__any(top > st.z[K - 1] || st.id[K - 1] == kNone)) {
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const float v = z[i] == z[i] ? z[i] : -INFINITY;
-                        const int id = c + i * step < c1 ? c + i * step : kNone;
-                        if (__any(v > st.z[K - 1] || st.id[K - 1] == kNone)) st.insert(v, id);
+                for (int h = 0; h < kAhead; h += 8) {
+                    float best = z[h];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) best = fmaxf(best, z[h + i]);
+                    best = fmaxf(best, -INFINITY);  // (of eight NaN)
+                    if (__any(best > st.z[K - 1] || st.id[K - 1] == kNone)) {
+                        int at = kNone;  // the first class that has it
+#pragma unroll
+                        for (int i = 7; i >= 0; --i) {
+                            const int ci = c + (h + i) * step;
+                            at = ci < c1 && (z[h + i] == best || best == -INFINITY) ? ci : at;
+                        }
+                        st.insert(best == best ? best : -INFINITY, at);
                     }
                 }
             }
+        };
+        const S *p = (const S *)a.scores + (size_t)b * a.V * a.U + (size_t)c0 * a.U;
+        int c = c0;
+        for (; c + kAhead * step <= c1; c += kAhead * step, p += kAhead * row) {
+            float z[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(reinterpret_cast<const S *>(reinterpret_cast<const char *>(p + i * row) + mine), 0);
+            if (!there) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) z[i] = -INFINITY;
+            }
+            take(z, c + (lane >> a.log_lanes));
+        }
+        if (c < c1) {
+            const int first = c + (lane >> a.log_lanes);
+            float z[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(column, (size_t)min(first + i * step, a.V - 1) * a.U);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) z[i] = there && first + i * step < c1 ? z[i] : -INFINITY;
+            take(z, first);
         }
         for (int d = lanes; d < 64; d <<= 1) st.join_lane(d);
     }
-    if (wave) {
-        sums[wave - 1][0][lane] = st.m;
-        sums[wave - 1][1][lane] = st.s;
-        sums[wave - 1][2][lane] = st.t;
+    auto leave = [&](int w) {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            list_z[wave - 1][i][lane] = st.z[i];
-            list_id[wave - 1][i][lane] = st.id[i];
+            list_z[w][i][lane] = st.z[i];
+            list_id[w][i][lane] = st.id[i];
         }
-    }
-    __syncthreads();
-    if (wave) return;
-    for (int w = 0; w < 3; ++w) {
+    };
+    auto join_list_of = [&](int w) {
         float oz[K ? K : 1];
         int oi[K ? K : 1];
 #pragma unroll
@@ -211,34 +278,73 @@ __global__ __launch_bounds__(256) void scores_fwd_kernel(ScoresFwd a)
             oz[i] = list_z[w][i][lane];
             oi[i] = list_id[w][i][lane];
         }
-        st.join(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane], oz, oi);
-    }
-    if (lane >= lanes || u >= a.U) return;
-    if (a.splits == 1) {
-        finish<S, K>(a, b, u, there, st);
+        st.join_list(oz, oi);
+    };
+    sums[wave][0][lane] = st.m;
+    sums[wave][1][lane] = st.s;
+    sums[wave][2][lane] = st.t;
+    leave(wave);
+    __syncthreads();
+    if (a.splits > 1) {
+        if (wave) return;
+        for (int w = 1; w < 4; ++w) {
+            st.join_sums(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane]);
+            join_list_of(w);
+        }
+        if (lane >= lanes || u >= a.U) return;
+        const size_t all = (size_t)a.B * a.U, at = (size_t)b * a.U + u;
+        float *p = a.part + (size_t)split * 3 * all + at;
+        p[0] = st.m;
+        p[all] = st.s;
+        p[2 * all] = st.t;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            a.part_z[((size_t)split * K + i) * all + at] = st.z[i];
+            a.part_id[((size_t)split * K + i) * all + at] = st.id[i];
+        }
         return;
     }
-    const size_t all = (size_t)a.B * a.U, at = (size_t)b * a.U + u;
-    float *p = a.part + (size_t)split * 3 * all + at;
-    p[0] = st.m;
-    p[all] = st.s;
-    p[2 * all] = st.t;
+    // every wavefront has the eights of all four, reads a fourth of them again, and the first one joins what they find
+    if constexpr (K > 0) {
+        for (int w = 0; w < 4; ++w)
+            if (w != wave) join_list_of(w);
+        State<K> best;
+        best.clear_list();
+        if (ut * lanes < len) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-        a.part_z[((size_t)split * K + i) * all + at] = st.z[i];
-        a.part_id[((size_t)split * K + i) * all + at] = st.id[i];
+            for (int i = 0; i < K; ++i)
+                if (i % 4 == wave) read_again<S, K>(a, column, st.z[i], st.id[i], best);
+        }
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            st.z[i] = best.z[i];
+            st.id[i] = best.id[i];
+        }
+        __syncthreads();
+        leave(wave);
+        __syncthreads();
     }
+    if (wave) return;
+    for (int w = 1; w < 4; ++w) {
+        st.join_sums(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane]);
+        join_list_of(w);
+    }
+    if (lane >= lanes || u >= a.U) return;
+    const float lse = finish_sums<S>(a, b, u, there, st.m, st.s, st.t);
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (i < a.top) finish_alternative(a, b, u, there, i, st.z[i], st.id[i], lse);
 }
 
-// Joins what `splits` workgroups found: neighbouring lanes take a place's splits
+// Joins what `splits` workgroups found: neighbouring lanes take a place's splits, and then a share of its eights
 template <typename S, int K>
 __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a, int log_splits)
 {
-    const int t = blockIdx.x * 256 + threadIdx.x, split = t & ((1 << log_splits) - 1), at = t >> log_splits, all = a.B * a.U;
-    const bool exists = at < all;
+    const int t = blockIdx.x * 256 + threadIdx.x, group = 1 << log_splits, split = t & (group - 1), all = a.B * a.U, at = min(t >> log_splits, all - 1);
+    const bool exists = t >> log_splits < all;
     State<K> st;
     st.clear();
-    if (exists && split < a.splits) {
+    if (split < a.splits) {
         const float *p = a.part + (size_t)split * 3 * all + at;
         st.m = p[0];
         st.s = p[all];
@@ -249,10 +355,30 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a, int log_s
             st.id[i] = a.part_id[((size_t)split * K + i) * all + at];
         }
     }
-    for (int d = 1; d < 1 << log_splits; d <<= 1) st.join_lane(d);
-    if (split || !exists) return;
+    for (int d = 1; d < group; d <<= 1) st.join_lane(d);
     const int b = at / a.U, u = at - b * a.U;
-    finish<S, K>(a, b, u, u < length_in(a.len, b, a.U), st);
+    const bool there = u < length_in(a.len, b, a.U);
+    float lse = 0.f;
+    if (split == 0 && exists) lse = finish_sums<S>(a, b, u, there, st.m, st.s, st.t);
+    if constexpr (K > 0) {
+        State<K> best;
+        best.clear_list();
+        for (int i0 = 0; i0 < K; i0 += group) {
+            float z = -INFINITY;
+            int id = kNone;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {  // (a list is in registers: no index of a lane's own)
+                z = i == i0 + split ? st.z[i] : z;
+                id = i == i0 + split ? st.id[i] : id;
+            }
+            read_again<S, K>(a, (const S *)a.scores + (size_t)b * a.V * a.U + u, z, there ? id : kNone, best);
+        }
+        for (int d = 1; d < group && d < K; d <<= 1) best.join_list_of_lane(d);
+        if (split || !exists) return;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i < a.top) finish_alternative(a, b, u, there, i, best.z[i], best.id[i], lse);
+    }
 }
 
 // The lists' length that serves `top`: of two a power
@@ -271,7 +397,7 @@ Plan plan_of(int B, int V, int U, int top)
     // four workgroups a CU, but a wavefront has 32 rounds of classes to do at least: what follows them takes about as long
     const long long groups = (long long)B * p.u_tiles;
     long long splits = 1024 / groups;
-    const long long most = V / (4LL * step * 32);
+    const long long most = V / (4LL * step * kRounds);
     if (splits > most) splits = most;
     if (splits > kMaxSplits) splits = kMaxSplits;
     if (splits < 1) splits = 1;
@@ -420,7 +546,7 @@ int check(int B, int V, int U, int dtype)
 {
     if (B <= 0 || V <= 0 || U <= 0 || !known_dtype(dtype)) return NM_ERR_BAD_ARG;
     const long long most = (1LL << 31) - 1;
-    if ((long long)B * V > most / U || V > most - (1 << 16)) return NM_ERR_UNSUPPORTED;  // (classes behind the last one are counted too)
+    if ((long long)B * V > most / U || V > most - (1 << 16) || U > 1 << 29) return NM_ERR_UNSUPPORTED;  // (classes behind the last one are counted too)
     // the grids, below 2^32 work items: a workgroup of the backward pass has 2048 elements, or one item's rest
     if ((long long)B * ((U + 63) / 64) >= 1LL << 23 || (long long)B * (((long long)V * U + 2047) / 2048) >= 1LL << 24) return NM_ERR_UNSUPPORTED;
     return NM_OK;

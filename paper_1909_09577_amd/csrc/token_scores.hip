@@ -6,8 +6,8 @@
 //
 // The largest scores in order: a lane takes eight classes at a time and keeps a list of the largest of their maxima.  The K largest scores lie in
 // the eights of the K largest maxima (an eight that is not among them has K scores before all of its own), so that one insertion is
-// made for eight classes at most, and at the end the K eights are read again and sorted.  Of two sorted lists a_i and b_i of K the K largest of
-// all are the larger ones of a_i and b_(K-1-i), which are in order again after log K exchanges.
+// made for eight classes at most, and at the end the K eights are read again and put in order.  Of two sorted lists a_i and b_i of K the K
+// largest of all are the larger ones of a_i and b_(K-1-i), which are in order again after log K exchanges.
 //
 // Backward: element by element from the saved lse and entropy, a thread on the same eight places of every so many classes.
 #include "../../include/nm_token_scores.h"
@@ -18,8 +18,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr int kNone = 0x7fffffff;  // class of an empty place in a list: behind all others
-constexpr int kMaxSplits = 64;
-constexpr int kRounds = 32;  // of classes side by side that a wavefront does at least where workgroups share a place's classes
+constexpr int kRounds = 16;  // of classes side by side that a wavefront does at least where workgroups share a place's classes
 
 struct ScoresFwd {
     int B, V, U;
@@ -32,30 +31,37 @@ struct ScoresFwd {
     int log_lanes;  // log2 of the places that a wavefront has side by side
     int u_tiles, splits, per;  // classes of a wavefront
     float *part;    // [splits][3][B*U]: m, s, t
-    float *part_z;  // [splits][K][B*U]
-    int *part_id;
+    uint64_t *part_keys;  // [splits][K][B*U]
 };
 
-template <int K>
-struct State {
-    float m, s, t;  // in powers of two
-    float z[K ? K : 1];
-    int id[K ? K : 1];
-    __device__ __forceinline__ void clear_list()
-    {
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            z[i] = -INFINITY;
-            id[i] = kNone;
-        }
-    }
-    __device__ __forceinline__ void clear()
-    {
-        m = -INFINITY;
-        s = t = 0.f;
-        clear_list();
-    }
-    static __device__ __forceinline__ bool before(float za, int ia, float zb, int ib) { return za > zb || (za == zb && ia < ib); }
+// A score and its class as one number: the larger one comes first in order, of equal scores the lower class (0.0 and -0.0 are equal), a NaN
+// with the -infinities.
+typedef uint64_t key_t;
+__device__ __forceinline__ key_t key_of(float z, int c)
+{
+    const uint32_t u = __float_as_uint((z == z ? z : -INFINITY) + 0.f);
+    const uint32_t ordered = u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+    return (key_t)ordered << 32 | (uint32_t)~c;
+}
+__device__ __forceinline__ int class_of(key_t k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float score_of(key_t k)
+{
+    const uint32_t o = (uint32_t)(k >> 32);
+    return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o);
+}
+constexpr key_t kEmpty = (key_t)0x007fffffu << 32 | 0x80000000u;  // -infinity of class 2^31 - 1: behind all others
+
+__device__ __forceinline__ key_t shuffled(key_t k, int mask)
+{
+    return (key_t)(uint32_t)__shfl_xor((int)(k >> 32), mask) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)k, mask);
+}
+__device__ __forceinline__ key_t of_lane(key_t k, int lane)  // (the same lane for all)
+{
+    return (key_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+
+struct Sums {
+    float m = -INFINITY, s = 0.f, t = 0.f;  // in powers of two
     // sums are taken to `top` from here on
     __device__ __forceinline__ void rebase(float top)
     {
@@ -66,17 +72,7 @@ struct State {
         }
         m = top;
     }
-    __device__ __forceinline__ void insert(float v, int c)
-    {
-#pragma unroll
-        for (int i = K - 1; i >= 0; --i) {
-            // place i takes the newcomer, its upper neighbour or stays
-            const bool here = before(v, c, z[i], id[i]), above = i > 0 && before(v, c, z[i ? i - 1 : 0], id[i ? i - 1 : 0]);
-            z[i] = here ? (above ? z[i ? i - 1 : 0] : v) : z[i];
-            id[i] = here ? (above ? id[i ? i - 1 : 0] : c) : id[i];
-        }
-    }
-    __device__ __forceinline__ void join_sums(float om, float os, float ot)
+    __device__ __forceinline__ void join(float om, float os, float ot)
     {
         const float top = fmaxf(m, om);
         if (m < top) rebase(top);
@@ -88,93 +84,57 @@ struct State {
         s += os;
         t += ot;
     }
-    __device__ __forceinline__ void join_list(const float (&oz)[K ? K : 1], const int (&oid)[K ? K : 1])
+    __device__ __forceinline__ void join_lane(int mask) { join(__shfl_xor(m, mask), __shfl_xor(s, mask), __shfl_xor(t, mask)); }
+};
+
+template <int K>
+struct List {  // the K largest, in order
+    key_t k[K ? K : 1];
+    __device__ __forceinline__ List()
     {
-        if constexpr (K > 0) {
-            float nz[K];
-            int ni[K];
 #pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const bool mine = before(z[i], id[i], oz[K - 1 - i], oid[K - 1 - i]);
-                nz[i] = mine ? z[i] : oz[K - 1 - i];
-                ni[i] = mine ? id[i] : oid[K - 1 - i];
-            }
-#pragma unroll
-            for (int d = K / 2; d >= 1; d >>= 1)
-#pragma unroll
-                for (int i = 0; i < K; ++i)
-                    if (!(i & d)) {
-                        const bool swap = before(nz[i + d], ni[i + d], nz[i], ni[i]);
-                        const float zl = swap ? nz[i + d] : nz[i], zh = swap ? nz[i] : nz[i + d];
-                        const int il = swap ? ni[i + d] : ni[i], ih = swap ? ni[i] : ni[i + d];
-                        nz[i] = zl;
-                        nz[i + d] = zh;
-                        ni[i] = il;
-                        ni[i + d] = ih;
-                    }
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                z[i] = nz[i];
-                id[i] = ni[i];
-            }
-        }
+        for (int i = 0; i < K; ++i) k[i] = kEmpty;
     }
-    __device__ __forceinline__ void join_list_of_lane(int mask)
+    __device__ __forceinline__ void insert(key_t v)
     {
-        float oz[K ? K : 1];
-        int oi[K ? K : 1];
+        bool here[K ? K : 1];
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            oz[i] = __shfl_xor(z[i], mask);
-            oi[i] = __shfl_xor(id[i], mask);
-        }
-        join_list(oz, oi);
+        for (int i = 0; i < K; ++i) here[i] = v > k[i];
+#pragma unroll
+        for (int i = K - 1; i >= 0; --i)  // place i takes the newcomer, its upper neighbour or stays
+            k[i] = here[i] ? (i > 0 && here[i ? i - 1 : 0] ? k[i ? i - 1 : 0] : v) : k[i];
+    }
+    __device__ __forceinline__ void join(const key_t (&o)[K ? K : 1])
+    {
+#pragma unroll
+        for (int i = 0; i < K; ++i) k[i] = k[i] > o[K - 1 - i] ? k[i] : o[K - 1 - i];
+#pragma unroll
+        for (int d = K / 2; d >= 1; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+                if (!(i & d)) {
+                    const key_t hi = k[i] > k[i + d] ? k[i] : k[i + d], lo = k[i] > k[i + d] ? k[i + d] : k[i];
+                    k[i] = hi;
+                    k[i + d] = lo;
+                }
     }
     __device__ __forceinline__ void join_lane(int mask)
     {
-        join_sums(__shfl_xor(m, mask), __shfl_xor(s, mask), __shfl_xor(t, mask));
-        join_list_of_lane(mask);
+        key_t o[K ? K : 1];
+#pragma unroll
+        for (int i = 0; i < K; ++i) o[i] = shuffled(k[i], mask);
+        join(o);
     }
 };
-
-// Eights: a wavefront has classes c0 .. c1-1, a lane of it every step-th of them from c0 + (lane's number) on, eight at a time.  The classes of
-// the eight that holds class c, in order.
-struct Eight {
-    int first, step, end;
-    __device__ __forceinline__ Eight(const ScoresFwd &a, int c)
-    {
-        step = 64 >> a.log_lanes;
-        const int c0 = c / a.per * a.per, round = (c - c0) / step;
-        first = c - (round & 7) * step;
-        end = min(a.V, c0 + a.per);
-    }
-};
-// The sorted scores of one of the listed eights are added to `list`
-template <typename S, int K>
-__device__ __forceinline__ void read_again(const ScoresFwd &a, const S *column, float top, int id, State<K> &list)
-{
-    const Eight e(a, id == kNone ? 0 : id);
-    float z[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = load_as_f32(column, (size_t)min(e.first + i * e.step, a.V - 1) * a.U);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = e.first + i * e.step;
-        const bool is = id != kNone && c < e.end;
-        const float v = is && z[i] == z[i] ? z[i] : -INFINITY;
-        const int vc = is ? c : kNone;
-        if (__any(State<K>::before(v, vc, list.z[K ? K - 1 : 0], list.id[K ? K - 1 : 0]))) list.insert(v, vc);
-    }
-}
 
 // The results of a place, but for its alternatives; the log-sum-exp
 template <typename S>
-__device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, bool there, float m, float s, float t)
+__device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, bool there, const Sums &v)
 {
     const size_t at = (size_t)b * a.U + u;
-    const float log_s = __builtin_amdgcn_logf(s), lse = ((m == -INFINITY ? 0.f : m) + log_s) * kLn2;
+    const float log_s = __builtin_amdgcn_logf(v.s), lse = ((v.m == -INFINITY ? 0.f : v.m) + log_s) * kLn2;
     if (a.lse) a.lse[at] = there ? lse : 0.f;
-    if (a.entropy) a.entropy[at] = there && s != 0.f ? (log_s - t / s) * kLn2 : 0.f;
+    if (a.entropy) a.entropy[at] = there && v.s != 0.f ? (log_s - v.t / v.s) * kLn2 : 0.f;
     if (a.logp) {
         const int target = there ? a.targets.at(at, a.V) : -1;
         const float z = target < 0 ? 0.f : load_as_f32((const S *)a.scores, ((size_t)b * a.V + target) * a.U + u);
@@ -182,38 +142,35 @@ __device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, b
     }
     return lse;
 }
-__device__ __forceinline__ void finish_alternative(const ScoresFwd &a, int b, int u, bool there, int i, float z, int id, float lse)
-{
-    const size_t to = ((size_t)b * a.top + i) * a.U + u;
-    a.top_ids[to] = there ? id : -1;
-    a.top_logp[to] = there ? (lse == -INFINITY ? lse : z - lse) : 0.f;
-}
 
 template <typename S, int K>
 __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFwd a)
 {
     constexpr int kAhead = 16;
-    __shared__ float sums[4][3][64];
-    __shared__ float list_z[K ? 4 : 1][K ? K : 1][64];
-    __shared__ int list_id[K ? 4 : 1][K ? K : 1][64];
+    __shared__ float sums[3][3][64];
+    __shared__ key_t lists[K ? 3 : 1][K ? K : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ut = blockIdx.x % a.u_tiles, rest = blockIdx.x / a.u_tiles, split = rest % a.splits, b = rest / a.splits;
     const int lanes = 1 << a.log_lanes, u = ut * lanes + (lane & (lanes - 1)), step = 64 >> a.log_lanes;
     const int len = length_in(a.len, b, a.U);
     const int c0 = (split * 4 + wave) * a.per, c1 = min(a.V, c0 + a.per);
     const bool there = u < len;
-    State<K> st;
-    st.clear();
-    const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + min(u, a.U - 1);
+    Sums st;
+    List<K> list;
     if (ut * lanes < len) {  // (uniform)
         // rows of `step` classes, kAhead of them at a time; a lane's bytes from a row's first element are of 32 bits
         const uint32_t mine = ((uint32_t)(lane >> a.log_lanes) * (uint32_t)a.U + (uint32_t)min(u, a.U - 1)) * (uint32_t)sizeof(S);
         const size_t row = (size_t)step * a.U;
-        auto take = [&](const float (&z)[kAhead], int c) {  // c: this lane's first class
-            float top = z[0];
+        auto take = [&](const float (&z)[kAhead], int c, bool whole) {  // c: this lane's first class
+            float best[kAhead / 8];
 #pragma unroll
-            for (int i = 1; i < kAhead; ++i) top = fmaxf(top, z[i]);
-            if (top * kLog2e > st.m) st.rebase(top * kLog2e);
+            for (int h = 0; h < kAhead / 8; ++h) {
+                best[h] = z[8 * h];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) best[h] = fmaxf(best[h], z[8 * h + i]);
+            }
+            const float top = fmaxf(best[0], best[1]) * kLog2e;
+            if (top > st.m) st.rebase(top);
             const float base = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -223,19 +180,16 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
             }
             if constexpr (K > 0) {
 #pragma unroll
-                for (int h = 0; h < kAhead; h += 8) {
-                    float best = z[h];
-#pragma unroll
-                    for (int i = 1; i < 8; ++i) best = fmaxf(best, z[h + i]);
-                    best = fmaxf(best, -INFINITY);  // (of eight NaN)
-                    if (__any(best > st.z[K - 1] || st.id[K - 1] == kNone)) {
-                        int at = kNone;  // the first class that has it
+                for (int h = 0; h < kAhead / 8; ++h) {
+                    const float m = best[h] == best[h] ? best[h] : -INFINITY;  // (of eight NaN)
+                    if (__any(m > score_of(list.k[K - 1]) || list.k[K - 1] == kEmpty)) {
+                        int at = kNone;  // the first class that has it; NaN count as -infinity
 #pragma unroll
                         for (int i = 7; i >= 0; --i) {
-                            const int ci = c + (h + i) * step;
-                            at = ci < c1 && (z[h + i] == best || best == -INFINITY) ? ci : at;
+                            const int ci = c + (8 * h + i) * step;
+                            at = (z[8 * h + i] == m || m == -INFINITY) && (whole || ci < c1) ? ci : at;
                         }
-                        st.insert(best == best ? best : -INFINITY, at);
+                        list.insert(at == kNone ? kEmpty : key_of(m, at));
                     }
                 }
             }
@@ -250,134 +204,127 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) z[i] = -INFINITY;
             }
-            take(z, c + (lane >> a.log_lanes));
+            take(z, c + (lane >> a.log_lanes), true);
         }
         if (c < c1) {
+            const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + min(u, a.U - 1);
             const int first = c + (lane >> a.log_lanes);
             float z[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(column, (size_t)min(first + i * step, a.V - 1) * a.U);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) z[i] = there && first + i * step < c1 ? z[i] : -INFINITY;
-            take(z, first);
+            take(z, first, false);
         }
-        for (int d = lanes; d < 64; d <<= 1) st.join_lane(d);
+        for (int d = lanes; d < 64; d <<= 1) {
+            st.join_lane(d);
+            list.join_lane(d);
+        }
     }
-    auto leave = [&](int w) {
+    if (wave) {
+        sums[wave - 1][0][lane] = st.m;
+        sums[wave - 1][1][lane] = st.s;
+        sums[wave - 1][2][lane] = st.t;
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            list_z[w][i][lane] = st.z[i];
-            list_id[w][i][lane] = st.id[i];
-        }
-    };
-    auto join_list_of = [&](int w) {
-        float oz[K ? K : 1];
-        int oi[K ? K : 1];
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            oz[i] = list_z[w][i][lane];
-            oi[i] = list_id[w][i][lane];
-        }
-        st.join_list(oz, oi);
-    };
-    sums[wave][0][lane] = st.m;
-    sums[wave][1][lane] = st.s;
-    sums[wave][2][lane] = st.t;
-    leave(wave);
+        for (int i = 0; i < K; ++i) lists[wave - 1][i][lane] = list.k[i];
+    }
     __syncthreads();
-    if (a.splits > 1) {
-        if (wave) return;
-        for (int w = 1; w < 4; ++w) {
-            st.join_sums(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane]);
-            join_list_of(w);
-        }
-        if (lane >= lanes || u >= a.U) return;
-        const size_t all = (size_t)a.B * a.U, at = (size_t)b * a.U + u;
-        float *p = a.part + (size_t)split * 3 * all + at;
-        p[0] = st.m;
-        p[all] = st.s;
-        p[2 * all] = st.t;
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            a.part_z[((size_t)split * K + i) * all + at] = st.z[i];
-            a.part_id[((size_t)split * K + i) * all + at] = st.id[i];
-        }
-        return;
-    }
-    // every wavefront has the eights of all four, reads a fourth of them again, and the first one joins what they find
-    if constexpr (K > 0) {
-        for (int w = 0; w < 4; ++w)
-            if (w != wave) join_list_of(w);
-        State<K> best;
-        best.clear_list();
-        if (ut * lanes < len) {
-#pragma unroll
-            for (int i = 0; i < K; ++i)
-                if (i % 4 == wave) read_again<S, K>(a, column, st.z[i], st.id[i], best);
-        }
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            st.z[i] = best.z[i];
-            st.id[i] = best.id[i];
-        }
-        __syncthreads();
-        leave(wave);
-        __syncthreads();
-    }
     if (wave) return;
-    for (int w = 1; w < 4; ++w) {
-        st.join_sums(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane]);
-        join_list_of(w);
+    for (int w = 0; w < 3; ++w) {
+        st.join(sums[w][0][lane], sums[w][1][lane], sums[w][2][lane]);
+        key_t o[K ? K : 1];
+#pragma unroll
+        for (int i = 0; i < K; ++i) o[i] = lists[w][i][lane];
+        list.join(o);
     }
     if (lane >= lanes || u >= a.U) return;
-    const float lse = finish_sums<S>(a, b, u, there, st.m, st.s, st.t);
+    if (K == 0 && a.splits == 1) {
+        finish_sums<S>(a, b, u, there, st);
+        return;
+    }
+    const size_t all = (size_t)a.B * a.U, at = (size_t)b * a.U + u;
+    float *p = a.part + (size_t)split * 3 * all + at;
+    p[0] = st.m;
+    p[all] = st.s;
+    p[2 * all] = st.t;
 #pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < a.top) finish_alternative(a, b, u, there, i, st.z[i], st.id[i], lse);
+    for (int i = 0; i < K; ++i) a.part_keys[((size_t)split * K + i) * all + at] = list.k[i];
 }
 
-// Joins what `splits` workgroups found: neighbouring lanes take a place's splits, and then a share of its eights
-template <typename S, int K>
-__global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a, int log_splits)
+// How many of the first n lanes' `others` come before this lane's number (those behind the n-th are empty, up to a multiple of eight)
+__device__ __forceinline__ int rank_of(key_t k, key_t others, int n)
 {
-    const int t = blockIdx.x * 256 + threadIdx.x, group = 1 << log_splits, split = t & (group - 1), all = a.B * a.U, at = min(t >> log_splits, all - 1);
-    const bool exists = t >> log_splits < all;
-    State<K> st;
-    st.clear();
-    if (split < a.splits) {
-        const float *p = a.part + (size_t)split * 3 * all + at;
+    int rank = 0;
+    for (int j = 0; j < n; j += 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rank += of_lane(others, j + i) > k;
+    return rank;
+}
+
+// A wavefront joins what `splits` workgroups found of a place.  A lane has one of their lists' entries, and finds its place in order by
+// comparing it with all others; then one of the classes of the K eights that come first, read again, and the same.
+template <typename S, int K>
+__global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
+{
+    const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = a.B * a.U;
+    if (at >= all) return;
+    const int b = at / a.U, u = at - b * a.U;
+    const bool there = u < length_in(a.len, b, a.U);
+    Sums st;
+    key_t mine = kEmpty;
+    if (lane < a.splits) {
+        const float *p = a.part + (size_t)lane * 3 * all + at;
         st.m = p[0];
         st.s = p[all];
         st.t = p[2 * (size_t)all];
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            st.z[i] = a.part_z[((size_t)split * K + i) * all + at];
-            st.id[i] = a.part_id[((size_t)split * K + i) * all + at];
-        }
     }
-    for (int d = 1; d < group; d <<= 1) st.join_lane(d);
-    const int b = at / a.U, u = at - b * a.U;
-    const bool there = u < length_in(a.len, b, a.U);
+    if (K && lane < a.splits * K) mine = a.part_keys[(size_t)lane * all + at];
+    for (int d = 1; d < a.splits; d <<= 1) st.join_lane(d);  // (to lane 0 all; lanes behind the last split have nothing to add)
     float lse = 0.f;
-    if (split == 0 && exists) lse = finish_sums<S>(a, b, u, there, st.m, st.s, st.t);
+    if (lane == 0) lse = finish_sums<S>(a, b, u, there, st);
     if constexpr (K > 0) {
-        State<K> best;
-        best.clear_list();
-        for (int i0 = 0; i0 < K; i0 += group) {
-            float z = -INFINITY;
-            int id = kNone;
+        lse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lse)));
+        constexpr int kEach = K > 8 ? 2 : 1;  // classes of a lane
+        const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + u;
+        key_t found[kEach];
 #pragma unroll
-            for (int i = 0; i < K; ++i) {  // (a list is in registers: no index of a lane's own)
-                z = i == i0 + split ? st.z[i] : z;
-                id = i == i0 + split ? st.id[i] : id;
+        for (int e = 0; e < kEach; ++e) found[e] = kEmpty;
+        if (there) {  // (uniform)
+            int rank = rank_of(mine, mine, a.splits * K);
+            if (mine == kEmpty) rank = 64;
+            const int i = lane & 7, step = 64 >> a.log_lanes;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                int c = kNone;
+#pragma unroll
+                for (int j = 0; j < 8 && 8 * e + j < K; ++j) {  // lanes 8*j .. 8*j+7: the eight in place 8*e + j
+                    const uint64_t has = __ballot(rank == 8 * e + j);
+                    const int id = has ? class_of(of_lane(mine, __builtin_ctzll(has))) : kNone;
+                    c = lane >> 3 == j ? id : c;
+                }
+                if (c == kNone) continue;
+                // a wavefront has had classes from c0 on, a lane of it every step-th, eight at a time
+                const int c0 = c / a.per * a.per, round = (c - c0) / step;
+                c += (i - (round & 7)) * step;
+                if (c < min(a.V, c0 + a.per)) found[e] = key_of(load_as_f32(column, (size_t)c * a.U), c);
             }
-            read_again<S, K>(a, (const S *)a.scores + (size_t)b * a.V * a.U + u, z, there ? id : kNone, best);
         }
-        for (int d = 1; d < group && d < K; d <<= 1) best.join_list_of_lane(d);
-        if (split || !exists) return;
 #pragma unroll
-        for (int i = 0; i < K; ++i)
-            if (i < a.top) finish_alternative(a, b, u, there, i, best.z[i], best.id[i], lse);
+        for (int e = 0; e < kEach; ++e) {
+            int rank = 0;
+#pragma unroll
+            for (int f = 0; f < kEach; ++f) rank += rank_of(found[e], found[f], (K < 8 ? K : 8) * 8);
+            if (there && found[e] != kEmpty && rank < a.top) {
+                const size_t to = ((size_t)b * a.top + rank) * a.U + u;
+                a.top_ids[to] = class_of(found[e]);
+                a.top_logp[to] = lse == -INFINITY ? lse : score_of(found[e]) - lse;
+            }
+        }
+        if (!there && lane < a.top) {
+            const size_t to = ((size_t)b * a.top + lane) * a.U + u;
+            a.top_ids[to] = -1;
+            a.top_logp[to] = 0.f;
+        }
     }
 }
 
@@ -386,26 +333,29 @@ int list_of(int top) { return top <= 1 ? top : top <= 4 ? 4 : top <= 8 ? 8 : 16;
 
 struct Plan {
     int log_lanes, u_tiles, splits, per;
-    size_t part_bytes, list_bytes;  // of the sums, of the scores of the lists
+    size_t part_bytes, list_bytes;
 };
 Plan plan_of(int B, int V, int U, int top)
 {
     Plan p = {};
+    // places side by side: as many as there are, and of long rows 32 where the last 64 would be less than half full
     while (p.log_lanes < 6 && (1 << p.log_lanes) < U) ++p.log_lanes;
-    const int lanes = 1 << p.log_lanes, step = 64 >> p.log_lanes;
+    if (U > 32 && U % 64 > 0 && U % 64 <= 32) p.log_lanes = 5;
+    const int lanes = 1 << p.log_lanes, step = 64 >> p.log_lanes, list = list_of(top);
     p.u_tiles = (U + lanes - 1) / lanes;
-    // four workgroups a CU, but a wavefront has 32 rounds of classes to do at least: what follows them takes about as long
+    // four workgroups a CU, but a wavefront has kRounds rounds of classes to do at least, and a wavefront joins all lists of a place
     const long long groups = (long long)B * p.u_tiles;
     long long splits = 1024 / groups;
-    const long long most = V / (4LL * step * kRounds);
+    const long long most = V / (4LL * step * kRounds), joined = 64 / (list ? list : 1);
     if (splits > most) splits = most;
-    if (splits > kMaxSplits) splits = kMaxSplits;
+    if (splits > joined) splits = joined;
     if (splits < 1) splits = 1;
     p.per = (int)((V + 4 * splits - 1) / (4 * splits));
     p.splits = (int)((V + 4LL * p.per - 1) / (4LL * p.per));
     const size_t all = (size_t)B * U;
-    p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * 3 * all * 4, 256) : 0;
-    p.list_bytes = p.splits > 1 ? align_up((size_t)p.splits * list_of(top) * all * 4, 256) : 0;
+    const bool parts = p.splits > 1 || list;
+    p.part_bytes = parts ? align_up((size_t)p.splits * 3 * all * 4, 256) : 0;
+    p.list_bytes = align_up((size_t)p.splits * list * all * sizeof(key_t), 256);
     return p;
 }
 
@@ -414,11 +364,8 @@ hipError_t run_list(const ScoresFwd &a, hipStream_t s)
 {
     scores_fwd_kernel<S, K><<<dim3((unsigned)a.B * a.u_tiles * a.splits), dim3(256), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    int log_splits = 0;
-    while ((1 << log_splits) < a.splits) ++log_splits;
-    const long long threads = ((long long)a.B * a.U) << log_splits;
-    scores_join_kernel<S, K><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a, log_splits);
+    if (e != hipSuccess || (K == 0 && a.splits == 1)) return e;
+    scores_join_kernel<S, K><<<dim3((unsigned)(((long long)a.B * a.U + 3) / 4)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename S>
@@ -567,7 +514,7 @@ size_t nm_token_scores_workspace_bytes(int B, int V, int U, int top, int dtype)
 {
     if (check(B, V, U, dtype) != NM_OK || check_top(V, top) != NM_OK) return 0;
     const Plan p = plan_of(B, V, U, top);
-    return p.part_bytes + 2 * p.list_bytes;
+    return p.part_bytes + p.list_bytes;
 }
 
 int nm_token_scores_fwd(int B, int V, int U, const void *scores, const void *targets, int target_bytes, const int *lengths, int top,
@@ -589,7 +536,7 @@ int nm_token_scores_fwd(int B, int V, int U, const void *scores, const void *tar
             if (meet(out[i], out[j])) return NM_ERR_BAD_ARG;
     }
     const Plan p = plan_of(B, V, U, top);
-    if (workspace_missing(workspace, workspace_bytes, p.part_bytes + 2 * p.list_bytes)) return NM_ERR_WORKSPACE;
+    if (workspace_missing(workspace, workspace_bytes, p.part_bytes + p.list_bytes)) return NM_ERR_WORKSPACE;
     ScoresFwd a = {};
     a.B = B; a.V = V; a.U = U;
     a.scores = scores;
@@ -599,8 +546,7 @@ int nm_token_scores_fwd(int B, int V, int U, const void *scores, const void *tar
     a.top = top;
     a.log_lanes = p.log_lanes; a.u_tiles = p.u_tiles; a.splits = p.splits; a.per = p.per;
     a.part = (float *)workspace;
-    a.part_z = (float *)((char *)workspace + p.part_bytes);
-    a.part_id = (int *)((char *)workspace + p.part_bytes + p.list_bytes);
+    a.part_keys = (uint64_t *)((char *)workspace + p.part_bytes);
     hipStream_t s = (hipStream_t)hip_stream;
     return status_of(dtype == NM_BF16 ? run_fwd<bf16_t>(a, s) : run_fwd<float>(a, s));
 }

@@ -100,9 +100,9 @@ hipError_t run_fwd(EmbedFwd a, hipStream_t s)
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
 constexpr int kThreads = 512, kWaves = kThreads / 64;  // of the workgroups that sort, turn and fill
-constexpr int kMine = 16;                              // places of a thread that sorts
-constexpr int kChunk = kThreads * kMine;               // places that a sorting workgroup looks at at a time
-constexpr int kRange = 1024;                           // tokens of a sorting workgroup at most
+constexpr int kChunk = kWaves * 1024;                  // places that a sorting workgroup looks at at a time
+constexpr int kList = 4096;                            // of its range that it can hold
+constexpr int kRange = 512;                            // tokens of a sorting workgroup at most
 constexpr int kRun = 8;                                // sorted places of a wavefront
 constexpr int kFill = 32768;                           // floats that a workgroup fills
 
@@ -114,6 +114,7 @@ struct __align__(16) Entry {
 struct EmbedBwd {
     int B, V, C, U, N;
     Ids ids;
+    double per_item;  // 1 / U
     const int *len;
     const void *dout, *rows;  // rows [N][C]: dout turned, or dout itself
     void *turned;             // where to, or NULL
@@ -136,70 +137,126 @@ __device__ __forceinline__ int wave_scan(int v, int lane)  // sum of the lanes u
     return v;
 }
 
-// The tokens of kMine places from p0 on, -1 where there is none
-__device__ __forceinline__ void tokens_at(const EmbedBwd &a, int p0, int (&id)[kMine])
+// The tokens of 16 places of each lane of a wavefront less v0 (negative: of a lower range), kNoToken where there is none: pairs side by side,
+// place p0 + 128*i + 2*lane + s in r[2*i + s]
+constexpr int kNoToken = 0x7fffffff;
+__device__ __forceinline__ void tokens_at(const EmbedBwd &a, int p0, int lane, int v0, int (&r)[16])
 {
-    if (p0 + kMine <= a.N) {
-        if (a.ids.wide) {
-            long long w[kMine];
-            __builtin_memcpy(w, reinterpret_cast<const long long *>(a.ids.p) + p0, sizeof(w));
+    if (a.ids.wide) {
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) id[i] = w[i] < 0 || w[i] >= a.V ? -1 : (int)w[i];
-        } else {
-            __builtin_memcpy(id, reinterpret_cast<const int *>(a.ids.p) + p0, sizeof(id));
+        for (int h = 0; h < 16; h += 8) {
+            uint32_t lo[8], hi[8];
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) id[i] = id[i] < 0 || id[i] >= a.V ? -1 : id[i];
+            for (int i = 0; i < 8; i += 2) {
+                const int p = p0 + 64 * (h + i) + 2 * lane;
+                u32x4_t w = {0u, ~0u, 0u, ~0u};
+                const char *at = reinterpret_cast<const char *>(a.ids.p) + (size_t)p * 8;
+                if (p + 1 < a.N) __builtin_memcpy(&w, at, 16);
+                else if (p < a.N) __builtin_memcpy(&w, at, 8);
+                lo[i] = w[0];
+                hi[i] = w[1];
+                lo[i + 1] = w[2];
+                hi[i + 1] = w[3];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[h + i] = hi[i] == 0 && lo[i] < (uint32_t)a.V ? (int)lo[i] - v0 : kNoToken;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) id[i] = p0 + i < a.N ? a.ids.at(p0 + i, a.V) : -1;
-    }
-    if (a.len && p0 < a.N) {
-        int b = p0 / a.U, u = p0 - b * a.U, len = a.len[b];
+        for (int i = 0; i < 16; i += 2) {
+            const int p = p0 + 64 * i + 2 * lane;
+            const int *at = reinterpret_cast<const int *>(a.ids.p) + p;
+            uint32_t w[2] = {~0u, ~0u};
+            if (p + 1 < a.N) __builtin_memcpy(w, at, 8);
+            else if (p < a.N) w[0] = (uint32_t)at[0];
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            if (u >= len) id[i] = -1;
-            if (++u == a.U) {
-                u = 0;
-                b = min(b + 1, a.B - 1);
-                len = a.len[b];
-            }
+            for (int s = 0; s < 2; ++s) r[i + s] = w[s] < (uint32_t)a.V ? (int)w[s] - v0 : kNoToken;
+        }
+    }
+    if (a.len) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int p = min(p0 + 128 * (i >> 1) + 2 * lane + (i & 1), a.N - 1);
+            int b = (int)((double)p * a.per_item);  // (within one of p / U)
+            b -= b * a.U > p;
+            b += (b + 1) * a.U <= p;
+            if (p - b * a.U >= a.len[b]) r[i] = kNoToken;
         }
     }
 }
 
-// One range of tokens: which places have them, in order of the tokens and of the places.  A thread has kMine neighbouring places of a chunk;
-// those of the range are packed into a list in their order, and each wavefront picks its tokens' out of it.
+// One range of tokens: which places have them, in order of the tokens and of the places.  A wavefront looks at 1024 neighbouring places
+// at a time; those of the range are packed into a list in their order, and each wavefront picks its own tokens' out of it.  Where the list
+// is too short for all, it is made again for the next ones.
 __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
 {
-    uint32_t *list = reinterpret_cast<uint32_t *>(smem);           // [kChunk]: token in the range, place in the chunk
-    int *count = reinterpret_cast<int *>(smem + kChunk * 4);       // [kRange]
+    int *count = reinterpret_cast<int *>(smem);                    // [kRange]
     int *begin = count + kRange;                                   // [kRange]
     int *next = begin + kRange;                                    // [kRange]: where the next place goes
-    int *sums = next + kRange;                                     // [2][kWaves]
+    int *sums = next + kRange;                                     // [3][kWaves]
+    int *place = sums + 3 * kWaves;                                // [kList]
+    uint16_t *bin = reinterpret_cast<uint16_t *>(place + kList);   // [kList]
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int v0 = blockIdx.x * a.range, bins = min(a.range, a.V - v0);
+    const int v0 = blockIdx.x * a.range, bins = min(a.range, a.V - v0), chunks = (a.N - 1) / kChunk + 1;
+    const uint64_t lower = (1ull << lane) - 1;
     for (int r = t; r < bins; r += kThreads) count[r] = 0;
-    __syncthreads();
-    int less = 0, id[kMine];
-    const int chunks = (a.N + kChunk - 1) / kChunk;
-    for (int k = 0; k < chunks; ++k) {
-        tokens_at(a, k * kChunk + t * kMine, id);
+    // the range's places that are number w0 .. w0+kList-1 among them go into the list; returns how many there are in all
+    int less = 0;
+    auto pack = [&](int w0) {
+        int found = 0;
+        less = 0;
+        for (int k = 0; k < chunks; ++k) {
+            const int p0 = k * kChunk + wave * 1024;
+            int r[16], mine = 0;
+            tokens_at(a, p0, lane, v0, r);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int r = id[i] - v0;
-            less += id[i] >= 0 && r < 0;
-            if (r >= 0 && r < bins && id[i] >= 0) atomicAdd(&count[r], 1);  // (whole numbers: any order gives the same)
+            for (int i = 0; i < 16; ++i) {
+                less += __builtin_popcountll(__ballot(r[i] < 0));
+                mine += __builtin_popcountll(__ballot((unsigned)r[i] < (unsigned)bins));
+            }
+            int *s = sums + (k & 1) * kWaves;  // (the other half may still be read)
+            if (lane == 0) s[wave] = mine;
+            __syncthreads();
+            int at = found - w0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                at += w < wave ? s[w] : 0;
+                found += s[w];
+            }
+            if (mine) {  // (uniform)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const bool in0 = (unsigned)r[i] < (unsigned)bins, in1 = (unsigned)r[i + 1] < (unsigned)bins;
+                    const uint64_t b0 = __ballot(in0), b1 = __ballot(in1);
+                    if (!(b0 | b1)) continue;
+                    const int to = at + __builtin_popcountll(b0 & lower) + __builtin_popcountll(b1 & lower), p = p0 + 64 * i + 2 * lane;
+                    if (in0 && (unsigned)to < (unsigned)kList) {
+                        place[to] = p;
+                        bin[to] = (uint16_t)r[i];
+                    }
+                    if (in1 && (unsigned)(to + in0) < (unsigned)kList) {
+                        place[to + in0] = p + 1;
+                        bin[to + in0] = (uint16_t)r[i + 1];
+                    }
+                    at += __builtin_popcountll(b0) + __builtin_popcountll(b1);
+                }
+            }
         }
+        __syncthreads();
+        return found;
+    };
+    const int all = pack(0);
+    for (int w0 = 0; w0 < all; w0 += kList) {  // how often every token occurs
+        if (w0) pack(w0);
+        for (int j = t; j < min(all - w0, kList); j += kThreads) atomicAdd(&count[bin[j]], 1);  // (whole numbers: any order gives the same)
+        __syncthreads();
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) less += __shfl_xor(less, d);
-    if (lane == 0) sums[wave] = less;
+    if (lane == 0) sums[2 * kWaves + wave] = less;
     __syncthreads();
     if (wave == 0) {  // where every token's places begin
         int base = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) base += sums[w];
+        for (int w = 0; w < kWaves; ++w) base += sums[2 * kWaves + w];
         for (int r0 = 0; r0 < bins; r0 += 64) {
             const int n = r0 + lane < bins ? count[r0 + lane] : 0, upto = wave_scan(n, lane);
             if (r0 + lane < bins) begin[r0 + lane] = next[r0 + lane] = base + upto - n;
@@ -207,44 +264,27 @@ __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
         }
         if (lane == 0 && v0 + bins == a.V) *a.total = base;
     }
-    for (int k = 0; k < chunks; ++k) {
-        if (chunks > 1) tokens_at(a, k * kChunk + t * kMine, id);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) n += id[i] >= v0 && id[i] < v0 + bins;
-        const int upto = wave_scan(n, lane);
-        if (lane == 63) sums[kWaves + wave] = upto;
-        __syncthreads();  // (and `begin` is there; the list's last readers are through)
-        int at = upto - n, all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) at += sums[kWaves + w];
-            all += sums[kWaves + w];
+    __syncthreads();
+    for (int w0 = 0; w0 < all; w0 += kList) {
+        if (all > kList) {
+            __syncthreads();
+            pack(w0);
         }
-        if (n) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i)
-                if (id[i] >= v0 && id[i] < v0 + bins) list[at++] = (uint32_t)(id[i] - v0) << 16 | (uint32_t)(t * kMine + i);
-        }
-        __syncthreads();
         // A wavefront's tokens are every kWaves-th.  Of 64 listed places it finds those of one of its tokens at a time.
-        for (int j = 0; j < all; j += 64) {
-            const uint32_t e = j + lane < all ? list[j + lane] : 0xffffffffu;
-            const int r = (int)(e >> 16);
-            uint64_t open = __ballot(j + lane < all && r % kWaves == wave);
+        const int listed = min(all - w0, kList);
+        for (int j = 0; j < listed; j += 64) {
+            const bool is = j + lane < listed;
+            const int r = is ? bin[j + lane] : 0;
+            uint64_t open = __ballot(is && r % kWaves == wave);
             while (open) {
                 const int token = __builtin_amdgcn_readlane(r, __builtin_ctzll(open));
-                const uint64_t same = __ballot(j + lane < all && r == token);
+                const uint64_t same = __ballot(is && r == token);
                 const int from = begin[token], at = next[token];
-                if ((same >> lane) & 1) {
-                    const int before = __builtin_popcountll(same & ((1ull << lane) - 1));
-                    a.order[at + before] = Entry{k * kChunk + (int)(e & 0xffff), v0 + token, from, from + count[token]};
-                }
+                if ((same >> lane) & 1) a.order[at + __builtin_popcountll(same & lower)] = Entry{place[j + lane], v0 + token, from, from + count[token]};
                 if (lane == 0) next[token] = at + __builtin_popcountll(same);  // (this wavefront's alone)
                 open &= ~same;
             }
         }
-        __syncthreads();
     }
 }
 
@@ -300,10 +340,10 @@ __device__ void turn_tile(const EmbedBwd &a, int tile, unsigned char *smem)
     }
 }
 
-constexpr int kSortBytes = kChunk * 4 + 3 * kRange * 4 + 2 * kWaves * 4;
+constexpr int kSortBytes = kList * 6 + 3 * kRange * 4 + 3 * kWaves * 4;
 
 template <typename S>
-__global__ __launch_bounds__(kThreads) void embed_order_kernel(EmbedBwd a)
+__global__ __launch_bounds__(kThreads, 8) void embed_order_kernel(EmbedBwd a)
 {
     __shared__ __align__(16) unsigned char smem[kSortBytes];
     static_assert(Turn<S>::kBytes <= kSortBytes, "");
@@ -318,11 +358,15 @@ __global__ __launch_bounds__(kThreads) void embed_order_kernel(EmbedBwd a)
         return;
     }
     const size_t all = (size_t)a.V * a.C, from = (size_t)(w - a.turners) * kFill;
-    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kFill / (kThreads * 8); ++i) {
-        const size_t at = from + (i * kThreads + threadIdx.x) * 8;
-        if (at < all) store8(a.dtable + at, (int)min(all - at, (size_t)8), zero);
+    for (int i = 0; i < kFill / (kThreads * 4); ++i) {
+        const size_t at = from + (i * kThreads + threadIdx.x) * 4;
+        const u32x4_t zero = {0u, 0u, 0u, 0u};
+        if (at + 4 <= all) {
+            __builtin_memcpy(a.dtable + at, &zero, 16);
+        } else {
+            for (size_t k = at; k < all; ++k) a.dtable[k] = 0.f;
+        }
     }
 }
 
@@ -493,6 +537,7 @@ int nm_embedding_bwd(int B, int V, int C, int U, const void *dout, const void *i
     a.B = B; a.V = V; a.C = C; a.U = U; a.N = (int)places;
     a.ids = {ids, id_bytes == 8};
     a.len = lengths;
+    a.per_item = 1.0 / U;
     a.dout = dout;
     a.turned = U > 1 ? ws : nullptr;
     a.rows = U > 1 ? ws : dout;

@@ -4,10 +4,11 @@
 // lse = m + log s and entropy = log s - t/s, in powers of two throughout.  Places lie side by side in memory, so lanes are places (64 of
 // them, or fewer places times several classes); wavefronts, workgroups and spare lanes share the classes, and join what they found in pairs.
 //
-// The largest scores in order: a lane takes eight classes at a time and keeps a list of the largest of their maxima.  The K largest scores lie in
-// the eights of the K largest maxima (an eight that is not among them has K scores before all of its own), so that one insertion is
-// made for eight classes at most, and at the end the K eights are read again and put in order.  Of two sorted lists a_i and b_i of K the K
-// largest of all are the larger ones of a_i and b_(K-1-i), which are in order again after log K exchanges.
+// The largest scores in order: a lane takes 16 neighbouring classes at a time and keeps a list of the largest maxima of groups of 16 (lists of
+// up to four) or eight of them.  The K largest scores lie in the groups of the K largest maxima (a group that is not among them has K scores
+// before all of its own; of equal maxima the lower group comes first, and with it its classes), so that one insertion is made for a
+// group at most, and at the end the K groups are read again and put in order.  Of two sorted lists a_i and b_i of K the K largest
+// of all are the larger ones of a_i and b_(K-1-i), which are in order again after log K exchanges.
 //
 // Backward: element by element from the saved lse and entropy, a thread on the same eight places of every so many classes.
 #include "../../include/nm_token_scores.h"
@@ -18,7 +19,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr int kNone = 0x7fffffff;  // class of an empty place in a list: behind all others
-constexpr int kRounds = 16;  // of classes side by side that a wavefront does at least where workgroups share a place's classes
 
 struct ScoresFwd {
     int B, V, U;
@@ -29,7 +29,7 @@ struct ScoresFwd {
     int *top_ids;
     int top;
     int log_lanes;  // log2 of the places that a wavefront has side by side
-    int u_tiles, splits, per;  // classes of a wavefront
+    int u_tiles, splits, per;  // per: classes of a wavefront, a multiple of kAhead
     float *part;    // [splits][3][B*U]: m, s, t
     uint64_t *part_keys;  // [splits][K][B*U]
 };
@@ -86,6 +86,9 @@ struct Sums {
     }
     __device__ __forceinline__ void join_lane(int mask) { join(__shfl_xor(m, mask), __shfl_xor(s, mask), __shfl_xor(t, mask)); }
 };
+
+constexpr int kAhead = 16;                                       // classes that a lane takes at a time
+constexpr int group_of(int list) { return list > 4 ? 8 : 16; }  // classes that a list's entry stands for
 
 template <int K>
 struct List {  // the K largest, in order
@@ -146,7 +149,7 @@ __device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, b
 template <typename S, int K>
 __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFwd a)
 {
-    constexpr int kAhead = 16;
+    constexpr int G = group_of(K), kGroups = kAhead / G;
     __shared__ float sums[3][3][64];
     __shared__ key_t lists[K ? 3 : 1][K ? K : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -158,18 +161,19 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
     Sums st;
     List<K> list;
     if (ut * lanes < len) {  // (uniform)
-        // rows of `step` classes, kAhead of them at a time; a lane's bytes from a row's first element are of 32 bits
-        const uint32_t mine = ((uint32_t)(lane >> a.log_lanes) * (uint32_t)a.U + (uint32_t)min(u, a.U - 1)) * (uint32_t)sizeof(S);
-        const size_t row = (size_t)step * a.U;
-        auto take = [&](const float (&z)[kAhead], int c, bool whole) {  // c: this lane's first class
-            float best[kAhead / 8];
+        // A lane's classes: kAhead of c + kAhead * (its number among those with its place); bytes from there are of 32 bits.  (Places behind the
+        // item's end are worked on like others where a tile has one that counts.)
+        const int r = lane >> a.log_lanes, round = kAhead * step;
+        const uint32_t mine = ((uint32_t)(r * kAhead) * (uint32_t)a.U + (uint32_t)min(u, a.U - 1)) * (uint32_t)sizeof(S);
+        auto take = [&](const float (&z)[kAhead], int c) {  // c: this lane's first class
+            float best[kGroups];
 #pragma unroll
-            for (int h = 0; h < kAhead / 8; ++h) {
-                best[h] = z[8 * h];
+            for (int h = 0; h < kGroups; ++h) {
+                best[h] = z[G * h];
 #pragma unroll
-                for (int i = 1; i < 8; ++i) best[h] = fmaxf(best[h], z[8 * h + i]);
+                for (int i = 1; i < G; ++i) best[h] = fmaxf(best[h], z[G * h + i]);
             }
-            const float top = fmaxf(best[0], best[1]) * kLog2e;
+            const float top = fmaxf(best[0], best[kGroups - 1]) * kLog2e;
             if (top > st.m) st.rebase(top);
             const float base = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
@@ -180,41 +184,42 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
             }
             if constexpr (K > 0) {
 #pragma unroll
-                for (int h = 0; h < kAhead / 8; ++h) {
-                    const float m = best[h] == best[h] ? best[h] : -INFINITY;  // (of eight NaN)
-                    if (__any(m > score_of(list.k[K - 1]) || list.k[K - 1] == kEmpty)) {
-                        int at = kNone;  // the first class that has it; NaN count as -infinity
-#pragma unroll
-                        for (int i = 7; i >= 0; --i) {
-                            const int ci = c + (8 * h + i) * step;
-                            at = (z[8 * h + i] == m || m == -INFINITY) && (whole || ci < c1) ? ci : at;
-                        }
-                        list.insert(at == kNone ? kEmpty : key_of(m, at));
-                    }
+                for (int h = 0; h < kGroups; ++h) {
+                    const key_t k = c + G * h < c1 ? key_of(best[h], c + G * h) : kEmpty;
+                    if (__any(k > list.k[K - 1])) list.insert(k);
                 }
             }
         };
-        const S *p = (const S *)a.scores + (size_t)b * a.V * a.U + (size_t)c0 * a.U;
+        const char *p = reinterpret_cast<const char *>((const S *)a.scores + (size_t)b * a.V * a.U + (size_t)c0 * a.U);
+        const size_t row = (size_t)a.U * sizeof(S);
         int c = c0;
-        for (; c + kAhead * step <= c1; c += kAhead * step, p += kAhead * row) {
+        S ahead[kAhead];  // the next classes' are on their way while these are worked on
+        auto request = [&]() {
+            if (a.U == 1) {  // (side by side)
+                __builtin_memcpy(ahead, p + mine, sizeof(ahead));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) ahead[i] = *reinterpret_cast<const S *>(p + i * row + mine);
+            }
+            p += round * row;
+        };
+        if (c + round <= c1) request();
+        for (; c + round <= c1; c += round) {
             float z[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(reinterpret_cast<const S *>(reinterpret_cast<const char *>(p + i * row) + mine), 0);
-            if (!there) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) z[i] = -INFINITY;
-            }
-            take(z, c + (lane >> a.log_lanes), true);
+            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(ahead, i);
+            if (c + 2 * round <= c1) request();
+            take(z, c + r * kAhead);
         }
         if (c < c1) {
             const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + min(u, a.U - 1);
-            const int first = c + (lane >> a.log_lanes);
+            const int first = c + r * kAhead;
             float z[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(column, (size_t)min(first + i * step, a.V - 1) * a.U);
+            for (int i = 0; i < kAhead; ++i) z[i] = load_as_f32(column, (size_t)min(first + i, a.V - 1) * a.U);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) z[i] = there && first + i * step < c1 ? z[i] : -INFINITY;
-            take(z, first, false);
+            for (int i = 0; i < kAhead; ++i) z[i] = first + i < c1 ? z[i] : -INFINITY;
+            take(z, first);
         }
         for (int d = lanes; d < 64; d <<= 1) {
             st.join_lane(d);
@@ -284,7 +289,7 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
     if (lane == 0) lse = finish_sums<S>(a, b, u, there, st);
     if constexpr (K > 0) {
         lse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lse)));
-        constexpr int kEach = K > 8 ? 2 : 1;  // classes of a lane
+        constexpr int G = group_of(K), kAll = K * G, kEach = (kAll + 63) / 64, kAtOnce = 64 / G;  // classes of all groups, of a lane; groups of 64 lanes
         const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + u;
         key_t found[kEach];
 #pragma unroll
@@ -292,28 +297,23 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
         if (there) {  // (uniform)
             int rank = rank_of(mine, mine, a.splits * K);
             if (mine == kEmpty) rank = 64;
-            const int i = lane & 7, step = 64 >> a.log_lanes;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 int c = kNone;
 #pragma unroll
-                for (int j = 0; j < 8 && 8 * e + j < K; ++j) {  // lanes 8*j .. 8*j+7: the eight in place 8*e + j
-                    const uint64_t has = __ballot(rank == 8 * e + j);
+                for (int j = 0; j < kAtOnce && kAtOnce * e + j < K; ++j) {  // lanes G*j .. G*j+G-1: the group in place kAtOnce*e + j
+                    const uint64_t has = __ballot(rank == kAtOnce * e + j);
                     const int id = has ? class_of(of_lane(mine, __builtin_ctzll(has))) : kNone;
-                    c = lane >> 3 == j ? id : c;
+                    c = lane / G == j ? id : c;
                 }
-                if (c == kNone) continue;
-                // a wavefront has had classes from c0 on, a lane of it every step-th, eight at a time
-                const int c0 = c / a.per * a.per, round = (c - c0) / step;
-                c += (i - (round & 7)) * step;
-                if (c < min(a.V, c0 + a.per)) found[e] = key_of(load_as_f32(column, (size_t)c * a.U), c);
+                if (c != kNone && c + lane % G < a.V) found[e] = key_of(load_as_f32(column, (size_t)(c + lane % G) * a.U), c + lane % G);
             }
         }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             int rank = 0;
 #pragma unroll
-            for (int f = 0; f < kEach; ++f) rank += rank_of(found[e], found[f], (K < 8 ? K : 8) * 8);
+            for (int f = 0; f < kEach; ++f) rank += rank_of(found[e], found[f], kAll < 64 ? kAll : 64);
             if (there && found[e] != kEmpty && rank < a.top) {
                 const size_t to = ((size_t)b * a.top + rank) * a.U + u;
                 a.top_ids[to] = class_of(found[e]);
@@ -343,14 +343,15 @@ Plan plan_of(int B, int V, int U, int top)
     if (U > 32 && U % 64 > 0 && U % 64 <= 32) p.log_lanes = 5;
     const int lanes = 1 << p.log_lanes, step = 64 >> p.log_lanes, list = list_of(top);
     p.u_tiles = (U + lanes - 1) / lanes;
-    // four workgroups a CU, but a wavefront has kRounds rounds of classes to do at least, and a wavefront joins all lists of a place
+    // four workgroups a CU, but a wavefront has a whole round of classes to do, and a wavefront joins all lists of a place
     const long long groups = (long long)B * p.u_tiles;
     long long splits = 1024 / groups;
-    const long long most = V / (4LL * step * kRounds), joined = 64 / (list ? list : 1);
+    const long long most = V / (4LL * step * kAhead), joined = 64 / (list ? list : 1);
     if (splits > most) splits = most;
     if (splits > joined) splits = joined;
     if (splits < 1) splits = 1;
-    p.per = (int)((V + 4 * splits - 1) / (4 * splits));
+    const long long whole = kAhead * step, per = ((V + 4 * splits - 1) / (4 * splits) + whole - 1) / whole * whole;  // whole rounds of a wavefront
+    p.per = (int)(per < V ? per : (V + kAhead - 1) / kAhead * kAhead);
     p.splits = (int)((V + 4LL * p.per - 1) / (4LL * p.per));
     const size_t all = (size_t)B * U;
     const bool parts = p.splits > 1 || list;

@@ -16,6 +16,7 @@ constexpr float kLag = 8.f;      // powers of two that the base of the sums may 
 constexpr int kMaxSplits = 64;
 constexpr int kTile = 32;        // places that a wavefront looks at at a time
 constexpr int kWaves = 4;
+constexpr int kFewColumns = 32;  // that a workgroup reads the cache for by itself
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -346,6 +347,237 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
     }
 }
 
+
+// Many columns: four wavefronts with 32 columns each share tiles of 64 places, which go from memory through registers to LDS, the next one
+// while this one is worked on.  Blocks of 32 x 32; bfloat16 alone.  Rows in LDS are 16 bytes longer than their contents, so that 16 lanes that
+// read 16 rows meet every bank once.
+constexpr int kManyTile = 64, kManyColumns = 128;
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+template <int DB>
+struct ManyLds {
+    static constexpr int kPitchK = DB * 32 + 16, kPitchV = kManyTile * 2 + 16, kRowsV = (DB + 1) / 2 * 32;
+    static constexpr int kBuffer = kManyTile * kPitchK + kRowsV * kPitchV, kBytes = 2 * kBuffer;
+};
+
+template <int DB>
+__global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
+{
+    typedef ManyLds<DB> L;
+    typedef bf16x8_t Frag;
+    constexpr int D = DB * 16, ND = (DB + 1) / 2, kGran = D / 8, kLoads = (kManyTile * kGran + 255) / 256, kAll = kManyTile * kGran;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i32 = lane & 31;
+    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
+    const int ct = rest % a.col_tiles, split = rest / a.col_tiles, b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const int n_new = length_in(a.q_len, b, a.U), len = max(a.len[b], 0);
+    const Column col = column_of(a, b, ct * kManyColumns + wave * 32 + i32, n_new, len);
+    int first = col.there ? col.lo : 0x7fffffff, last = col.there ? col.hi : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        first = min(first, __shfl_xor(first, d));
+        last = max(last, __shfl_xor(last, d));
+    }
+    const int wave_first = __builtin_amdgcn_readfirstlane(first), wave_last = __builtin_amdgcn_readfirstlane(last);
+    int *range = reinterpret_cast<int *>(smem);
+    if (lane == 0) {
+        range[wave] = wave_first;
+        range[4 + wave] = wave_last;
+    }
+    __syncthreads();
+    first = min(min(range[0], range[1]), min(range[2], range[3]));
+    last = max(max(range[4], range[5]), max(range[6], range[7]));
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    __syncthreads();
+    const int t_first = last ? first / kManyTile : 0, t_last = (last + kManyTile - 1) / kManyTile, share = (t_last - t_first + a.splits - 1) / a.splits;
+    const int t_begin = t_first + split * share, t_end = min(t_last, t_begin + share);
+
+    const int size = 1 << a.log_page;
+    const int *table = a.table + (size_t)b * a.max_pages;
+    const bf16_t *kbase = (const bf16_t *)a.k + (size_t)kvh * size * D, *vbase = (const bf16_t *)a.v + (size_t)kvh * size * D;
+    const size_t page_stride = (size_t)a.Hkv * size * D;
+    auto there = [&](int pg) { return (unsigned)pg < (unsigned)a.pages; };
+    // the pages of a tile's four groups of 16 places
+    struct Pages {
+        int p0, p1, p2, p3;
+        __device__ __forceinline__ int of(int j) const { return j < 2 ? (j == 0 ? p0 : p1) : (j == 2 ? p2 : p3); }
+    };
+    auto page_at = [&](int place) { return table[min(place >> a.log_page, a.max_pages - 1)]; };
+    auto pages_of = [&](int t) {
+        const int p = t * kManyTile;
+        return Pages{page_at(p), page_at(p + 16), page_at(p + 32), page_at(p + 48)};
+    };
+    auto all_there = [&](const Pages &p) { return there(p.p0) && there(p.p1) && there(p.p2) && there(p.p3); };
+    Pages pg = {}, next_pg = {};
+    u32x4_t kr[kLoads], vr[kLoads];
+    const int vg = tid & 7;  // the thread's group of eight places of the values' rows
+    auto load = [&](int t, const Pages &p) {
+        const Pages q = {there(p.p0) ? p.p0 : 0, there(p.p1) ? p.p1 : 0, there(p.p2) ? p.p2 : 0, there(p.p3) ? p.p3 : 0};
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int e = min(i * 256 + tid, kAll - 1), row = e / kGran, g = e - row * kGran;
+            const int page = q.of(row >> 4);
+            kr[i] = *reinterpret_cast<const u32x4_t *>(kbase + page * page_stride + (size_t)((t * kManyTile + row) & (size - 1)) * D + g * 8);
+        }
+        const int page = q.of(vg >> 1);
+        const bf16_t *v = vbase + page * page_stride + ((t * kManyTile + 8 * vg) & (size - 1));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) vr[i] = *reinterpret_cast<const u32x4_t *>(v + (size_t)min(i * 32 + (tid >> 3), D - 1) * size);
+    };
+    auto write = [&](unsigned char *buf, int t, const Pages &p) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int e = i * 256 + tid, row = e / kGran, g = e - row * kGran;
+            if (kAll % 256 == 0 || e < kAll) *reinterpret_cast<u32x4_t *>(buf + row * L::kPitchK + g * 16) = kr[i];
+        }
+        const int t0 = t * kManyTile, pos = t0 + 8 * vg;
+        if (t0 < first || t0 + kManyTile > last || !all_there(p)) {  // (uniform) values that no token looks at
+            const bool exists = there(p.of(vg >> 1));
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                bf16_t e[8];
+                __builtin_memcpy(e, &vr[i], 16);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = exists && pos + j >= first && pos + j < last ? e[j] : (bf16_t)0;
+                __builtin_memcpy(&vr[i], e, 16);
+            }
+        }
+        unsigned char *v = buf + kManyTile * L::kPitchK + vg * 16;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = i * 32 + (tid >> 3);
+            if (D % 32 == 0 || row < D) *reinterpret_cast<u32x4_t *>(v + row * L::kPitchV) = vr[i];
+        }
+    };
+
+    if (t_begin < t_end) {
+        pg = pages_of(t_begin);
+        load(t_begin, pg);
+    }
+    Frag q[DB];
+    {
+        const bf16_t *p = (const bf16_t *)a.q + (size_t)b * a.qs + (size_t)(kvh * a.G + col.g) * D * a.U + col.u;
+#pragma unroll
+        for (int s = 0; s < DB; ++s) {
+            bf16_t e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                e[j] = p[(size_t)(16 * s + 8 * half + j) * a.U];
+                if (!col.there) e[j] = 0;
+            }
+            __builtin_memcpy(&q[s], e, 16);
+        }
+    }
+    float mx = -INFINITY, sum = 0.f;
+    f32x16_t acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    // places are dealt to the rows of the scores such that a lane's register r is place 16*(r/8) + 8*half + r%8 of a block
+    const int k_row = (i32 & 16) | (i32 & 4) << 1 | (i32 & 8) >> 1 | (i32 & 3);
+
+    auto compute = [&](const unsigned char *buf, int t0, bool whole) {
+        const unsigned char *kp = buf + k_row * L::kPitchK + half * 16, *vp = buf + kManyTile * L::kPitchK + i32 * L::kPitchV + half * 16;
+        f32x16_t s[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+        for (int st = 0; st < DB; ++st)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+                s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const Frag *>(kp + n * 32 * L::kPitchK + st * 32), q[st], s[n], 0, 0, 0);
+        float z[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) z[j] = s[j >> 4][j & 15] * a.c;
+        if (!__all(whole && (!col.there || (col.lo <= t0 && t0 + kManyTile <= col.hi)))) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const int pos = t0 + 32 * (j >> 4) + 16 * ((j >> 3) & 1) + 8 * half + (j & 7);
+                const bool seen = (pos >= col.lo) & (pos < col.hi) & there(pg.of(j >> 3));
+                z[j] = seen ? z[j] : -INFINITY;
+            }
+        }
+        float top = z[0];
+#pragma unroll
+        for (int j = 1; j < 32; ++j) top = fmaxf(top, z[j]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > mx + kLag)) {
+            top = fmaxf(top, mx);
+            const float shrink = __builtin_amdgcn_exp2f(mx - (top == -INFINITY ? 0.f : top));
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[d] *= shrink;
+            mx = top;
+        }
+        const float base = mx == -INFINITY ? 0.f : mx;
+        Frag p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float e[8], part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(z[8 * k + j] - base);
+                part += e[j];
+            }
+            sum += part;
+            const u32x4_t w = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+            p[k] = __builtin_bit_cast(Frag, w);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const Frag *>(vp + d * 32 * L::kPitchV + k * 32), p[k], acc[d], 0, 0, 0);
+    };
+    for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
+        unsigned char *buf = smem + turn * L::kBuffer;
+        write(buf, t, pg);
+        const bool more = t + 1 < t_end;
+        if (more) next_pg = pages_of(t + 1);
+        __syncthreads();  // (the other buffer is written next: all are through with it before they pass here again)
+        if (more) load(t + 1, next_pg);
+        const int t0 = t * kManyTile;
+        if (t0 < wave_last && t0 + kManyTile > wave_first) compute(buf, t0, all_there(pg));
+        pg = next_pg;
+    }
+    float total = sum;
+    total += __shfl_xor(total, 32);
+    if (!col.exists) return;
+    const int head = kvh * a.G + col.g;
+    const size_t rows = (size_t)a.B * a.H * a.U, row = ((size_t)b * a.H + head) * a.U + col.u;
+    const bool some = col.there && total != 0.f;
+    if (half == 0) {
+        if (a.splits > 1) {
+            float *ml = a.part_ml + ((size_t)split * rows + row) * 2;
+            ml[0] = some ? mx : -INFINITY;
+            ml[1] = some ? total : 0.f;
+        } else if (a.lse) {
+            a.lse[row] = some ? (mx + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+        }
+    }
+    const float inv = some ? (a.splits > 1 ? 1.f : 1.f / total) : 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int ch = 32 * d + 2 * r + 4 * half;
+            if (D % 32 && ch >= D) continue;
+            f32x4_t v = {acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]};
+            if (!some) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (a.splits > 1) {
+                *reinterpret_cast<f32x4_t *>(a.part + ((size_t)split * rows + row) * D + ch) = v;
+            } else {
+                bf16_t *o = (bf16_t *)a.out + (size_t)b * a.os + ((size_t)head * D + ch) * a.U + col.u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) store_from_f32(o, (size_t)j * a.U, v[j] * inv);
+            }
+        }
+}
+
 // Joins the sums of `splits` workgroups in order: a wavefront takes a row (a token of a head), a lane one split's maximum and sum, and then
 // eight channels of every fourth split.  (One thread for a row's maxima, split after split, took 17 us for 512 rows of 16 splits.)
 template <typename S, int ROWS>
@@ -406,17 +638,21 @@ __global__ __launch_bounds__(ROWS * 64) void paged_join_kernel(Paged a)
 }
 
 struct Plan {
-    int blocks, col_tiles, splits;  // blocks: of 16 columns of a workgroup
+    bool many;
+    int blocks, col_tiles, splits;  // blocks: of 16 columns of a workgroup with few of them
     size_t part_bytes, ml_bytes;
 };
-Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, int)
+Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, int dtype)
 {
     Plan p = {};
-    const long long columns = (long long)(H / Hkv) * U;
+    const long long columns = (long long)(H / Hkv) * U, room = (long long)max_pages * page_size;
+    p.many = dtype == NM_BF16 && columns > kFewColumns;
     p.blocks = columns > 16 ? 2 : 1;
-    p.col_tiles = (int)((columns + 16 * p.blocks - 1) / (16 * p.blocks));
-    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = ((long long)max_pages * page_size + kTile * kWaves - 1) / (kTile * kWaves);
-    long long splits = (1024 + groups - 1) / groups;
+    const int of_group = p.many ? kManyColumns : 16 * p.blocks, of_round = p.many ? kManyTile : kTile * kWaves;
+    p.col_tiles = (int)((columns + of_group - 1) / of_group);
+    // workgroups share a token's places where there are fewer than two (four) a CU, but look at two rounds of places at least
+    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = p.many ? 512 : 1024;
+    long long splits = p.many ? wanted / groups : (wanted + groups - 1) / groups;
     if (splits > rounds / 2) splits = rounds / 2;
     if (splits > kMaxSplits) splits = kMaxSplits;
     p.splits = splits < 1 ? 1 : (int)splits;
@@ -424,6 +660,17 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, 
     p.part_bytes = p.splits > 1 ? align_up(p.splits * rows * D * 4, 256) : 0;
     p.ml_bytes = p.splits > 1 ? align_up(p.splits * rows * 2 * 4, 256) : 0;
     return p;
+}
+
+template <int DB>
+hipError_t run_many(const Paged &a, hipStream_t s)
+{
+    static LdsOptIn opt;
+    auto *fn = paged_many_kernel<DB>;
+    const hipError_t e = ensure_dynamic_lds(opt, (const void *)fn, ManyLds<DB>::kBytes);
+    if (e != hipSuccess) return e;
+    fn<<<dim3((unsigned)(a.B * a.Hkv) * a.col_tiles * a.splits), dim3(256), ManyLds<DB>::kBytes, s>>>(a);
+    return hipGetLastError();
 }
 
 template <typename S, int DB, int NC>
@@ -438,23 +685,26 @@ hipError_t run_few(const Paged &a, hipStream_t s)
     return hipGetLastError();
 }
 template <typename S, int DB>
-hipError_t run_blocks(const Paged &a, int blocks, hipStream_t s)
+hipError_t run_blocks(const Paged &a, const Plan &p, hipStream_t s)
 {
-    return blocks == 1 ? run_few<S, DB, 1>(a, s) : run_few<S, DB, 2>(a, s);
+    if constexpr (sizeof(S) == 2) {
+        if (p.many) return run_many<DB>(a, s);
+    }
+    return p.blocks == 1 ? run_few<S, DB, 1>(a, s) : run_few<S, DB, 2>(a, s);
 }
 template <typename S>
-hipError_t run(const Paged &a, int blocks, hipStream_t s)
+hipError_t run(const Paged &a, const Plan &p, hipStream_t s)
 {
     hipError_t e;
     switch (a.D / 16) {
-    case 1: e = run_blocks<S, 1>(a, blocks, s); break;
-    case 2: e = run_blocks<S, 2>(a, blocks, s); break;
-    case 3: e = run_blocks<S, 3>(a, blocks, s); break;
-    case 4: e = run_blocks<S, 4>(a, blocks, s); break;
-    case 5: e = run_blocks<S, 5>(a, blocks, s); break;
-    case 6: e = run_blocks<S, 6>(a, blocks, s); break;
-    case 7: e = run_blocks<S, 7>(a, blocks, s); break;
-    default: e = run_blocks<S, 8>(a, blocks, s); break;
+    case 1: e = run_blocks<S, 1>(a, p, s); break;
+    case 2: e = run_blocks<S, 2>(a, p, s); break;
+    case 3: e = run_blocks<S, 3>(a, p, s); break;
+    case 4: e = run_blocks<S, 4>(a, p, s); break;
+    case 5: e = run_blocks<S, 5>(a, p, s); break;
+    case 6: e = run_blocks<S, 6>(a, p, s); break;
+    case 7: e = run_blocks<S, 7>(a, p, s); break;
+    default: e = run_blocks<S, 8>(a, p, s); break;
     }
     if (e != hipSuccess || a.splits == 1) return e;
     const size_t rows = (size_t)a.B * a.H * a.U;
@@ -470,7 +720,7 @@ int check(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, int
     if (D % 16 || D > 128 || page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return NM_ERR_UNSUPPORTED;
     if ((long long)max_pages * page_size > most - 512 || (long long)B * max_pages > most) return NM_ERR_UNSUPPORTED;
     if ((long long)H * D > most / U || (long long)B * H > most / 2 / U) return NM_ERR_UNSUPPORTED;
-    // the grid, of 256 work items for 16 or 32 columns and a split: below 2^32 (from 2^10 workgroups on nothing is split)
+    // the grid, of 256 work items for 16 columns or more and a split: below 2^32 (from 2^10 workgroups on nothing is split)
     if ((long long)B * Hkv >= 1LL << 23 || (long long)B * Hkv * (((long long)H / Hkv * U + 15) / 16) >= 1LL << 23) return NM_ERR_UNSUPPORTED;
     return NM_OK;
 }
@@ -522,7 +772,7 @@ int nm_paged_attn_fwd(int B, int heads, int kv_heads, int D, int U, const void *
     a.part_ml = (float *)((char *)workspace + p.part_bytes);
     a.col_tiles = p.col_tiles; a.splits = p.splits;
     hipStream_t s = (hipStream_t)hip_stream;
-    return status_of(dtype == NM_BF16 ? run<bf16_t>(a, p.blocks, s) : run<float>(a, p.blocks, s));
+    return status_of(dtype == NM_BF16 ? run<bf16_t>(a, p, s) : run<float>(a, p, s));
 }
 
 }  // extern "C"

@@ -29,7 +29,8 @@
  *    a cache at 0).  x and dout are not used at tokens behind an item's end, whatever they hold; out, dx and the returned queries are 0 there.
  *  - a token whose place in the cache does not exist (before 0, behind max_pages * page_size, on a page outside [0, pages)) is not
  *    written.  No two tokens of a call may have the same place.  Everything else in the cache stays as it was.
- *  - D is even and at most 128; rot is even and at most D.  A tensor spans fewer than 2^40 elements, an item of it fewer than 2^31.
+ *  - D is even and at most 128; rot is even and at most D.  A tensor spans fewer than 2^40 elements, an item of it fewer than 2^31, a
+ *    head of an item less than 4 GiB.
  *  - without an eps the norm of a head of zeros is NaN.
  */
 #ifndef NM_HEAD_NORM_H

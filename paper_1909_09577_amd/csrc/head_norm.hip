@@ -1,9 +1,9 @@
 // Norms of queries and keys for each head and their rotation by position (definition: include/nm_head_norm.h).
 //
 // Work goes by units of two channels: the pairs that turn together, then the channels that do not turn, two by two.  Two divisions:
-//   tiles  a wavefront owns 32 tokens of a head, a lane eight neighbouring tokens of every 16th unit, so that the sums over a head's
-//          channels are a few values of a lane and four exchanges, and every tensor is read and written once, in 64-byte pieces.  The
-//          angles of a tile's tokens are made once for all heads that the workgroup takes, in LDS.  The last tile of a row begins 32
+//   tiles  one to four wavefronts own 32 tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
+//          channels are eight values of a lane, four exchanges and LDS, and every tensor is read and written once, in 64-byte pieces.  The
+//          angles of a tile's tokens are made once for all heads that the workgroup takes.  The last tile of a row begins 32
 //          tokens before its end; what two tiles share is made twice, alike.
 //   single a wavefront owns one token of a head, a lane a unit: rows of fewer than eight tokens, and everything that goes into the cache.
 // An angle is position * freqs[i] as a part of a turn in double, of which only the fraction goes on in float: 500000 tokens into a
@@ -55,189 +55,203 @@ __device__ __forceinline__ float2 turn(int position, double freq)
     return cs;
 }
 
-template <typename S, int P, bool BACK>
-__global__ __launch_bounds__(256) void heads_tile_kernel(Heads a)
+// Eight tokens of a channel as they lie in memory
+template <typename S>
+struct Eight;
+template <>
+struct Eight<bf16_t> {
+    u32x4_t r;
+    __device__ __forceinline__ void load(const bf16_t *head, uint32_t at) { __builtin_memcpy(&r, reinterpret_cast<const char *>(head) + at, 16); }
+    __device__ __forceinline__ float at(int e) const { return __uint_as_float(e & 1 ? r[e >> 1] & 0xffff0000u : r[e >> 1] << 16); }
+};
+template <>
+struct Eight<float> {
+    float r[8];
+    __device__ __forceinline__ void load(const float *head, uint32_t at) { __builtin_memcpy(r, reinterpret_cast<const char *>(head) + at, 32); }
+    __device__ __forceinline__ float at(int e) const { return r[e]; }
+};
+
+constexpr int kAnglePitch = kTile + 2;  // (rows that begin at other banks)
+
+// PER wavefronts take a head, 16 units each: with all channels of a head in one wavefront, a lane's registers would be too many for more than one
+// or two wavefronts a SIMD.
+template <int PER>
+struct TileForm {
+    static constexpr int kHeads = 4 / PER, kWaves = kHeads * PER, kThreads = kWaves * 64;  // heads side by side
+};
+
+template <typename S, int PER, bool BACK>
+__global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Heads a)
 {
-    extern __shared__ __align__(16) float2 angles[];  // [rot/2][kTile]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane & 3, cl = lane >> 2;
-    const int chunk = blockIdx.y, half = a.rot >> 1, units = a.D >> 1;
-    const bool keys = chunk >= a.q_chunks;
-    const int h_end = keys ? a.H + a.Hkv : a.H, h0 = keys ? a.H + (chunk - a.q_chunks) * a.heads_each : chunk * a.heads_each;
+    typedef TileForm<PER> F;
+    typedef Eight<S> E;
+    extern __shared__ __align__(16) float2 angles[];  // [D/2][kAnglePitch]
+    __shared__ float sums[2][F::kWaves][kTile];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane & 3;
+    const int slot = wave / PER, unit = wave % PER * 16 + (lane >> 2), units = a.D >> 1, half = a.rot >> 1;
+    const bool is = unit < units, keys = blockIdx.y >= a.q_chunks;
+    const int h_begin = keys ? a.H + (blockIdx.y - a.q_chunks) * a.heads_each : blockIdx.y * a.heads_each;
+    const int h_end = min(h_begin + a.heads_each, keys ? a.H + a.Hkv : a.H);
+    int i0, i1;
+    channels_of(a, min(unit, units - 1), i0, i1);
     const float *weight = a.norm ? (keys ? a.kw : a.qw) : nullptr;
-    float w0[P], w1[P], dw0[P], dw1[P];
+    const float w0 = weight ? weight[i0] : 1.f, w1 = weight ? weight[i1] : 1.f, per_d = 1.f / (float)a.D;
+    const uint32_t c0 = (uint32_t)i0 * (uint32_t)a.U * (uint32_t)sizeof(S), c1 = (uint32_t)i1 * (uint32_t)a.U * (uint32_t)sizeof(S);  // bytes in a head
+    float dw0 = 0.f, dw1 = 0.f;
+    // sums over a head's channels, for the lane's eight tokens, in order
+    auto over_head = [&](float (&v)[8], int buffer) {
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const int j = min(cl + 16 * k, units - 1);
-        int c0, c1;
-        channels_of(a, j, c0, c1);
-        w0[k] = weight ? weight[c0] : 1.f;
-        w1[k] = weight ? weight[c1] : 1.f;
-        dw0[k] = dw1[k] = 0.f;
-    }
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int d = 4; d < 64; d <<= 1) v[e] += __shfl_xor(v[e], d);
+        if constexpr (PER > 1) {
+            if (lane < 4) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sums[buffer][wave][8 * lane + e] = v[e];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = sums[buffer][slot * PER][8 * g + e];
+#pragma unroll
+                for (int w = 1; w < PER; ++w) v[e] += sums[buffer][slot * PER + w][8 * g + e];
+            }
+        }
+    };
     for (int tile = blockIdx.x; tile < a.B * a.u_tiles; tile += gridDim.x) {
         const int b = tile / a.u_tiles, u0 = (tile - b * a.u_tiles) * kTile, ub = max(0, min(u0, a.U - kTile));
         const int len = length_in(a.len, b, a.U);
-        if (a.rot && ub < len) {
+        const bool active = is && ub + 8 * g < a.U, some = ub < len;                // (rows of fewer than 32 tokens)
+        const int t = min(ub + 8 * g, a.U - 8), first = a.U < kTile ? 8 * g : u0;  // tokens before `first` are another lane's too
+        const uint32_t at0 = c0 + (uint32_t)t * (uint32_t)sizeof(S), at1 = c1 + (uint32_t)t * (uint32_t)sizeof(S);
+        const size_t head = (size_t)a.D * a.U;
+        E x0, x1, d0, d1;
+        auto load = [&](int h) {
+            const int from = min(h, h_end - 1);
+            if (!BACK || a.norm) {
+                const S *x = (const S *)a.x + (size_t)b * a.xs + from * head;
+                x0.load(x, at0);
+                x1.load(x, at1);
+            }
+            if constexpr (BACK) {
+                const S *d = (const S *)a.dout + (size_t)b * a.ds + from * head;
+                d0.load(d, at0);
+                d1.load(d, at1);
+            }
+        };
+        if (some) load(h_begin + slot);  // (on its way while the angles are made)
+        if (a.rot && some) {  // (units that do not turn have the angle 0: a branch for them would cost more)
             __syncthreads();  // (the tile before is through with them)
-            for (int i = threadIdx.x; i < half * kTile; i += 256) {
-                const int p = ub + (i & (kTile - 1));
-                angles[i] = turn(a.positions ? a.positions[(size_t)b * a.U + min(p, a.U - 1)] : p, a.freqs[i / kTile]);
+            for (int i = threadIdx.x; i < units * kTile; i += F::kThreads) {
+                const int p = ub + (i & (kTile - 1)), row = i / kTile;
+                float2 cs = {1.f, 0.f};
+                if (row < half) cs = turn(a.positions ? a.positions[(size_t)b * a.U + min(p, a.U - 1)] : p, a.freqs[row]);
+                angles[row * kAnglePitch + (i & (kTile - 1))] = cs;
             }
             __syncthreads();
         }
-        if (ub + 8 * g >= a.U) continue;  // (rows of fewer than 32 tokens)
-        const int t = min(ub + 8 * g, a.U - 8), first = a.U < kTile ? 8 * g : u0;  // tokens before `first` are another lane's too
-        for (int h = h0 + wave; h < min(h0 + a.heads_each, h_end); h += 4) {
-            const S *x = (const S *)a.x + (size_t)b * a.xs + (size_t)h * a.D * a.U + t;
-            S *out = (S *)a.out + (size_t)b * a.os + (size_t)h * a.D * a.U + t;
-            float x0[P][8], x1[P][8], d0[P][8], d1[P][8];
-            if (ub >= len) {  // (uniform)
-                const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        float2 cs[8];
+        if (a.rot && some) {
 #pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const int j = cl + 16 * k;
-                    if (j >= units) continue;
-                    store8(out + (size_t)(2 * j) * a.U, 8, zero);
-                    store8(out + (size_t)(2 * j + 1) * a.U, 8, zero);
-                }
-                continue;
-            }
+            for (int e = 0; e < 8; ++e) cs[e] = angles[min(unit, units - 1) * kAnglePitch + (t - ub) + e];
+        }
+        for (int hh = h_begin, turn_of = 0; hh < h_end; hh += F::kHeads, turn_of ^= 1) {
+            const int h = hh + slot;
+            const bool stores = active && h < h_end;
+            char *out = reinterpret_cast<char *>((S *)a.out + (size_t)b * a.os + min(h, h_end - 1) * head);
+            float y0[8], y1[8];
+            if (!some) {  // (uniform)
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int j = min(cl + 16 * k, units - 1);
-                int c0, c1;
-                channels_of(a, j, c0, c1);
-                if (!BACK || a.norm) {
-                    load8(x + (size_t)c0 * a.U, 8, x0[k]);
-                    load8(x + (size_t)c1 * a.U, 8, x1[k]);
-                }
-                if constexpr (BACK) {
-                    const S *d = (const S *)a.dout + (size_t)b * a.ds + (size_t)h * a.D * a.U + t;
-                    load8(d + (size_t)c0 * a.U, 8, d0[k]);
-                    load8(d + (size_t)c1 * a.U, 8, d1[k]);
-                }
-            }
-            float r[8];
-            if (a.norm) {
+                for (int e = 0; e < 8; ++e) y0[e] = y1[e] = 0.f;
+            } else {
+                float r[8], v0[8], v1[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float s = 0.f;
-#pragma unroll
-                    for (int k = 0; k < P; ++k)
-                        if (cl + 16 * k < units) s += x0[k][e] * x0[k][e] + x1[k][e] * x1[k][e];
-#pragma unroll
-                    for (int d = 4; d < 64; d <<= 1) s += __shfl_xor(s, d);
-                    r[e] = rsqrtf(s / (float)a.D + a.eps);
+                    v0[e] = (!BACK || a.norm) ? x0.at(e) : 0.f;
+                    v1[e] = (!BACK || a.norm) ? x1.at(e) : 0.f;
+                    y0[e] = BACK ? d0.at(e) : 0.f;
+                    y1[e] = BACK ? d1.at(e) : 0.f;
                 }
-            }
-            auto angle = [&](int k, int e) { return angles[(size_t)(cl + 16 * k) * kTile + (t - ub) + e]; };
-            if constexpr (!BACK) {
+                if (hh + F::kHeads < h_end) load(h + F::kHeads);
+                if (a.norm) {
 #pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const int j = cl + 16 * k;
-                    if (j >= units) continue;
-                    int c0, c1;
-                    channels_of(a, j, c0, c1);
-                    float y0[8], y1[8];
+                    for (int e = 0; e < 8; ++e) r[e] = is ? v0[e] * v0[e] + v1[e] * v1[e] : 0.f;
+                    over_head(r, BACK ? 0 : turn_of);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        y0[e] = a.norm ? x0[k][e] * r[e] * w0[k] : x0[k][e];
-                        y1[e] = a.norm ? x1[k][e] * r[e] * w1[k] : x1[k][e];
+                        r[e] = rsqrtf(r[e] * per_d + a.eps);
+                        v0[e] *= r[e];
+                        v1[e] *= r[e];
                     }
-                    if (j < half) {
+                }
+                if constexpr (!BACK) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float n0 = v0[e] * w0, n1 = v1[e] * w1;
+                        y0[e] = a.rot ? n0 * cs[e].x - n1 * cs[e].y : n0;
+                        y1[e] = a.rot ? n1 * cs[e].x + n0 * cs[e].y : n1;
+                    }
+                } else {
+                    if (a.rot) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const float2 cs = angle(k, e);
                             const float v = y0[e];
-                            y0[e] = v * cs.x - y1[e] * cs.y;
-                            y1[e] = y1[e] * cs.x + v * cs.y;
+                            y0[e] = v * cs[e].x + y1[e] * cs[e].y;
+                            y1[e] = y1[e] * cs[e].x - v * cs[e].y;
                         }
                     }
+                    if (a.norm) {
+                        float m[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float p0 = y0[e] * v0[e], p1 = y1[e] * v1[e];
+                            const bool mine = stores && t + e >= first && t + e < len;
+                            dw0 += mine ? p0 : 0.f;
+                            dw1 += mine ? p1 : 0.f;
+                            m[e] = is ? w0 * p0 + w1 * p1 : 0.f;
+                        }
+                        over_head(m, 1);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float mean = m[e] * per_d;
+                            y0[e] = r[e] * (w0 * y0[e] - v0[e] * mean);
+                            y1[e] = r[e] * (w1 * y1[e] - v1[e] * mean);
+                        }
+                    }
+                }
+                if (t + 8 > len) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         y0[e] = t + e < len ? y0[e] : 0.f;
                         y1[e] = t + e < len ? y1[e] : 0.f;
                     }
-                    store8(out + (size_t)c0 * a.U, 8, y0);
-                    store8(out + (size_t)c1 * a.U, 8, y1);
                 }
-            } else {
-                float m[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m[e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const int j = cl + 16 * k;
-                    if (j < half) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float2 cs = angle(k, e);
-                            const float v = d0[k][e];
-                            d0[k][e] = v * cs.x + d1[k][e] * cs.y;
-                            d1[k][e] = d1[k][e] * cs.x - v * cs.y;
-                        }
-                    }
-                    if (!a.norm || j >= units) continue;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        x0[k][e] *= r[e];
-                        x1[k][e] *= r[e];
-                        const float p0 = d0[k][e] * x0[k][e], p1 = d1[k][e] * x1[k][e];
-                        const bool mine = t + e >= first && t + e < len;
-                        dw0[k] += mine ? p0 : 0.f;
-                        dw1[k] += mine ? p1 : 0.f;
-                        m[e] += w0[k] * p0 + w1[k] * p1;
-                    }
-                }
-                if (a.norm) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-#pragma unroll
-                        for (int d = 4; d < 64; d <<= 1) m[e] += __shfl_xor(m[e], d);
-                        m[e] /= (float)a.D;
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const int j = cl + 16 * k;
-                    if (j >= units) continue;
-                    int c0, c1;
-                    channels_of(a, j, c0, c1);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (a.norm) {
-                            d0[k][e] = r[e] * (w0[k] * d0[k][e] - x0[k][e] * m[e]);
-                            d1[k][e] = r[e] * (w1[k] * d1[k][e] - x1[k][e] * m[e]);
-                        }
-                        d0[k][e] = t + e < len ? d0[k][e] : 0.f;
-                        d1[k][e] = t + e < len ? d1[k][e] : 0.f;
-                    }
-                    store8(out + (size_t)c0 * a.U, 8, d0[k]);
-                    store8(out + (size_t)c1 * a.U, 8, d1[k]);
-                }
+            }
+            if (stores) {
+                store8(reinterpret_cast<S *>(out + at0), 8, y0);
+                store8(reinterpret_cast<S *>(out + at1), 8, y1);
             }
         }
     }
     if constexpr (BACK) {
         if (!a.part) return;  // (uniform)
-        __shared__ float sums[4][kMaxD];
+        __shared__ float all[F::kHeads][kMaxD];
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                dw0[k] += __shfl_xor(dw0[k], d);
-                dw1[k] += __shfl_xor(dw1[k], d);
-            }
-            const int j = cl + 16 * k;
-            if (g || j >= units) continue;
-            int c0, c1;
-            channels_of(a, j, c0, c1);
-            sums[wave][c0] = dw0[k];
-            sums[wave][c1] = dw1[k];
+        for (int d = 1; d < 4; d <<= 1) {
+            dw0 += __shfl_xor(dw0, d);
+            dw1 += __shfl_xor(dw1, d);
+        }
+        if (g == 0 && is) {
+            all[slot][i0] = dw0;
+            all[slot][i1] = dw1;
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < a.D; c += 256)
-            a.part[((size_t)chunk * gridDim.x + blockIdx.x) * a.D + c] = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
+        for (int c = threadIdx.x; c < a.D; c += F::kThreads) {
+            float s = all[0][c];
+#pragma unroll
+            for (int i = 1; i < F::kHeads; ++i) s += all[i][c];
+            a.part[((size_t)blockIdx.y * gridDim.x + blockIdx.x) * a.D + c] = s;
+        }
     }
 }
 
@@ -389,10 +403,11 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
     return p;
 }
 
-template <typename S, int P, bool BACK>
+template <typename S, int PER, bool BACK>
 hipError_t run_tile(const Heads &a, const Plan &p, hipStream_t s)
 {
-    heads_tile_kernel<S, P, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(256), (size_t)(a.rot / 2) * kTile * sizeof(float2), s>>>(a);
+    heads_tile_kernel<S, PER, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(TileForm<PER>::kThreads),
+                                      (size_t)(a.rot ? a.D / 2 : 0) * kAnglePitch * sizeof(float2), s>>>(a);
     return hipGetLastError();
 }
 template <typename S, bool BACK>
@@ -423,7 +438,7 @@ int check(int B, int H, int Hkv, int D, int U, const void *q_weight, const void 
         return NM_ERR_BAD_ARG;
     if (D % 2 || D > kMaxD) return NM_ERR_UNSUPPORTED;
     const long long most = (1LL << 31) - 1, heads = (long long)H + 2LL * Hkv;
-    if (heads > most / D || heads * D > most / U) return NM_ERR_UNSUPPORTED;
+    if (heads > most / D || heads * D > most / U || (long long)D * (long long)element(dtype) > ((1LL << 32) - 1) / U) return NM_ERR_UNSUPPORTED;  // (a head's rows: below 4 GiB)
     // the grids: below 2^32 work items, of 64 for a token of a head or 256 for a tile of four heads; no more than 2^16 chunks of heads
     if ((long long)B * U > most / 2 || heads > 1 << 16 || (U < 8 ? (long long)B * U * heads >= 1LL << 25 : (long long)B * ((U + 31) / 32) * (heads / 4 + 2) >= 1LL << 23))
         return NM_ERR_UNSUPPORTED;

@@ -28,7 +28,8 @@ struct Paged {
     int pages, log_page, max_pages;
     const int *table, *len, *q_len;
     int window;
-    float c;  // scale * log2(e)
+    float c;  // |scale| * log2(e)
+    uint32_t flip;  // sign bit of the scale, for the tokens' channels
     void *out;
     float *lse, *part, *part_ml;  // [splits][B*H*U][D], [splits][B*H*U][2]
     int col_tiles, splits;
@@ -60,6 +61,9 @@ struct Mma<float> {
     }
 };
 
+__device__ __forceinline__ bf16_t flipped(bf16_t v, uint32_t flip) { return (bf16_t)(v ^ (flip >> 16)); }
+__device__ __forceinline__ float flipped(float v, uint32_t flip) { return __uint_as_float(__float_as_uint(v) ^ flip); }
+
 // The new tokens' places that a column may look at, [lo, hi)
 struct Column {
     int g, u, lo, hi;
@@ -80,6 +84,21 @@ __device__ __forceinline__ Column column_of(const Paged &a, int b, int m, int n,
     return c;
 }
 
+// The work of a workgroup.  Neighbouring workgroups go to different XCDs; those that read the same places of the same heads to the same one, and
+// the shares of a sequence to several of them, for sequences differ in length.
+struct Work {
+    int b, kvh, col_tile, split;
+    __device__ __forceinline__ Work(const Paged &a)
+    {
+        const int heads = a.B * a.Hkv, i = blockIdx.x % (heads * a.splits);
+        col_tile = blockIdx.x / (heads * a.splits);
+        split = i / heads;
+        const int bh = (int)((i - split * heads + (long long)split * a.Hkv) % heads);
+        b = bh / a.Hkv;
+        kvh = bh - b * a.Hkv;
+    }
+};
+
 // NC blocks of 16 columns; DB blocks of 16 channels
 template <typename S, int DB, int NC>
 __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
@@ -92,8 +111,8 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
     constexpr int kPer = 16 / sizeof(S);                             // elements of an operand's 16 bytes
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, i = lane & 15;
-    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
-    const int ct = rest % a.col_tiles, split = rest / a.col_tiles, b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const Work work(a);
+    const int ct = work.col_tile, split = work.split, b = work.b, kvh = work.kvh;
     const int n_new = length_in(a.q_len, b, a.U), len = max(a.len[b], 0);
 
     Column col[NC];
@@ -127,7 +146,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int d = M::first_channel(s, quarter) + j;
-                e[j] = p[(size_t)min(d, a.D - 1) * a.U];
+                e[j] = flipped(p[(size_t)min(d, a.D - 1) * a.U], a.flip);
                 if (!col[n].there || d >= a.D) e[j] = S(0);
             }
             __builtin_memcpy(&q[n][s], e, 16);
@@ -209,7 +228,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
             // (as plain floats: elements of a matrix result that are changed under a branch come out wrong from this compiler)
             float z[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = s[n][j >> 2][j & 3] * a.c;
+            for (int j = 0; j < 8; ++j) z[j] = s[n][j >> 2][j & 3];
             if (edge) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -222,7 +241,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
 #pragma unroll
             for (int j = 1; j < 8; ++j) top = fmaxf(top, z[j]);
             top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
             if (__any(top > mx[n] + kLag)) {
                 top = fmaxf(top, mx[n]);
                 const float shrink = __builtin_amdgcn_exp2f(mx[n] - (top == -INFINITY ? 0.f : top));
@@ -235,7 +254,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
             float e[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                e[j] = __builtin_amdgcn_exp2f(z[j] - base);
+                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], a.c, -base));
                 sum[n] += e[j];
             }
             if constexpr (kBf16) {
@@ -368,8 +387,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
     constexpr int D = DB * 16, ND = (DB + 1) / 2, kGran = D / 8, kLoads = (kManyTile * kGran + 255) / 256, kAll = kManyTile * kGran;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i32 = lane & 31;
-    const int bh = blockIdx.x % (a.B * a.Hkv), rest = blockIdx.x / (a.B * a.Hkv);
-    const int ct = rest % a.col_tiles, split = rest / a.col_tiles, b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+    const Work work(a);
+    const int ct = work.col_tile, split = work.split, b = work.b, kvh = work.kvh;
     const int n_new = length_in(a.q_len, b, a.U), len = max(a.len[b], 0);
     const Column col = column_of(a, b, ct * kManyColumns + wave * 32 + i32, n_new, len);
     int first = col.there ? col.lo : 0x7fffffff, last = col.there ? col.hi : 0;
@@ -412,7 +431,21 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
     Pages pg = {}, next_pg = {};
     u32x4_t kr[kLoads], vr[kLoads];
     const int vg = tid & 7;  // the thread's group of eight places of the values' rows
+    // where this thread's parts of a tile lie: from its first place on, where one page has them all
+    const uint32_t k_off = (uint32_t)tid * 16, v_off = ((uint32_t)(tid >> 3) * (uint32_t)size + 8 * vg) * 2;
     auto load = [&](int t, const Pages &p) {
+        if (a.log_page >= 6) {  // (uniform)
+            const size_t page = (size_t)(there(p.p0) ? p.p0 : 0) * page_stride;
+            const int row0 = (t * kManyTile) & (size - 1);
+            const char *kp = reinterpret_cast<const char *>(kbase + page + (size_t)row0 * D), *vp = reinterpret_cast<const char *>(vbase + page + row0);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                kr[i] = *reinterpret_cast<const u32x4_t *>(kp + i * 4096 + (kAll % 256 == 0 || i + 1 < kLoads ? k_off : min(k_off, (uint32_t)(kAll - 1 - i * 256) * 16)));
+                const uint32_t row = (uint32_t)i * 64 * (uint32_t)size;  // 32 rows of values
+                vr[i] = *reinterpret_cast<const u32x4_t *>(vp + row + (D % 32 == 0 || i + 1 < kLoads ? v_off : min(v_off, (uint32_t)((D - 1 - i * 32) * size + 8 * vg) * 2)));
+            }
+            return;
+        }
         const Pages q = {there(p.p0) ? p.p0 : 0, there(p.p1) ? p.p1 : 0, there(p.p2) ? p.p2 : 0, there(p.p3) ? p.p3 : 0};
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -463,7 +496,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
             bf16_t e[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                e[j] = p[(size_t)(16 * s + 8 * half + j) * a.U];
+                e[j] = flipped(p[(size_t)(16 * s + 8 * half + j) * a.U], a.flip);
                 if (!col.there) e[j] = 0;
             }
             __builtin_memcpy(&q[s], e, 16);
@@ -492,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
                 s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const Frag *>(kp + n * 32 * L::kPitchK + st * 32), q[st], s[n], 0, 0, 0);
         float z[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) z[j] = s[j >> 4][j & 15] * a.c;
+        for (int j = 0; j < 32; ++j) z[j] = s[j >> 4][j & 15];
         if (!__all(whole && (!col.there || (col.lo <= t0 && t0 + kManyTile <= col.hi)))) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
@@ -504,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
         float top = z[0];
 #pragma unroll
         for (int j = 1; j < 32; ++j) top = fmaxf(top, z[j]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
         if (__any(top > mx + kLag)) {
             top = fmaxf(top, mx);
             const float shrink = __builtin_amdgcn_exp2f(mx - (top == -INFINITY ? 0.f : top));
@@ -520,7 +553,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
             float e[8], part = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                e[j] = __builtin_amdgcn_exp2f(z[8 * k + j] - base);
+                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[8 * k + j], a.c, -base));
                 part += e[j];
             }
             sum += part;
@@ -766,7 +799,9 @@ int nm_paged_attn_fwd(int B, int heads, int kv_heads, int D, int U, const void *
     while (1 << a.log_page < page_size) ++a.log_page;
     a.table = page_table; a.len = lengths; a.q_len = q_lengths;
     a.window = window;
-    a.c = scale * 1.4426950408889634f;
+    const float c = (scale < 0.f ? -scale : scale) * 1.4426950408889634f;
+    a.c = c < 1e-37f ? 1e-37f : c;  // (not zero: masked scores are -infinity times this)
+    a.flip = scale < 0.f ? 0x80000000u : 0u;
     a.out = o; a.lse = lse;
     a.part = (float *)workspace;
     a.part_ml = (float *)((char *)workspace + p.part_bytes);

@@ -2,8 +2,8 @@
 //
 // Work goes by units of two channels: the pairs that turn together, then the channels that do not turn, two by two.  Two divisions:
 //   tiles  one to four wavefronts own 32 tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
-//          channels are eight values of a lane, four exchanges and LDS, and every tensor is read and written once, in 64-byte pieces.  The
-//          angles of a tile's tokens are made once for all heads that the workgroup takes.  The last tile of a row begins 32
+//          channels are eight values of a lane, four exchanges and LDS, and every tensor is read and written once, in 64-byte pieces.  A lane
+//          makes the angles of its unit and tokens once for all heads that the workgroup takes.  The last tile of a row begins 32
 //          tokens before its end; what two tiles share is made twice, alike.
 //   single a wavefront owns one token of a head, a lane a unit: rows of fewer than eight tokens, and everything that goes into the cache.
 // An angle is position * freqs[i] as a part of a turn in double, of which only the fraction goes on in float: 500000 tokens into a
@@ -45,15 +45,20 @@ __device__ __forceinline__ void channels_of(const Heads &a, int unit, int &c0, i
     c1 = apart ? unit + half : 2 * unit + 1;
 }
 
-// cosine and sine of position * freq
-__device__ __forceinline__ float2 turn(int position, double freq)
+// Cosine and sine of a position's angle; per_turn: turns from one position to the next.  The fraction of a turn is made in double and goes on as
+// the nearest quarter and what is left of it, at most an eighth: there the series of both functions end after x^9 and x^8 within half a unit of float.
+__device__ __forceinline__ float2 turn(int position, double per_turn)
 {
-    const double t = (double)position * (freq * 0.15915494309189533577);  // in turns
-    const float f = (float)(t - rint(t));
-    float2 cs;
-    sincospif(2.f * f, &cs.y, &cs.x);
-    return cs;
+    const double t = (double)position * per_turn;
+    const float f = (float)(t - rint(t)), quarter = rintf(4.f * f);
+    const float x = __builtin_fmaf(quarter, -0.25f, f) * 6.28318530717958648f, z = x * x;
+    const float s = __builtin_fmaf(x * z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
+    const float c = __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.f / 40320, -1.f / 720), 1.f / 24), -0.5f), 1.f);
+    const uint32_t n = (uint32_t)(int)quarter;
+    const float co = n & 1 ? s : c, si = n & 1 ? c : s;
+    return {__uint_as_float(__float_as_uint(co) ^ ((n + 1) & 2) << 30), __uint_as_float(__float_as_uint(si) ^ (n & 2) << 30)};
 }
+constexpr double kPerRadian = 0.15915494309189533577;  // turns
 
 // Eight tokens of a channel as they lie in memory
 template <typename S>
@@ -71,8 +76,6 @@ struct Eight<float> {
     __device__ __forceinline__ float at(int e) const { return r[e]; }
 };
 
-constexpr int kAnglePitch = kTile + 2;  // (rows that begin at other banks)
-
 // PER wavefronts take a head, 16 units each: with all channels of a head in one wavefront, a lane's registers would be too many for more than one
 // or two wavefronts a SIMD.
 template <int PER>
@@ -85,7 +88,6 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
 {
     typedef TileForm<PER> F;
     typedef Eight<S> E;
-    extern __shared__ __align__(16) float2 angles[];  // [D/2][kAnglePitch]
     __shared__ float sums[2][F::kWaves][kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane & 3;
     const int slot = wave / PER, unit = wave % PER * 16 + (lane >> 2), units = a.D >> 1, half = a.rot >> 1;
@@ -101,9 +103,7 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
     // sums over a head's channels, for the lane's eight tokens, in order
     auto over_head = [&](float (&v)[8], int buffer) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int d = 4; d < 64; d <<= 1) v[e] += __shfl_xor(v[e], d);
+        for (int e = 0; e < 8; ++e) v[e] = sum_of_every_fourth(v[e]);
         if constexpr (PER > 1) {
             if (lane < 4) {
 #pragma unroll
@@ -140,20 +140,12 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
             }
         };
         if (some) load(h_begin + slot);  // (on its way while the angles are made)
-        if (a.rot && some) {  // (units that do not turn have the angle 0: a branch for them would cost more)
-            __syncthreads();  // (the tile before is through with them)
-            for (int i = threadIdx.x; i < units * kTile; i += F::kThreads) {
-                const int p = ub + (i & (kTile - 1)), row = i / kTile;
-                float2 cs = {1.f, 0.f};
-                if (row < half) cs = turn(a.positions ? a.positions[(size_t)b * a.U + min(p, a.U - 1)] : p, a.freqs[row]);
-                angles[row * kAnglePitch + (i & (kTile - 1))] = cs;
-            }
-            __syncthreads();
-        }
-        float2 cs[8];
+        float2 cs[8];  // of the lane's tokens, for its unit of every head
         if (a.rot && some) {
+            const double per_turn = unit < half ? a.freqs[unit] * kPerRadian : 0.0;
+            const int *positions = a.positions ? a.positions + (size_t)b * a.U + t : nullptr;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cs[e] = angles[min(unit, units - 1) * kAnglePitch + (t - ub) + e];
+            for (int e = 0; e < 8; ++e) cs[e] = turn(positions ? positions[e] : t + e, per_turn);
         }
         for (int hh = h_begin, turn_of = 0; hh < h_end; hh += F::kHeads, turn_of ^= 1) {
             const int h = hh + slot;
@@ -302,7 +294,7 @@ __global__ __launch_bounds__(256) void heads_single_kernel(Heads a)
         float y0 = 0.f, y1 = 0.f;
         if (there) {  // (uniform)
             float2 cs = {1.f, 0.f};
-            if (lane < half) cs = turn(position, a.freqs[lane]);
+            if (lane < half) cs = turn(position, a.freqs[lane] * kPerRadian);
             const float *weight = a.norm ? (key ? a.kw : a.qw) : nullptr;
             const float w0 = weight ? weight[c0] : 1.f, w1 = weight ? weight[c1] : 1.f;
             float x0 = 0.f, x1 = 0.f, r = 1.f;
@@ -406,8 +398,7 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
 template <typename S, int PER, bool BACK>
 hipError_t run_tile(const Heads &a, const Plan &p, hipStream_t s)
 {
-    heads_tile_kernel<S, PER, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(TileForm<PER>::kThreads),
-                                      (size_t)(a.rot ? a.D / 2 : 0) * kAnglePitch * sizeof(float2), s>>>(a);
+    heads_tile_kernel<S, PER, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(TileForm<PER>::kThreads), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename S, bool BACK>

@@ -62,6 +62,29 @@ __device__ __forceinline__ int length_in(const int *len, int b, int n)
     return v < 0 ? 0 : (v > n ? n : v);
 }
 
+// Sums over lanes by the vector unit alone (an exchange through LDS takes the LDS unit of all wavefronts of a CU as long as a dozen
+// additions take a SIMD).
+template <int N>
+__device__ __forceinline__ float turned_in_row(float v)  // lane i of 16 gets lane i - N
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float sum_of_rows(float v)  // over the four rows of 16 lanes
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float pair = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const uint32_t p = __float_as_uint(pair);
+    const auto b = __builtin_amdgcn_permlane32_swap(p, p, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float sum_of_every_fourth(float v)  // over the lanes with this lane's two lowest bits
+{
+    v += turned_in_row<4>(v);
+    v += turned_in_row<8>(v);
+    return sum_of_rows(v);
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 inline bool known_dtype(int dtype) { return dtype == NM_BF16 || dtype == NM_F32; }
 inline size_t element(int dtype) { return dtype == NM_BF16 ? 2 : 4; }

@@ -1,9 +1,9 @@
 // Norms of queries and keys for each head and their rotation by position (definition: include/nm_head_norm.h).
 //
 // Work goes by units of two channels: the pairs that turn together, then the channels that do not turn, two by two.  Two divisions:
-//   tiles  one to four wavefronts own 32 tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
-//          channels are eight values of a lane, four exchanges and LDS, and every tensor is read and written once, in 64-byte pieces.  A lane
-//          makes the angles of its unit and tokens once for all heads that the workgroup takes.  The last tile of a row begins 32
+//   tiles  one to eight wavefronts own 64 (32) tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
+//          channels are eight values of a lane, a few exchanges and LDS, and every tensor is read and written once, in 128-byte pieces.  A lane
+//          makes the angles of its unit and tokens once for all heads that the workgroup takes.  The last tile of a row begins as many
 //          tokens before its end; what two tiles share is made twice, alike.
 //   single a wavefront owns one token of a head, a lane a unit: rows of fewer than eight tokens, and everything that goes into the cache.
 // An angle is position * freqs[i] as a part of a turn in double, of which only the fraction goes on in float: 500000 tokens into a
@@ -14,9 +14,9 @@
 namespace nm {
 namespace {
 
-constexpr int kTile = 32;          // tokens
 constexpr int kMostTiles = 1024;   // that workgroups of the backward pass have side by side: rows of partial sums
 constexpr int kMaxD = 128;
+constexpr int kWideFrom = 64;      // tokens of a row from which on tiles have 64 of them
 
 struct Heads {
     int B, H, Hkv, D, U;
@@ -76,21 +76,23 @@ struct Eight<float> {
     __device__ __forceinline__ float at(int e) const { return r[e]; }
 };
 
-// PER wavefronts take a head, 16 units each: with all channels of a head in one wavefront, a lane's registers would be too many for more than one
-// or two wavefronts a SIMD.
-template <int PER>
+// PER wavefronts take a head, 64 / GROUPS units each and GROUPS groups of eight tokens: with all channels of a head in one wavefront, a lane's
+// registers would be too many for more than one or two wavefronts a SIMD.
+template <int GROUPS, int PER>
 struct TileForm {
-    static constexpr int kHeads = 4 / PER, kWaves = kHeads * PER, kThreads = kWaves * 64;  // heads side by side
+    static constexpr int kTile = 8 * GROUPS, kUnits = 64 / GROUPS;                                           // tokens; units of a wavefront
+    static constexpr int kHeads = PER < 4 ? 4 / PER : 1, kWaves = kHeads * PER, kThreads = kWaves * 64;  // heads side by side
 };
 
-template <typename S, int PER, bool BACK>
-__global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Heads a)
+template <typename S, int GROUPS, int PER, bool BACK>
+__global__ __launch_bounds__((TileForm<GROUPS, PER>::kThreads), sizeof(S) == 2 ? 4 : 2) void heads_tile_kernel(Heads a)
 {
-    typedef TileForm<PER> F;
+    typedef TileForm<GROUPS, PER> F;
     typedef Eight<S> E;
+    constexpr int kTile = F::kTile;
     __shared__ float sums[2][F::kWaves][kTile];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane & 3;
-    const int slot = wave / PER, unit = wave % PER * 16 + (lane >> 2), units = a.D >> 1, half = a.rot >> 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane % GROUPS;
+    const int slot = wave / PER, unit = wave % PER * F::kUnits + lane / GROUPS, units = a.D >> 1, half = a.rot >> 1;
     const bool is = unit < units, keys = blockIdx.y >= a.q_chunks;
     const int h_begin = keys ? a.H + (blockIdx.y - a.q_chunks) * a.heads_each : blockIdx.y * a.heads_each;
     const int h_end = min(h_begin + a.heads_each, keys ? a.H + a.Hkv : a.H);
@@ -103,9 +105,9 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
     // sums over a head's channels, for the lane's eight tokens, in order
     auto over_head = [&](float (&v)[8], int buffer) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = sum_of_every_fourth(v[e]);
+        for (int e = 0; e < 8; ++e) v[e] = sum_of_every<GROUPS>(v[e]);
         if constexpr (PER > 1) {
-            if (lane < 4) {
+            if (lane < GROUPS) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sums[buffer][wave][8 * lane + e] = v[e];
             }
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
     for (int tile = blockIdx.x; tile < a.B * a.u_tiles; tile += gridDim.x) {
         const int b = tile / a.u_tiles, u0 = (tile - b * a.u_tiles) * kTile, ub = max(0, min(u0, a.U - kTile));
         const int len = length_in(a.len, b, a.U);
-        const bool active = is && ub + 8 * g < a.U, some = ub < len;                // (rows of fewer than 32 tokens)
+        const bool active = is && ub + 8 * g < a.U, some = ub < len;                // (rows shorter than a tile)
         const int t = min(ub + 8 * g, a.U - 8), first = a.U < kTile ? 8 * g : u0;  // tokens before `first` are another lane's too
         const uint32_t at0 = c0 + (uint32_t)t * (uint32_t)sizeof(S), at1 = c1 + (uint32_t)t * (uint32_t)sizeof(S);
         const size_t head = (size_t)a.D * a.U;
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(TileForm<PER>::kThreads) void heads_tile_kernel(Hea
         if (!a.part) return;  // (uniform)
         __shared__ float all[F::kHeads][kMaxD];
 #pragma unroll
-        for (int d = 1; d < 4; d <<= 1) {
+        for (int d = 1; d < GROUPS; d <<= 1) {
             dw0 += __shfl_xor(dw0, d);
             dw1 += __shfl_xor(dw1, d);
         }
@@ -380,13 +382,14 @@ __global__ __launch_bounds__(256) void heads_join_kernel(const float *part, int 
 // How the heads and tokens are shared among workgroups
 struct Plan {
     bool tiles;
-    int u_tiles, heads_each, q_chunks, k_chunks, side;  // side: workgroups along the tokens
+    int groups, u_tiles, heads_each, q_chunks, k_chunks, side;  // side: workgroups along the tokens
 };
 Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
 {
     Plan p = {};
     p.tiles = U >= 8;
-    p.u_tiles = (U + kTile - 1) / kTile;
+    p.groups = U >= kWideFrom ? 8 : 4;
+    p.u_tiles = (U + 8 * p.groups - 1) / (8 * p.groups);
     p.heads_each = 4;
     const long long work = p.tiles ? (long long)B * p.u_tiles : ((long long)B * U + 3) / 4;
     p.side = (int)(back && work > kMostTiles ? kMostTiles : work);
@@ -395,10 +398,10 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
     return p;
 }
 
-template <typename S, int PER, bool BACK>
+template <typename S, int GROUPS, int PER, bool BACK>
 hipError_t run_tile(const Heads &a, const Plan &p, hipStream_t s)
 {
-    heads_tile_kernel<S, PER, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(TileForm<PER>::kThreads), 0, s>>>(a);
+    heads_tile_kernel<S, GROUPS, PER, BACK><<<dim3(p.side, p.q_chunks + p.k_chunks), dim3(TileForm<GROUPS, PER>::kThreads), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename S, bool BACK>
@@ -414,11 +417,23 @@ hipError_t run(Heads a, hipStream_t s)
         heads_single_kernel<S, BACK, false><<<grid, dim3(256), 0, s>>>(a);
         return hipGetLastError();
     }
-    switch ((a.D / 2 + 15) / 16) {
-    case 1: return run_tile<S, 1, BACK>(a, p, s);
-    case 2: return run_tile<S, 2, BACK>(a, p, s);
-    case 3: return run_tile<S, 3, BACK>(a, p, s);
-    default: return run_tile<S, 4, BACK>(a, p, s);
+    if (p.groups == 4) {
+        switch ((a.D / 2 + 15) / 16) {
+        case 1: return run_tile<S, 4, 1, BACK>(a, p, s);
+        case 2: return run_tile<S, 4, 2, BACK>(a, p, s);
+        case 3: return run_tile<S, 4, 3, BACK>(a, p, s);
+        default: return run_tile<S, 4, 4, BACK>(a, p, s);
+        }
+    }
+    switch ((a.D / 2 + 7) / 8) {
+    case 1: return run_tile<S, 8, 1, BACK>(a, p, s);
+    case 2: return run_tile<S, 8, 2, BACK>(a, p, s);
+    case 3: return run_tile<S, 8, 3, BACK>(a, p, s);
+    case 4: return run_tile<S, 8, 4, BACK>(a, p, s);
+    case 5: return run_tile<S, 8, 5, BACK>(a, p, s);
+    case 6: return run_tile<S, 8, 6, BACK>(a, p, s);
+    case 7: return run_tile<S, 8, 7, BACK>(a, p, s);
+    default: return run_tile<S, 8, 8, BACK>(a, p, s);
     }
 }
 

@@ -78,9 +78,10 @@ __device__ __forceinline__ float sum_of_rows(float v)  // over the four rows of 
     const auto b = __builtin_amdgcn_permlane32_swap(p, p, false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-__device__ __forceinline__ float sum_of_every_fourth(float v)  // over the lanes with this lane's two lowest bits
+template <int N>
+__device__ __forceinline__ float sum_of_every(float v)  // over the lanes whose number is this lane's modulo N (4 or 8)
 {
-    v += turned_in_row<4>(v);
+    if constexpr (N == 4) v += turned_in_row<4>(v);
     v += turned_in_row<8>(v);
     return sum_of_rows(v);
 }

@@ -420,7 +420,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
     // the pages of a tile's four groups of 16 places
     struct Pages {
         int p0, p1, p2, p3;
-        __device__ __forceinline__ int of(int j) const { return j < 2 ? (j == 0 ? p0 : p1) : (j == 2 ? p2 : p3); }
+        __device__ __forceinline__ int of(int j) const  // (of values: a choice between members would put them into scratch memory)
+        {
+            const int lower = j & 1 ? +p1 : +p0, upper = j & 1 ? +p3 : +p2;
+            return j & 2 ? +upper : +lower;
+        }
     };
     auto page_at = [&](int place) { return table[min(place >> a.log_page, a.max_pages - 1)]; };
     auto pages_of = [&](int t) {
@@ -683,9 +687,11 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, 
     p.blocks = columns > 16 ? 2 : 1;
     const int of_group = p.many ? kManyColumns : 16 * p.blocks, of_round = p.many ? kManyTile : kTile * kWaves;
     p.col_tiles = (int)((columns + of_group - 1) / of_group);
-    // workgroups share a token's places where there are fewer than two (four) a CU, but look at two rounds of places at least
-    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = p.many ? 512 : 1024;
-    long long splits = p.many ? wanted / groups : (wanted + groups - 1) / groups;
+    // workgroups share a token's places where there are fewer than two a CU, but look at two rounds of places at least.  (Shares of equal size
+    // whatever the sequences' lengths, which every workgroup and every row of the join has to find: 32 sequences of 4000 to 8000 places the same,
+    // chunks of 500 tokens 71 us and 31 for the join against 63 and 17.)
+    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = 512;
+    long long splits = wanted / groups;
     if (splits > rounds / 2) splits = rounds / 2;
     if (splits > kMaxSplits) splits = kMaxSplits;
     p.splits = splits < 1 ? 1 : (int)splits;

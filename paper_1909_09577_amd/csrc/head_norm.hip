@@ -120,7 +120,11 @@ __global__ __launch_bounds__((TileForm<GROUPS, PER>::kThreads), sizeof(S) == 2 ?
             }
         }
     };
-    for (int tile = blockIdx.x; tile < a.B * a.u_tiles; tile += gridDim.x) {
+    // neighbouring workgroups go to different XCDs: neighbouring tiles, which share lines of memory, are eight apart
+    const int tiles = a.B * a.u_tiles, each = (tiles + 7) / 8;
+    for (int i = blockIdx.x; i < each * 8; i += gridDim.x) {
+        const int tile = i % 8 * each + i / 8;
+        if (tile >= tiles) continue;  // (uniform)
         const int b = tile / a.u_tiles, u0 = (tile - b * a.u_tiles) * kTile, ub = max(0, min(u0, a.U - kTile));
         const int len = length_in(a.len, b, a.U);
         const bool active = is && ub + 8 * g < a.U, some = ub < len;                // (rows shorter than a tile)
@@ -392,7 +396,8 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
     p.u_tiles = (U + 8 * p.groups - 1) / (8 * p.groups);
     p.heads_each = 4;
     const long long work = p.tiles ? (long long)B * p.u_tiles : ((long long)B * U + 3) / 4;
-    p.side = (int)(back && work > kMostTiles ? kMostTiles : work);
+    const long long side = p.tiles ? (work + 7) / 8 * 8 : work;
+    p.side = (int)(back && side > kMostTiles ? kMostTiles : side);
     p.q_chunks = (H + p.heads_each - 1) / p.heads_each;
     p.k_chunks = (Hkv + p.heads_each - 1) / p.heads_each;
     return p;

@@ -153,7 +153,8 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
     __shared__ float sums[3][3][64];
     __shared__ key_t lists[K ? 3 : 1][K ? K : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ut = blockIdx.x % a.u_tiles, rest = blockIdx.x / a.u_tiles, split = rest % a.splits, b = rest / a.splits;
+    // neighbouring workgroups go to different XCDs: tiles of the same rows, which share lines of memory, are as many apart as there are others
+    const int others = a.B * a.splits, ut = blockIdx.x / others, rest = blockIdx.x - ut * others, split = rest % a.splits, b = rest / a.splits;
     const int lanes = 1 << a.log_lanes, u = ut * lanes + (lane & (lanes - 1)), step = 64 >> a.log_lanes;
     const int len = length_in(a.len, b, a.U);
     const int c0 = (split * 4 + wave) * a.per, c1 = min(a.V, c0 + a.per);
@@ -472,6 +473,8 @@ __global__ __launch_bounds__(256) void scores_bwd_flat_kernel(ScoresBwd a)
     store8((G *)a.out + (size_t)b * item + i0, n, g);
 }
 
+constexpr int kWorkgroups = 512;
+
 template <typename S, typename G>
 hipError_t run_bwd(ScoresBwd a, hipStream_t s)
 {
@@ -484,7 +487,9 @@ hipError_t run_bwd(ScoresBwd a, hipStream_t s)
     a.group_tiles = (a.groups + 255) / 256;
     a.side = (a.groups + a.group_tiles - 1) / a.group_tiles;
     a.rows = 256 / a.side;
-    a.rounds = 16;
+    // two workgroups a CU: what a thread reads of its places takes as long as some rounds (16 x 5000 x 333: 16 rounds 45 us, 32 37)
+    const long long rounds = ((long long)a.V * a.B * a.group_tiles / a.rows + kWorkgroups - 1) / kWorkgroups;
+    a.rounds = (int)((rounds < 4 ? 4 : rounds > 64 ? 64 : rounds) + 3) / 4 * 4;
     const long long tiles = (a.V + a.rows * a.rounds - 1) / (a.rows * a.rounds);
     scores_bwd_kernel<S, G><<<dim3((unsigned)(tiles * a.group_tiles * a.B)), dim3(256), 0, s>>>(a);
     return hipGetLastError();

@@ -4,9 +4,15 @@ Each layer has three blocks -- attention to the tokens written so far, attention
 ReLU between them -- and around each block the norms, the learned scale and the residual add, which are one call.  Projections are
 1x1 convolutions of the encoder's layout [batch][channels][time]; the tokens' attention to each other is the same call as that to the
 states, over windows that end with the token; every weight and every vector moves in one AdamW call.  This module only wires
-calls into libnmconv1d: torch provides device memory, the token table's one-hot rows and the loss's element-wise gradient.
+calls into libnmconv1d: torch provides device memory, and, where positions are added, the token table's one-hot rows and the loss's
+element-wise gradient.
 
-    python -m paper_1909_09577_amd.attn_decoder      # learns to copy a transcript that the states spell out, then decodes it
+Positions are added to the embeddings as sinusoids (positions="added"), or every head's queries and keys are normalised and turned by
+them (positions="rotated").  With the latter the embedding is a lookup, its gradient a sum over sorted tokens, the loss comes from the
+token scores' calls, and decoding keeps its keys and values in the pages of a cache, which takes tokens one by one or in chunks.
+
+    python -m paper_1909_09577_amd.attn_decoder            # learns to copy a transcript that the states spell out, then decodes it
+    python -m paper_1909_09577_amd.attn_decoder --rotated  # the same with rotated queries and keys and a paged cache
 """
 from __future__ import annotations
 
@@ -19,16 +25,22 @@ def _conv(x, w, **kw):
 
 class AttentionDecoder:
     """vocab classes, `channels` wide, `heads` heads over kv_heads shared ones, `layers` layers, states of `states` channels.
-    dtype: "bf16" (float32 masters, bfloat16 copies) or "f32"; state_bits: of AdamW's moments, 8 or 32."""
+    dtype: "bf16" (float32 masters, bfloat16 copies) or "f32"; state_bits: of AdamW's moments, 8 or 32; positions: "added" or "rotated"
+    (heads of a multiple of 16 channels then)."""
 
     def __init__(self, vocab, channels, heads, layers, states, kv_heads=None, hidden=None, dtype="bf16", state_bits=8, weight_decay=0.01,
-                 layer_norm=False, seed=0, device="cuda"):
+                 layer_norm=False, seed=0, device="cuda", positions="added"):
         import torch
         self.vocab, self.channels, self.heads, self.layers, self.layer_norm = vocab, channels, heads, layers, layer_norm
         self.kv_heads = heads if kv_heads is None else kv_heads
         self.dim = channels // heads
         if self.dim * heads != channels or heads % self.kv_heads:
             raise ValueError("heads must divide channels, kv_heads heads")
+        if positions not in ("added", "rotated"):
+            raise ValueError('positions must be "added" or "rotated"')
+        self.rotated = positions == "rotated"
+        if self.rotated and self.dim % 16:
+            raise ValueError("rotated heads must have a multiple of 16 channels")
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.device, self.steps, self.seed = device, 0, seed
         kv, hidden = self.kv_heads * self.dim, hidden or 4 * channels
@@ -43,9 +55,16 @@ class AttentionDecoder:
             self.master[name] = torch.full((n,), value, device=device)
             self.vectors.add(name)
 
-        weight("table", channels, vocab, vocab ** 0.5 * 0.5)
+        if self.rotated:  # a row for each token, times the root of its length
+            self.master["table"] = torch.randn(vocab, channels, device=device, generator=gen) * (0.5 * channels ** -0.5)
+            self.freqs = 10000.0 ** (-torch.arange(0, self.dim, 2, device=device, dtype=torch.float64) / self.dim)
+        else:
+            weight("table", channels, vocab, vocab ** 0.5 * 0.5)
         for l in range(layers):
             weight(f"{l}.self.in", channels + 2 * kv, channels)
+            if self.rotated:
+                vector(f"{l}.self.q_norm", self.dim, 1.0)
+                vector(f"{l}.self.k_norm", self.dim, 1.0)
             weight(f"{l}.cross.in", channels, channels)
             weight(f"{l}.cross.states", 2 * kv, states)
             weight(f"{l}.ffn.in", hidden, channels)
@@ -93,9 +112,12 @@ class AttentionDecoder:
         angle = at[None] * (10000.0 ** (-(c // 2) * 2 / self.channels))[:, None]
         return torch.where((c % 2 == 0)[:, None], angle.sin(), angle.cos()).mul(0.5).to(self.dtype)
 
-    def _embed(self, tokens, first):
-        """(one-hot rows [B, vocab, U], h [B, channels, U]) of token numbers [B, U]."""
+    def _embed(self, tokens, first, lengths=None):
+        """(one-hot rows [B, vocab, U], or the token numbers where there are none, h [B, channels, U]) of token numbers [B, U]."""
         import torch
+        if self.rotated:
+            tokens = tokens.contiguous()
+            return tokens, nm.nm_embedding_fwd(tokens, self.weights["table"], scale=self.channels ** 0.5, lengths=lengths)
         rows = (tokens[:, None] == torch.arange(self.vocab, device=self.device)[None, :, None]).to(self.dtype)
         pos = self._positions(first, tokens.shape[1])[None].expand(tokens.shape[0], -1, -1).contiguous()
         return rows, _conv(rows, self.weights["table"], residual=pos)
@@ -117,6 +139,11 @@ class AttentionDecoder:
     def _conv_bwd(self, name, x, dy, **kw):
         return nm.nm_conv1d_bwd(x, dy, self.weights[name], dw=self.grad[name], **kw)[0]
 
+    def _turning(self, l):
+        """What the norms and the rotation of layer l's queries and keys take."""
+        w = self.weights
+        return {"heads": self.heads, "kv_heads": self.kv_heads, "q_weight": w[f"{l}.self.q_norm"], "k_weight": w[f"{l}.self.k_norm"], "freqs": self.freqs}
+
     def _split(self, t):
         """Queries, keys and values of a projection's output, in place."""
         n, kv = t.shape[1] - 2 * self.kv_heads * self.dim, self.kv_heads * self.dim
@@ -133,13 +160,17 @@ class AttentionDecoder:
         past = torch.stack([torch.zeros_like(u), u + 1], 1).expand(B, U, 2).contiguous()
         own = dict(heads, lengths=token_lengths, q_lengths=token_lengths, windows=past)
         to_states = dict(heads, lengths=state_lengths, q_lengths=token_lengths)
-        rows, h = self._embed(tokens, 0)
+        rows, h = self._embed(tokens, 0, token_lengths)
         saved = {"rows": rows, "h0": h, "states": states, "own": own, "to_states": to_states, "lengths": token_lengths, "layers": []}
         _, n = nm.nm_residual_norm_fwd(h, next_weight=w["0.self.next"], next_bias=self._bias("0.self.next"), layer=self.layer_norm, lengths=token_lengths)
         for l in range(self.layers):
             s = {"self.n": n}
             s["qkv"] = _conv(n, w[f"{l}.self.in"])
-            s["self.o"], s["self.lse"] = nm.nm_cross_attn_fwd(*self._split(s["qkv"]), want_lse=True, **own)
+            q, k, v = self._split(s["qkv"])
+            if self.rotated:
+                s["qk"] = nm.nm_head_norm_fwd(s["qkv"][:, :q.shape[1] + k.shape[1]], lengths=token_lengths, **self._turning(l))
+                q, k = s["qk"][:, :q.shape[1]], s["qk"][:, q.shape[1]:]
+            s["self.o"], s["self.lse"] = nm.nm_cross_attn_fwd(q, k, v, want_lse=True, **own)
             s["self.f"] = _conv(s["self.o"], w[f"{l}.self.out"])
             s["self.h"], n = h, s["cross.n"] = self._around(l, "self", h, s["self.f"], token_lengths)
             s["q"], s["kv"] = _conv(n, w[f"{l}.cross.in"]), _conv(states, w[f"{l}.cross.states"])
@@ -177,13 +208,23 @@ class AttentionDecoder:
             dh, df = self._around_bwd(l, "self", dh, dn, s["self.h"], s["self.f"], lengths)
             do = self._conv_bwd(f"{l}.self.out", s["self.o"], df)
             dqkv = torch.empty_like(s["qkv"])
-            dq, dk, dv = self._split(dqkv)
-            nm.nm_cross_attn_bwd(do, *self._split(s["qkv"]), s["self.o"], s["self.lse"], dq=dq, dk=dk, dv=dv, **saved["own"])
+            (q, k, v), (dq, dk, dv) = self._split(s["qkv"]), self._split(dqkv)
+            if self.rotated:
+                nq, both = q.shape[1], q.shape[1] + k.shape[1]
+                q, k, dqk = s["qk"][:, :nq], s["qk"][:, nq:], torch.empty_like(s["qk"])
+                dq, dk = dqk[:, :nq], dqk[:, nq:]
+            nm.nm_cross_attn_bwd(do, q, k, v, s["self.o"], s["self.lse"], dq=dq, dk=dk, dv=dv, **saved["own"])
+            if self.rotated:
+                nm.nm_head_norm_bwd(dqk, s["qkv"][:, :both], lengths=lengths, dx=dqkv[:, :both], dq_weight=g[f"{l}.self.q_norm"],
+                                    dk_weight=g[f"{l}.self.k_norm"], **self._turning(l))
             dn = self._conv_bwd(f"{l}.self.in", s["self.n"], dqkv)
         first = "0.self.next"
         got = nm.nm_residual_norm_bwd(dh, dn, saved["h0"], next_weight=self.weights[first], next_bias=self._bias(first), layer=self.layer_norm,
                                       lengths=lengths, out={"dnext_weight": g[first], "dnext_bias": g.get(first + "_bias")})
-        nm.nm_conv1d_bwd_weight(saved["rows"], got["dx"], 1, dw=g["table"])
+        if self.rotated:
+            nm.nm_embedding_bwd(got["dx"], saved["rows"], self.vocab, scale=self.channels ** 0.5, lengths=lengths, dtable=g["table"])
+        else:
+            nm.nm_conv1d_bwd_weight(saved["rows"], got["dx"], 1, dw=g["table"])
         return dstates
 
     def loss(self, logp, targets, token_lengths):
@@ -191,6 +232,10 @@ class AttentionDecoder:
         import torch
         there = torch.arange(targets.shape[1], device=self.device)[None] < token_lengths[:, None]
         per = there.float() / there.sum().clamp_min(1)
+        if self.rotated:
+            targets = targets.contiguous()
+            of = nm.nm_token_scores_fwd(logp, targets, lengths=token_lengths)
+            return -(of["logp"] * per).sum(), nm.nm_token_scores_bwd(logp, targets, of["lse"], None, -per, lengths=token_lengths)
         picked = logp.gather(1, targets[:, None]).squeeze(1)
         grad = (logp.exp() - (targets[:, None] == torch.arange(self.vocab, device=self.device)[None, :, None]).float()) * per[:, None]
         return -(picked * per).sum(), torch.where(there[:, None], grad, 0.0)
@@ -205,11 +250,17 @@ class AttentionDecoder:
         return loss, dstates
 
     # ---- decoding -----------------------------------------------------------------------------------
-    def start(self, states, state_lengths, room):
+    def start(self, states, state_lengths, room, page=64):
         """What the tokens of a batch of utterances need: every layer's keys and values of the states, and room for those of `room`
-        tokens (channel-major, a token's column is filled when it is known)."""
+        tokens (channel-major, a token's column is filled when it is known; with rotated positions in pages of `page` tokens)."""
         import torch
         B, width = states.shape[0], 2 * self.kv_heads * self.dim
+        if self.rotated:
+            each = -(-room // page)
+            empty = lambda *shape: [torch.empty(B * each, self.kv_heads, *shape, dtype=self.dtype, device=self.device) for _ in range(self.layers)]  # noqa: E731
+            return {"kv": [_conv(states, self.weights[f"{l}.cross.states"]) for l in range(self.layers)], "state_lengths": state_lengths, "at": 0, "room": room,
+                    "k": empty(page, self.dim), "v": empty(self.dim, page), "filled": torch.zeros(B, dtype=torch.int32, device=self.device),
+                    "pages": torch.arange(B * each, dtype=torch.int32, device=self.device).view(B, each)}
         return {"kv": [_conv(states, self.weights[f"{l}.cross.states"]) for l in range(self.layers)], "state_lengths": state_lengths, "at": 0, "room": room,
                 "cache": [torch.empty(B, width, room, dtype=self.dtype, device=self.device) for _ in range(self.layers)],
                 "filled": torch.zeros(B, dtype=torch.int32, device=self.device)}
@@ -218,6 +269,8 @@ class AttentionDecoder:
         """Log-probabilities [B, vocab] of what follows the tokens int64 [B], the latest of every utterance."""
         if run["at"] >= run["room"]:
             raise ValueError("no room for another token")
+        if self.rotated:
+            return self.extend(tokens[:, None], run)[:, :, 0]
         w, heads = self.weights, {"heads": self.heads, "kv_heads": self.kv_heads}
         _, h = self._embed(tokens[:, None], run["at"])
         run["filled"] += 1
@@ -233,6 +286,36 @@ class AttentionDecoder:
             h, n = self._around(l, "ffn", h, _conv(_conv(n, w[f"{l}.ffn.in"], relu=True), w[f"{l}.ffn.out"]), None)
         run["at"] += 1
         return nm.nm_decoder_logsoftmax_fwd(n, w["classes"][:, :, 0], w["classes_bias"])[:, :, 0]
+
+
+    def extend(self, tokens, run, counts=None):
+        """Log-probabilities [B, vocab, U] of what follows each of the new tokens int64 [B, U], of which an utterance has the first counts[b]
+        (int32 [B]; None: all; what comes back behind them says nothing).  With rotated positions."""
+        if not self.rotated:
+            raise ValueError("chunks of tokens need rotated positions")
+        if run["at"] + tokens.shape[1] > run["room"]:
+            raise ValueError("no room for so many tokens")
+        w, heads = self.weights, {"heads": self.heads, "kv_heads": self.kv_heads}
+        _, h = self._embed(tokens, 0, counts)
+        run["filled"] += tokens.shape[1] if counts is None else counts
+        _, n = nm.nm_residual_norm_fwd(h, next_weight=w["0.self.next"], next_bias=self._bias("0.self.next"), layer=self.layer_norm, lengths=counts)
+        for l in range(self.layers):
+            cache = run["k"][l], run["v"][l], run["pages"], run["filled"]
+            q = nm.nm_head_norm_cache(_conv(n, w[f"{l}.self.in"]), *cache, q_lengths=counts, **self._turning(l))
+            o, _ = nm.nm_paged_attn_fwd(q, *cache, q_lengths=counts, **heads)
+            h, n = self._around(l, "self", h, _conv(o, w[f"{l}.self.out"]), counts)
+            o, _ = nm.nm_cross_attn_fwd(_conv(n, w[f"{l}.cross.in"]), *self._split(run["kv"][l])[1:], lengths=run["state_lengths"], q_lengths=counts, **heads)
+            h, n = self._around(l, "cross", h, _conv(o, w[f"{l}.cross.out"]), counts)
+            h, n = self._around(l, "ffn", h, _conv(_conv(n, w[f"{l}.ffn.in"], relu=True), w[f"{l}.ffn.out"]), counts)
+        run["at"] += tokens.shape[1]
+        return nm.nm_decoder_logsoftmax_fwd(n, w["classes"][:, :, 0], w["classes_bias"])
+
+    def best(self, logp, count):
+        """The `count` likeliest classes of log-probabilities [B, vocab] or [B, vocab, U] and theirs, in order: int32 and float32
+        [B, count] or [B, count, U]."""
+        of = nm.nm_token_scores_fwd((logp if logp.dim() == 3 else logp[:, :, None]).contiguous(), top=count)
+        ids, scores = of["top_ids"], of["top_logp"]
+        return (ids, scores) if logp.dim() == 3 else (ids[:, :, 0], scores[:, :, 0])
 
 
 def spelled(batch, tokens, frames, vocab, channels, dtype, seed, device="cuda"):
@@ -255,10 +338,14 @@ def spelled(batch, tokens, frames, vocab, channels, dtype, seed, device="cuda"):
     return ins, targets, states, (n + 1).to(torch.int32), (n * per).to(torch.int32)
 
 
-def main():
+def main(argv=None):
+    import argparse
     import torch
+    ap = argparse.ArgumentParser(description="learns to copy a transcript that the states spell out, then decodes it")
+    ap.add_argument("--rotated", action="store_true", help="queries and keys turned by position, a paged cache")
+    positions = "rotated" if ap.parse_args(argv).rotated else "added"
     vocab, room = 29, 12
-    dec = AttentionDecoder(vocab, 256, 4, 2, 256, kv_heads=2, seed=1)
+    dec = AttentionDecoder(vocab, 256, 4, 2, 256, kv_heads=2, seed=1, positions=positions)
     for i in range(400):
         batch = spelled(32, room, 96, vocab, 256, dec.dtype, seed=i)
         loss, _ = dec.step(*batch, lr=2e-3 * min((i + 1) / 50, (400 - i) / 350))
@@ -267,7 +354,8 @@ def main():
     ins, targets, states, n, frames = spelled(8, room, 96, vocab, 256, dec.dtype, seed=10 ** 6)
     run, token, out = dec.start(states, frames, room + 1), ins[:, 0], []
     for _ in range(room + 1):
-        token = dec.next(token, run).argmax(1)
+        logp = dec.next(token, run)
+        token = dec.best(logp, 1)[0][:, 0].long() if dec.rotated else logp.argmax(1)
         out.append(token)
     there = torch.arange(room + 1, device="cuda")[None] < n[:, None]
     right = (torch.stack(out, 1) == targets)[there].float().mean().item()

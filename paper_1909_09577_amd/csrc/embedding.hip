@@ -102,7 +102,7 @@ hipError_t run_fwd(EmbedFwd a, hipStream_t s)
 constexpr int kThreads = 512, kWaves = kThreads / 64;  // of the workgroups that sort, turn and fill
 constexpr int kChunk = kWaves * 1024;                  // places that a sorting workgroup looks at at a time
 constexpr int kList = 4096;                            // of its range that it can hold
-constexpr int kRange = 512;                            // tokens of a sorting workgroup at most
+constexpr int kRange = 256;                            // tokens of a sorting workgroup at most
 constexpr int kRun = 8;                                // sorted places of a wavefront
 constexpr int kFill = 32768;                           // floats that a workgroup fills
 
@@ -186,14 +186,16 @@ __device__ __forceinline__ void tokens_at(const EmbedBwd &a, int p0, int lane, i
 }
 
 // One range of tokens: which places have them, in order of the tokens and of the places.  A wavefront looks at 1024 neighbouring places
-// at a time; those of the range are packed into a list in their order, and each wavefront picks its own tokens' out of it.  Where the list
-// is too short for all, it is made again for the next ones.
+// at a time; those of the range are packed into a list in their order, of which each wavefront takes its own stretch: it counts the tokens
+// there, and from what the wavefronts before it counted knows where its places go.  Where the list is too short for all, it is made again for
+// the next ones.
 __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
 {
     int *count = reinterpret_cast<int *>(smem);                    // [kRange]
     int *begin = count + kRange;                                   // [kRange]
-    int *next = begin + kRange;                                    // [kRange]: where the next place goes
-    int *sums = next + kRange;                                     // [3][kWaves]
+    int *next = begin + kRange;                                    // [kRange]: where the list's first place goes
+    int *ours = next + kRange;                                     // [kWaves][kRange]: a stretch's tokens; where its next place goes
+    int *sums = ours + kWaves * kRange;                            // [3][kWaves]
     int *place = sums + 3 * kWaves;                                // [kList]
     uint16_t *bin = reinterpret_cast<uint16_t *>(place + kList);   // [kList]
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -245,11 +247,23 @@ __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
         __syncthreads();
         return found;
     };
-    const int all = pack(0);
-    for (int w0 = 0; w0 < all; w0 += kList) {  // how often every token occurs
-        if (w0) pack(w0);
-        for (int j = t; j < min(all - w0, kList); j += kThreads) atomicAdd(&count[bin[j]], 1);  // (whole numbers: any order gives the same)
+    // a wavefront's stretch of a list, a multiple of 64 places; how often every token occurs in each
+    int *mine = ours + wave * kRange;
+    auto stretch = [&](int listed) { return ((listed + kWaves - 1) / kWaves + 63) / 64 * 64; };
+    auto tally = [&](int listed) {
+        for (int r = t; r < kWaves * kRange; r += kThreads) ours[r] = 0;
         __syncthreads();
+        const int side = stretch(listed), j1 = min(listed, (wave + 1) * side);
+        for (int j = wave * side + lane; j < j1; j += 64) atomicAdd(&mine[bin[j]], 1);  // (whole numbers: any order gives the same)
+        __syncthreads();
+    };
+    const int all = pack(0);
+    for (int w0 = 0; w0 < all; w0 += kList) {
+        if (w0) pack(w0);
+        tally(min(all - w0, kList));
+        for (int r = t; r < bins; r += kThreads)
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) count[r] += ours[w * kRange + r];
     }
     if (lane == 0) sums[2 * kWaves + wave] = less;
     __syncthreads();
@@ -266,24 +280,38 @@ __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
     }
     __syncthreads();
     for (int w0 = 0; w0 < all; w0 += kList) {
+        const int listed = min(all - w0, kList);
         if (all > kList) {
             __syncthreads();
             pack(w0);
+            tally(listed);
         }
-        // A wavefront's tokens are every kWaves-th.  Of 64 listed places it finds those of one of its tokens at a time.
-        const int listed = min(all - w0, kList);
-        for (int j = 0; j < listed; j += 64) {
-            const bool is = j + lane < listed;
-            const int r = is ? bin[j + lane] : 0;
-            uint64_t open = __ballot(is && r % kWaves == wave);
-            while (open) {
-                const int token = __builtin_amdgcn_readlane(r, __builtin_ctzll(open));
-                const uint64_t same = __ballot(is && r == token);
-                const int from = begin[token], at = next[token];
-                if ((same >> lane) & 1) a.order[at + __builtin_popcountll(same & lower)] = Entry{place[j + lane], v0 + token, from, from + count[token]};
-                if (lane == 0) next[token] = at + __builtin_popcountll(same);  // (this wavefront's alone)
-                open &= ~same;
+        for (int r = t; r < bins; r += kThreads) {
+            int at = next[r];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const int n = ours[w * kRange + r];
+                ours[w * kRange + r] = at;
+                at += n;
             }
+            next[r] = at;
+        }
+        __syncthreads();
+        const int side = stretch(listed), j1 = min(listed, (wave + 1) * side);
+        for (int j = wave * side; j < j1; j += 64) {
+            const bool is = j + lane < j1;
+            const int r = is ? bin[j + lane] : 0;
+            uint64_t same = __ballot(is);  // the lanes with the same token
+            for (int bit = 1; bit < bins; bit <<= 1) {
+                const uint64_t set = __ballot((r & bit) != 0);
+                same &= r & bit ? set : ~set;
+            }
+            if (is) {
+                const int from = begin[r], at = mine[r];
+                a.order[at + __builtin_popcountll(same & lower)] = Entry{place[j + lane], v0 + r, from, from + count[r]};
+                if (!(same & lower)) mine[r] = at + __builtin_popcountll(same);
+            }
+            __builtin_amdgcn_wave_barrier();  // (what a lane wrote, others read)
         }
     }
 }
@@ -340,10 +368,10 @@ __device__ void turn_tile(const EmbedBwd &a, int tile, unsigned char *smem)
     }
 }
 
-constexpr int kSortBytes = kList * 6 + 3 * kRange * 4 + 3 * kWaves * 4;
+constexpr int kSortBytes = kList * 6 + (3 + kWaves) * kRange * 4 + 3 * kWaves * 4;
 
 template <typename S>
-__global__ __launch_bounds__(kThreads, 8) void embed_order_kernel(EmbedBwd a)
+__global__ __launch_bounds__(kThreads, 6) void embed_order_kernel(EmbedBwd a)
 {
     __shared__ __align__(16) unsigned char smem[kSortBytes];
     static_assert(Turn<S>::kBytes <= kSortBytes, "");

@@ -347,7 +347,7 @@ Plan plan_of(int B, int V, int U, int top)
     // four workgroups a CU, but a wavefront has a whole round of classes to do, and a wavefront joins all lists of a place
     const long long groups = (long long)B * p.u_tiles;
     long long splits = 1024 / groups;
-    const long long most = V / (4LL * step * kAhead), joined = 64 / (list ? list : 1);
+    const long long most = (V + 4LL * step * kAhead - 1) / (4LL * step * kAhead), joined = 64 / (list ? list : 1);
     if (splits > most) splits = most;
     if (splits > joined) splits = joined;
     if (splits < 1) splits = 1;

@@ -615,6 +615,16 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
         }
 }
 
+// ROWS rows of outputs from row0 on (there are fewer than 2^30), by EACH threads for a row: neighbouring lanes store neighbouring tokens.
+template <typename S, int ROWS, int EACH>
+__device__ __forceinline__ void store_rows(const Paged &a, const float (&tile)[ROWS][128 + 1], size_t row0)
+{
+    const uint32_t r = threadIdx.x % ROWS, to = (uint32_t)row0 + r, U = (uint32_t)a.U, bh = to / U, u = to - bh * U, b = bh / (uint32_t)a.H, h = bh - b * (uint32_t)a.H;
+    if (to >= (uint32_t)a.B * (uint32_t)a.H * U) return;
+    S *out = (S *)a.out + (size_t)b * a.os + (size_t)h * a.D * U + u;
+    for (int d = threadIdx.x / ROWS; d < a.D; d += EACH) store_from_f32(out, (size_t)d * U, tile[r][d]);
+}
+
 // Joins the sums of `splits` workgroups in order: a wavefront takes a row (a token of a head), a lane one split's maximum and sum, and then
 // eight channels of every fourth split.  (One thread for a row's maxima, split after split, took 17 us for 512 rows of 16 splits.)
 template <typename S, int ROWS>
@@ -665,13 +675,45 @@ __global__ __launch_bounds__(ROWS * 64) void paged_join_kernel(Paged a)
         for (int j = 0; j < 8; ++j) tile[r][d0 + j] = v[j];
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < ROWS * a.D; e += ROWS * 64) {  // neighbouring lanes store neighbouring tokens
-        const int er = e % ROWS, d = e / ROWS;
-        const size_t to = row0 + er;
-        if (to >= rows) continue;
-        const size_t bh = to / a.U, u = to - bh * a.U, b = bh / a.H, h = bh - b * a.H;
-        store_from_f32((S *)a.out, b * a.os + (h * a.D + d) * a.U + u, tile[er][d]);
+    store_rows<S, ROWS, 64>(a, tile, row0);
+}
+
+// The same for few splits and many tokens: a thread takes eight channels of a row, one split after the other.
+constexpr int kFewSplits = 4, kJoinRows = 32;
+template <typename S>
+__global__ __launch_bounds__(kJoinRows * 16) void paged_join_few_kernel(Paged a)
+{
+    __shared__ float tile[kJoinRows][128 + 1];
+    const size_t rows = (size_t)a.B * a.H * a.U, row0 = (size_t)blockIdx.x * kJoinRows;
+    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
+    const size_t row = min(row0 + r, rows - 1);
+    float2 ml[kFewSplits];
+    float p[kFewSplits][8];
+    const float *part = a.part + row * a.D + min(d0, a.D - 8);
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {  // (those behind the last split read it again, and count for nothing)
+        const int of = min(s, a.splits - 1);
+        ml[s] = *reinterpret_cast<const float2 *>(a.part_ml + (of * rows + row) * 2);
+        load8(part + of * rows * a.D, 8, p[s]);
     }
+    float top = ml[0].x;
+#pragma unroll
+    for (int s = 1; s < kFewSplits; ++s) top = fmaxf(top, ml[s].x);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, total = 0.f;
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+        if (s >= a.splits) continue;
+        const float w = __builtin_amdgcn_exp2f(ml[s].x - (top == -INFINITY ? 0.f : top));
+        total += w * ml[s].y;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += w * p[s][j];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    if (a.lse && d0 == 0 && row0 + r < rows) a.lse[row] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[r][d0 + j] = v[j] * inv;
+    __syncthreads();
+    store_rows<S, kJoinRows, 16>(a, tile, row0);
 }
 
 struct Plan {
@@ -747,7 +789,8 @@ hipError_t run(const Paged &a, const Plan &p, hipStream_t s)
     }
     if (e != hipSuccess || a.splits == 1) return e;
     const size_t rows = (size_t)a.B * a.H * a.U;
-    if (a.U >= 16) paged_join_kernel<S, 16><<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s>>>(a);
+    if (a.splits <= kFewSplits && a.U >= kJoinRows) paged_join_few_kernel<S><<<dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)), dim3(kJoinRows * 16), 0, s>>>(a);
+    else if (a.U >= 16) paged_join_kernel<S, 16><<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s>>>(a);
     else paged_join_kernel<S, 4><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }

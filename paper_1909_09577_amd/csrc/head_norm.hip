@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kMostTiles = 1024;   // that workgroups of the backward pass have side by side: rows of partial sums
 constexpr int kMaxD = 128;
-constexpr int kWideFrom = 64;      // tokens of a row from which on tiles have 64 of them
+constexpr int kGroups = 4;         // of eight tokens, that a tile has
 
 struct Heads {
     int B, H, Hkv, D, U;
@@ -268,10 +268,10 @@ __global__ __launch_bounds__(256) void heads_single_kernel(Heads a)
     const bool keys_chunk = BACK && chunk >= a.q_chunks;
     const int h_first = !BACK ? 0 : keys_chunk ? a.H + (chunk - a.q_chunks) * a.heads_each : chunk * a.heads_each;
     const int h_count = !BACK ? all : min(a.heads_each, (keys_chunk ? a.H + a.Hkv : a.H) - h_first);
-    const long long count = (long long)tokens * h_count, stride = (long long)gridDim.x * 4;
+    const int count = tokens * h_count, stride = gridDim.x * 4;  // (below 2^25 and, of the grid, 2^26)
     float dw0 = 0.f, dw1 = 0.f;
-    for (long long i = (long long)blockIdx.x * 4 + wave; i < count; i += stride) {
-        const int bh = (int)(i / a.U), u = (int)(i - (long long)bh * a.U), b = bh / h_count, h = h_first + bh - b * h_count;
+    for (int i = blockIdx.x * 4 + wave; i < count; i += stride) {
+        const int bh = i / a.U, u = i - bh * a.U, b = bh / h_count, h = h_first + bh - b * h_count;
         const S *x = (const S *)a.x + (size_t)b * a.xs + (size_t)h * a.D * a.U + u;
         int len, position = u;
         if constexpr (CACHE) {
@@ -386,14 +386,13 @@ __global__ __launch_bounds__(256) void heads_join_kernel(const float *part, int 
 // How the heads and tokens are shared among workgroups
 struct Plan {
     bool tiles;
-    int groups, u_tiles, heads_each, q_chunks, k_chunks, side;  // side: workgroups along the tokens
+    int u_tiles, heads_each, q_chunks, k_chunks, side;  // side: workgroups along the tokens
 };
 Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
 {
     Plan p = {};
     p.tiles = U >= 8;
-    p.groups = U >= kWideFrom ? 8 : 4;
-    p.u_tiles = (U + 8 * p.groups - 1) / (8 * p.groups);
+    p.u_tiles = (U + 8 * kGroups - 1) / (8 * kGroups);
     p.heads_each = 4;
     const long long work = p.tiles ? (long long)B * p.u_tiles : ((long long)B * U + 3) / 4;
     const long long side = p.tiles ? (work + 7) / 8 * 8 : work;
@@ -422,23 +421,12 @@ hipError_t run(Heads a, hipStream_t s)
         heads_single_kernel<S, BACK, false><<<grid, dim3(256), 0, s>>>(a);
         return hipGetLastError();
     }
-    if (p.groups == 4) {
-        switch ((a.D / 2 + 15) / 16) {
-        case 1: return run_tile<S, 4, 1, BACK>(a, p, s);
-        case 2: return run_tile<S, 4, 2, BACK>(a, p, s);
-        case 3: return run_tile<S, 4, 3, BACK>(a, p, s);
-        default: return run_tile<S, 4, 4, BACK>(a, p, s);
-        }
-    }
-    switch ((a.D / 2 + 7) / 8) {
-    case 1: return run_tile<S, 8, 1, BACK>(a, p, s);
-    case 2: return run_tile<S, 8, 2, BACK>(a, p, s);
-    case 3: return run_tile<S, 8, 3, BACK>(a, p, s);
-    case 4: return run_tile<S, 8, 4, BACK>(a, p, s);
-    case 5: return run_tile<S, 8, 5, BACK>(a, p, s);
-    case 6: return run_tile<S, 8, 6, BACK>(a, p, s);
-    case 7: return run_tile<S, 8, 7, BACK>(a, p, s);
-    default: return run_tile<S, 8, 8, BACK>(a, p, s);
+    constexpr int kUnits = 64 / kGroups;
+    switch ((a.D / 2 + kUnits - 1) / kUnits) {
+    case 1: return run_tile<S, kGroups, 1, BACK>(a, p, s);
+    case 2: return run_tile<S, kGroups, 2, BACK>(a, p, s);
+    case 3: return run_tile<S, kGroups, 3, BACK>(a, p, s);
+    default: return run_tile<S, kGroups, 4, BACK>(a, p, s);
     }
 }
 

@@ -79,9 +79,10 @@ __device__ __forceinline__ float sum_of_rows(float v)  // over the four rows of 
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 template <int N>
-__device__ __forceinline__ float sum_of_every(float v)  // over the lanes whose number is this lane's modulo N (4 or 8)
+__device__ __forceinline__ float sum_of_every(float v)  // over the lanes whose number is this lane's modulo N (2 or 4)
 {
-    if constexpr (N == 4) v += turned_in_row<4>(v);
+    if constexpr (N == 2) v += turned_in_row<2>(v);
+    if constexpr (N <= 4) v += turned_in_row<4>(v);
     v += turned_in_row<8>(v);
     return sum_of_rows(v);
 }

@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void scores_bwd_flat_kernel(ScoresBwd a)
     const int len = length_in(a.len, b, a.U), n = (int)min(item - i0, 8LL);
     float z[8], g[8];
     load8((const S *)a.scores + (size_t)b * item + i0, n, z);
-    int c = (int)(i0 / a.U), u = (int)(i0 - (long long)c * a.U);
+    int c = (int)((uint32_t)i0 / (uint32_t)a.U), u = (int)i0 - c * a.U;  // (an item has fewer than 2^31)
     Place p = place_of(a, b, u, len);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {

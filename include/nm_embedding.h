@@ -12,7 +12,7 @@
  *  - dtype (NM_BF16 or NM_F32) is the storage type of table, out and dout; dtable is float.  Sums are float32, in the order of the
  *    places, in groups that depend on how often a token occurs.
  *  - ids [B][U]: int32 (id_bytes 4) or int64 (id_bytes 8).  lengths [B] int32, optional (NULL); any values are taken, clipped to
- *    [0,U].  dout is not read at u >= lengths[b] or where the id is outside [0,V), whatever it holds.
+ *    [0,U].  dout is not used at u >= lengths[b] or where the id is outside [0,V), whatever it holds.
  *  - workspace: nm_embedding_bwd_workspace_bytes bytes, 256-byte aligned.
  *  - V * C and B * C * U must be below 2^31, B * U at most 2^31 - 2^14 - 1, B at most 65535; tiles of 64 tokens and 64 channels, the items'
  *    last ones counted whole, below 2^23.

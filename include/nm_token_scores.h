@@ -19,7 +19,7 @@
  *  - dtype (NM_BF16 or NM_F32) is the storage type of scores; that of dscores is grad_dtype.  Everything else is float, sums too.  Scores are
  *    sums of anything: logits, or log-probabilities as nm_decoder_logsoftmax_fwd gives them.  +infinity gives NaN.
  *  - targets [B][U]: int32 (target_bytes 4) or int64 (8).  lengths [B] int32, optional (NULL); any values are taken, clipped to [0,U].
- *    scores are not read at u >= lengths[b], whatever they hold.
+ *    scores are not used at u >= lengths[b], whatever they hold.
  *  - top is at most 16 and at most V.
  *  - workspace: nm_token_scores_workspace_bytes bytes, 256-byte aligned (NULL where that is 0).
  *  - B * V * U must be below 2^31, V at most 2^31 - 2^16 - 1, U at most 2^29.

@@ -1,11 +1,17 @@
 // Norms of queries and keys for each head and their rotation by position (definition: include/nm_head_norm.h).
 //
 // Work goes by units of two channels: the pairs that turn together, then the channels that do not turn, two by two.  Two divisions:
-//   tiles  one to eight wavefronts own 64 (32) tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
-//          channels are eight values of a lane, a few exchanges and LDS, and every tensor is read and written once, in 128-byte pieces.  A lane
-//          makes the angles of its unit and tokens once for all heads that the workgroup takes.  The last tile of a row begins as many
-//          tokens before its end; what two tiles share is made twice, alike.
+//   tiles  one to four wavefronts own 32 tokens of a head, a lane eight neighbouring tokens of a unit, so that the sums over a head's
+//          channels are eight values of a lane, a few exchanges and LDS, and every tensor is read and written once.  A lane makes the angles of
+//          its unit and tokens once for all heads that the workgroup takes.  The last tile of a row begins as many tokens before its end; what
+//          two tiles share is made twice, alike.  Tiles that share 128-byte lines of memory run on the same XCD: with 64 tokens a tile has
+//          lines of its own, but half as many workgroups (backward of 4 x 1333 tokens, 10 heads of 128: 21 us instead of 17).
 //   single a wavefront owns one token of a head, a lane a unit: rows of fewer than eight tokens, and everything that goes into the cache.
+//          (32 items, 20 heads of 64, forward and backward with its join: 8 tokens each 5.1 and 14 us, as tiles 5.6 and 10; 16 tokens 8.2 and
+//          18 against 5.7 and 10.)
+// Forward of 32 x 150 tokens, 20 heads of 64: 11 us, backward of 4 x 1333, 10 heads of 128: 17 + 4; their bytes would take 4 and 8.  Vector units are
+// busy a quarter of the time and memory at a third to half of its rate: a launch of few short workgroups, whose loads, sums and stores
+// follow one another.  Single tokens of 32 items into the cache: 3.9 us, the launch and one chain of loads.
 // An angle is position * freqs[i] as a part of a turn in double, of which only the fraction goes on in float: 500000 tokens into a
 // recording a float product would leave the angle to 1/30.
 #include "../../include/nm_head_norm.h"

@@ -5,6 +5,11 @@
 // (the new tokens of all heads that share keys and values), and the places are dealt to the rows such that a lane ends up with
 // those eight neighbouring places of its column that the second product wants from it: probabilities stay in the registers that they were
 // made in.  One pass with a running maximum and sum for each column.
+//
+// Measured (bfloat16): 32 sequences of 4000 to 8001 places, 2 shared heads of 128, one token each: 46 + 5 us for 197 MB (4.3 TB/s; 8 of them before
+// the first loads return and after the last).  4 x 500 tokens behind 3000 to 6000 places, 8 heads of 128 over 2: 64 + 9 us; the products alone
+// would take 22, the vector units (exponentials, maxima, packing) as long again, and a wavefront does one after the other.  One
+// sequence of 2000 places: 7 + 4 us, two launches of few workgroups.
 #include "../../include/nm_paged_attention.h"
 #include "token_ops.h"
 
@@ -16,7 +21,9 @@ constexpr float kLag = 8.f;      // powers of two that the base of the sums may 
 constexpr int kMaxSplits = 64;
 constexpr int kTile = 32;        // places that a wavefront looks at at a time
 constexpr int kWaves = 4;
-constexpr int kFewColumns = 32;  // that a workgroup reads the cache for by itself
+// columns that a workgroup reads the cache for by itself (8 sequences of 2000 places, 32 columns: 9.8 us against 10.4 for heads of 64, 14.0 against
+// 12.0 for 128, with probabilities in two terms; 48 columns 12.7 against 12.2)
+constexpr int kFewColumns = 32;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -678,7 +685,8 @@ __global__ __launch_bounds__(ROWS * 64) void paged_join_kernel(Paged a)
     store_rows<S, ROWS, 64>(a, tile, row0);
 }
 
-// The same for few splits and many tokens: a thread takes eight channels of a row, one split after the other.
+// The same for few splits and many tokens: a thread takes eight channels of a row, one split after the other.  (16000 rows of 4 splits: 9 us
+// against 15, for 37 MB.)
 constexpr int kFewSplits = 4, kJoinRows = 32;
 template <typename S>
 __global__ __launch_bounds__(kJoinRows * 16) void paged_join_few_kernel(Paged a)
@@ -729,10 +737,11 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, 
     p.blocks = columns > 16 ? 2 : 1;
     const int of_group = p.many ? kManyColumns : 16 * p.blocks, of_round = p.many ? kManyTile : kTile * kWaves;
     p.col_tiles = (int)((columns + of_group - 1) / of_group);
-    // workgroups share a token's places where there are fewer than two a CU, but look at two rounds of places at least.  (Shares of equal size
+    // workgroups share a token's places where there are fewer than two a CU (of few columns: one; two 49 us instead of 46 for 32 sequences of
+    // 4000 to 8000 places, one of many columns 83 instead of 64 for chunks of 500 tokens), but look at two rounds of places at least.  (Shares of equal size
     // whatever the sequences' lengths, which every workgroup and every row of the join has to find: 32 sequences of 4000 to 8000 places the same,
-    // chunks of 500 tokens 71 us and 31 for the join against 63 and 17.)
-    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = 512;
+    // those chunks 71 us and 31 for the join against 63 and 17 then.)
+    const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = p.many ? 512 : 256;
     long long splits = wanted / groups;
     if (splits > rounds / 2) splits = rounds / 2;
     if (splits > kMaxSplits) splits = kMaxSplits;

@@ -296,6 +296,8 @@ class AttentionDecoder:
         if run["at"] + tokens.shape[1] > run["room"]:
             raise ValueError("no room for so many tokens")
         w, heads = self.weights, {"heads": self.heads, "kv_heads": self.kv_heads}
+        if counts is not None:
+            counts = counts.clamp(0, tokens.shape[1])
         _, h = self._embed(tokens, 0, counts)
         run["filled"] += tokens.shape[1] if counts is None else counts
         _, n = nm.nm_residual_norm_fwd(h, next_weight=w["0.self.next"], next_bias=self._bias("0.self.next"), layer=self.layer_norm, lengths=counts)

@@ -8,7 +8,7 @@
 //
 // Measured (bfloat16): 32 sequences of 4000 to 8001 places, 2 shared heads of 128, one token each: 46 + 5 us for 197 MB (4.3 TB/s; 8 of them before
 // the first loads return and after the last).  4 x 500 tokens behind 3000 to 6000 places, 8 heads of 128 over 2: 64 + 9 us; the products alone
-// would take 22, the vector units (exponentials, maxima, packing) as long again, and a wavefront does one after the other.  One
+// would take 22; matrix pipes are busy 19 % of the time, vector units 21 and LDS 24, for a wavefront does one after the other.  One
 // sequence of 2000 places: 7 + 4 us, two launches of few workgroups.
 #include "../../include/nm_paged_attention.h"
 #include "token_ops.h"
@@ -86,7 +86,7 @@ __device__ __forceinline__ Column column_of(const Paged &a, int b, int m, int n,
     c.there = c.exists && c.u < n;
     const int at = len - n + c.u;
     c.hi = c.there ? max(0, min(at + 1, a.max_pages << a.log_page)) : 0;
-    c.lo = c.there && a.window ? max(0, at + 1 - a.window) : 0;
+    c.lo = c.there && a.window && a.window <= at ? at + 1 - a.window : 0;
     if (c.hi <= c.lo) c.there = false;
     return c;
 }

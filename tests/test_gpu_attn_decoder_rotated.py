@@ -145,6 +145,19 @@ def test_chunks_follow_the_teacher_forced_pass(dtype):
     assert torch.equal(ids.long(), want.indices[:, :3]) and torch.allclose(best, want.values[:, :3], atol=1e-5)
 
 
+def test_counts_beyond_a_chunk_are_its_width():
+    import torch
+    dec = make(dtype="f32", state_bits=32)
+    tokens, _, states, _, frames = batch(dec)
+    got = []
+    for counts in ([9, 0, 4], [100, -5, 4]):
+        run = dec.start(states, frames, 20, page=16)
+        first = dec.extend(tokens, run, torch.tensor(counts, dtype=torch.int32, device="cuda"))
+        got.append((first[0], first[2, :, :4], dec.next(tokens[:, 0], run)))
+        assert run["filled"].tolist() == [10, 1, 5]
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_training_in_low_precision_with_8_bit_states():
     import torch
     from paper_1909_09577_amd.attn_decoder import AttentionDecoder, spelled

@@ -21,7 +21,7 @@ def run_and_check(B, V, C, U, dtype, *, lengths=None, wide=True, tokens="any", s
     import torch
     r = np.random.default_rng(seed)
     ids = {"any": lambda: r.integers(0, V, (B, U)), "one": lambda: np.full((B, U), V - 1),
-           "outside": lambda: r.integers(-2, V + 2, (B, U)), "few": lambda: r.integers(0, max(1, V // 50), (B, U)) * 7 % V}[tokens]()
+           "outside": lambda: r.integers(-2, V + 2, (B, U)), "few": lambda: r.integers(0, max(1, V // 50), (B, U)) * 7 % V, "low": lambda: r.integers(0, 3, (B, U))}[tokens]()
     table, dout = (host(to(r.standard_normal(s), dtype)) for s in ((V, C), (B, C, U)))
     dev_ids = torch.from_numpy(ids).cuda().to(torch.int64 if wide else torch.int32)
     ln = lengths_on("cuda", lengths)
@@ -77,6 +77,11 @@ def test_accumulation(tokens):
 @pytest.mark.parametrize("tokens", ["any", "one", "few"])
 def test_more_places_than_a_sorting_workgroup_has_at_a_time(tokens):
     run_and_check(3, 5000, 8, 8100, "bf16", tokens=tokens, lengths=[8100, 8000, 4097])
+
+
+@pytest.mark.parametrize("V", [600, 20000])
+def test_more_places_of_some_tokens_than_a_list_holds(V):
+    run_and_check(3, V, 8, 5000, "bf16", tokens="low", lengths=[5000, 4999, 3])
 
 
 def test_infinities_and_nan_stay_with_their_token():

@@ -154,3 +154,21 @@ def test_offsets_beyond_32_bits():
     a, _ = nm.nm_paged_attn_fwd(many, k, v, table, n, heads=H, kv_heads=1)
     b, _ = nm.nm_paged_attn_fwd(many, ks, vs, small, n, heads=H, kv_heads=1)
     assert torch.equal(a, b) and torch.isfinite(a.float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[400, 37, 0], [1100, 33, 20], [70, 64, 40]], ids=str)
+@pytest.mark.parametrize("U", [16, 33])
+def test_joins_of_few_and_many_shares(U, lengths, dtype):
+    run_and_check(3, 4, 2, 48, U, dtype, 32, lengths)
+    run_and_check(3, 4, 1, 128, U, dtype, 16, lengths, q_lengths=[U, U - 1, 1])
+
+
+@pytest.mark.parametrize("U", [1, 40])
+def test_a_window_longer_than_anything(U):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn(*s, device="cuda", generator=g).bfloat16() for s in ((2, 4 * 32, U), (9, 2, 16, 32), (9, 2, 32, 16)))
+    table, lengths = ints([[0, 3, 5, 7], [8, 1, 2, 4]]), ints([60, U // 2])
+    want, got = (nm.nm_paged_attn_fwd(q, k, v, table, lengths, heads=4, kv_heads=2, window=w, want_lse=True) for w in (0, 2 ** 31 - 1))
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])

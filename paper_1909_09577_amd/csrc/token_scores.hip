@@ -13,7 +13,7 @@
 // Backward: element by element from the saved lse and entropy, a thread on the same eight places of every so many classes.
 //
 // Measured: 32 x 150 places of 5000 classes, four alternatives, bfloat16: 18 + 8 us; the scores that count, 36 MB, would take 7.  The vector units
-// are busy half of the time (an exponential, a maximum and two sums a score), and the join reads 32 lines of memory a place again.  16 single
+// are busy a third of the time (an exponential, a maximum and two sums a score), and the join reads 32 lines of memory a place again.  16 single
 // places of 32000 classes, eight alternatives, float32: 11 + 5 us, chains of exchanges between lanes.  Backward of 16 x 333 places of 5000
 // classes, float32 to bfloat16: 37 us for 160 MB, 4.3 TB/s.
 #include "../../include/nm_token_scores.h"

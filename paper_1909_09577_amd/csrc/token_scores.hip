@@ -135,18 +135,19 @@ struct List {  // the K largest, in order
     }
 };
 
-// The results of a place, but for its alternatives; the log-sum-exp
+// The results of a place, but for its alternatives; the log-sum-exp, in double until differences with it are made
 template <typename S>
-__device__ __forceinline__ float finish_sums(const ScoresFwd &a, int b, int u, bool there, const Sums &v)
+__device__ __forceinline__ double finish_sums(const ScoresFwd &a, int b, int u, bool there, const Sums &v)
 {
     const size_t at = (size_t)b * a.U + u;
-    const float log_s = __builtin_amdgcn_logf(v.s), lse = ((v.m == -INFINITY ? 0.f : v.m) + log_s) * kLn2;
-    if (a.lse) a.lse[at] = there ? lse : 0.f;
+    const float log_s = __builtin_amdgcn_logf(v.s);
+    const double lse = ((double)(v.m == -INFINITY ? 0.f : v.m) + log_s) * 0.69314718055994530942;
+    if (a.lse) a.lse[at] = there ? (float)lse : 0.f;
     if (a.entropy) a.entropy[at] = there && v.s != 0.f ? (log_s - v.t / v.s) * kLn2 : 0.f;
     if (a.logp) {
         const int target = there ? a.targets.at(at, a.V) : -1;
         const float z = target < 0 ? 0.f : load_as_f32((const S *)a.scores, ((size_t)b * a.V + target) * a.U + u);
-        a.logp[at] = target < 0 ? 0.f : (lse == -INFINITY ? lse : z - lse);
+        a.logp[at] = target < 0 ? 0.f : (float)(lse == -INFINITY ? lse : z - lse);
     }
     return lse;
 }
@@ -290,10 +291,10 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
     }
     if (K && lane < a.splits * K) mine = a.part_keys[(size_t)lane * all + at];
     for (int d = 1; d < a.splits; d <<= 1) st.join_lane(d);  // (to lane 0 all; lanes behind the last split have nothing to add)
-    float lse = 0.f;
+    double lse = 0.;
     if (lane == 0) lse = finish_sums<S>(a, b, u, there, st);
     if constexpr (K > 0) {
-        lse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lse)));
+        lse = __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(lse)), __builtin_amdgcn_readfirstlane(__double2loint(lse)));
         constexpr int kAll = K * G, kEach = (kAll + 63) / 64, kAtOnce = 64 / G;  // classes of all groups, of a lane; groups of 64 lanes
         const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + u;
         key_t found[kEach];
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
             if (there && found[e] != kEmpty && rank < a.top) {
                 const size_t to = ((size_t)b * a.top + rank) * a.U + u;
                 a.top_ids[to] = class_of(found[e]);
-                a.top_logp[to] = lse == -INFINITY ? lse : score_of(found[e]) - lse;
+                a.top_logp[to] = (float)(lse == -INFINITY ? lse : score_of(found[e]) - lse);
             }
         }
         if (!there && lane < a.top) {

@@ -13,8 +13,8 @@
 //          A frequent token's runs leave parts.
 //   join   adds the parts of such a token in order.
 // 16 x 1601 places, 32000 tokens of 512 channels, bfloat16: 25 + 15 + 9 us.  What has to move, 92 MB, would take 18; the turned copy of dout
-// and rows that are filled and then written again are half as much once more, the order alone takes 18 us beside them, and the join is what
-// its 3200 workgroups take to begin and to find that most have nothing to do.
+// and rows that are filled and then written again are half as much once more, the order alone takes 18 us beside them, and the join waits for
+// the 292 parts of the most frequent token (a quarter as many workgroups, four runs each, took 8 us, and of 32 x 150 places 5.5 instead of 4.2).
 #include "../../include/nm_embedding.h"
 #include "token_ops.h"
 

@@ -15,7 +15,7 @@
  * Conventions are those of nm_conv1d.h (device pointers the caller owns, one stream, enqueue only, argument errors before
  * any device call, deterministic results), with these additions:
  *  - dtype (NM_BF16 or NM_F32) is the storage type of q, o and the cache; lse is float.  Sums, maxima and probabilities are float32; in
- *    NM_BF16 mode probabilities enter the second product as bfloat16, of calls with up to 32 tokens times G as two such terms.
+ *    NM_BF16 mode probabilities enter the second product as two bfloat16 terms, off by 2^-16 of themselves.
  *  - q and o are [B][heads*D][U] with dense rows; *_stride is the distance of their batch items in elements.
  *  - lengths, q_lengths and page_table are int32; any values are taken: lengths below 0 are 0, q_lengths are clipped to [0,U].  Rows of the
  *    cache that no token of the call looks at are not used, whatever they hold (NaN included); the others have to be finite, and so has q at

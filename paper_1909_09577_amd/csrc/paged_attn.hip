@@ -7,8 +7,8 @@
 // made in.  One pass with a running maximum and sum for each column.
 //
 // Measured (bfloat16): 32 sequences of 4000 to 8001 places, 2 shared heads of 128, one token each: 46 + 5 us for 197 MB (4.3 TB/s; 8 of them before
-// the first loads return and after the last).  4 x 500 tokens behind 3000 to 6000 places, 8 heads of 128 over 2: 64 + 9 us; the products alone
-// would take 22; matrix pipes are busy 19 % of the time, vector units 21 and LDS 24, for a wavefront does one after the other.  One
+// the first loads return and after the last).  4 x 500 tokens behind 3000 to 6000 places, 8 heads of 128 over 2: 77 + 9 us; the products alone
+// would take 22, and those of the probabilities' second term half as much; a wavefront's products, exponentials and LDS reads follow one another.  One
 // sequence of 2000 places: 7 + 4 us, two launches of few workgroups.
 #include "../../include/nm_paged_attention.h"
 #include "token_ops.h"
@@ -21,8 +21,8 @@ constexpr float kLag = 8.f;      // powers of two that the base of the sums may 
 constexpr int kMaxSplits = 64;
 constexpr int kTile = 32;        // places that a wavefront looks at at a time
 constexpr int kWaves = 4;
-// columns that a workgroup reads the cache for by itself (8 sequences of 2000 places, 32 columns: 9.8 us against 10.4 for heads of 64, 14.0 against
-// 12.0 for 128, with probabilities in two terms; 48 columns 12.7 against 12.2)
+// columns that a workgroup reads the cache for by itself (8 sequences of 2000 places, 32 columns: 9.9 us against 11.5 for heads of 64, 13.8 against
+// 12.8 for 128; 48 columns 11.8 against 13.0 and 14.2 against 14.8, but for twice the reads of a cache that is here in the caches nearby)
 constexpr int kFewColumns = 32;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -558,7 +558,9 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
             mx = top;
         }
         const float base = mx == -INFINITY ? 0.f : mx;
-        Frag p[4];
+        // two bfloat16 terms: what one alone leaves, up to 2^-9 of a probability, is more than the result's own rounding where values cancel (error
+        // of chunks of 500 tokens against 64 bits 2.3e-3 with one term, 1.7e-3 with two, the result's rounding; 66 and 79 us)
+        Frag p0[4], p1[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             float e[8], part = 0.f;
@@ -568,14 +570,25 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(Paged a)
                 part += e[j];
             }
             sum += part;
-            const u32x4_t w = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
-            p[k] = __builtin_bit_cast(Frag, w);
+            u32x4_t hi, lo;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                hi[j] = pack_bf16x2(e[2 * j], e[2 * j + 1]);
+                lo[j] = pack_bf16x2(e[2 * j] - __uint_as_float(hi[j] << 16), e[2 * j + 1] - __uint_as_float(hi[j] & 0xffff0000u));
+            }
+            p0[k] = __builtin_bit_cast(Frag, hi);
+            p1[k] = __builtin_bit_cast(Frag, lo);
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
+            Frag v[ND];
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
-                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const Frag *>(vp + d * 32 * L::kPitchV + k * 32), p[k], acc[d], 0, 0, 0);
+            for (int d = 0; d < ND; ++d) v[d] = *reinterpret_cast<const Frag *>(vp + d * 32 * L::kPitchV + k * 32);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p1[k], acc[d], 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p0[k], acc[d], 0, 0, 0);
+        }
     };
     for (int t = t_begin, turn = 0; t < t_end; ++t, turn ^= 1) {
         unsigned char *buf = smem + turn * L::kBuffer;

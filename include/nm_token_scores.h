@@ -17,7 +17,8 @@
  * Conventions are those of nm_conv1d.h (device pointers the caller owns, one stream, enqueue only, argument errors before
  * any device call, deterministic results), with these additions:
  *  - dtype (NM_BF16 or NM_F32) is the storage type of scores; that of dscores is grad_dtype.  Everything else is float, sums too.  Scores are
- *    sums of anything: logits, or log-probabilities as nm_decoder_logsoftmax_fwd gives them.  +infinity gives NaN.
+ *    sums of anything, of any finite size: logits, or log-probabilities as nm_decoder_logsoftmax_fwd gives them.  +infinity gives NaN.  A
+ *    log-probability below float's range is -infinity.
  *  - targets [B][U]: int32 (target_bytes 4) or int64 (8).  lengths [B] int32, optional (NULL); any values are taken, clipped to [0,U].
  *    scores are not used at u >= lengths[b], whatever they hold.
  *  - top is at most 16 and at most V.

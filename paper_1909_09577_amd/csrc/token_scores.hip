@@ -1,7 +1,8 @@
 // Log-probabilities of given tokens, entropies, the likeliest classes, and the scores' gradient (definition: include/nm_token_scores.h).
 //
 // Forward: one pass over the scores with a running maximum m, s = sum exp(z - m) and t = sum exp(z - m) * (z - m), of which
-// lse = m + log s and entropy = log s - t/s, in powers of two throughout.  Places lie side by side in memory, so lanes are places (64 of
+// lse = m + log s and entropy = log s - t/s.  m is subtracted before anything is scaled to powers of two (0.4 us of 25 at 32 x 150 places of
+// 5000 classes): scores may be of any finite size, and places filled with a type's lowest value.  Places lie side by side in memory, so lanes are places (64 of
 // them, or fewer places times several classes); wavefronts, workgroups and spare lanes share the classes, and join what they found in pairs.
 //
 // The largest scores in order: a lane takes 16 neighbouring classes at a time and keeps a list of the largest maxima of eights of them (of all 16,
@@ -65,13 +66,16 @@ __device__ __forceinline__ key_t of_lane(key_t k, int lane)  // (the same lane f
     return (key_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
 }
 
+// A difference of scores in powers of two, a finite one (what it is an exponent of is zero long before)
+__device__ __forceinline__ float twos(float d) { return fmaxf(d * kLog2e, -1e30f); }
+
 struct Sums {
-    float m = -INFINITY, s = 0.f, t = 0.f;  // in powers of two
+    float m = -INFINITY, s = 0.f, t = 0.f;  // t in powers of two
     // sums are taken to `top` from here on
     __device__ __forceinline__ void rebase(float top)
     {
         if (s != 0.f) {
-            const float d = m - top, f = __builtin_amdgcn_exp2f(d);
+            const float d = twos(m - top), f = __builtin_amdgcn_exp2f(d);
             t = f * (t + d * s);
             s *= f;
         }
@@ -82,7 +86,7 @@ struct Sums {
         const float top = fmaxf(m, om);
         if (m < top) rebase(top);
         if (om < top && os != 0.f) {
-            const float d = om - top, f = __builtin_amdgcn_exp2f(d);
+            const float d = twos(om - top), f = __builtin_amdgcn_exp2f(d);
             ot = f * (ot + d * os);
             os *= f;
         }
@@ -135,19 +139,27 @@ struct List {  // the K largest, in order
     }
 };
 
-// The results of a place, but for its alternatives; the log-sum-exp, in double until differences with it are made
+// A place's log-sum-exp in two parts, the largest score and the logarithm of the sum: together they would leave nothing of the latter where scores
+// are large.  Differences with it are made in double.
+struct Lse {
+    float m, log_s;  // (0 and -infinity where nothing is left)
+    __device__ __forceinline__ double log_sum() const { return (double)log_s * 0.69314718055994530942; }
+    __device__ __forceinline__ double whole() const { return (double)m + log_sum(); }
+    __device__ __forceinline__ float logq(float z) const { return log_s == -INFINITY ? -INFINITY : (float)(((double)z - m) - log_sum()); }
+};
+
+// The results of a place, but for its alternatives
 template <typename S>
-__device__ __forceinline__ double finish_sums(const ScoresFwd &a, int b, int u, bool there, const Sums &v)
+__device__ __forceinline__ Lse finish_sums(const ScoresFwd &a, int b, int u, bool there, const Sums &v)
 {
     const size_t at = (size_t)b * a.U + u;
-    const float log_s = __builtin_amdgcn_logf(v.s);
-    const double lse = ((double)(v.m == -INFINITY ? 0.f : v.m) + log_s) * 0.69314718055994530942;
-    if (a.lse) a.lse[at] = there ? (float)lse : 0.f;
-    if (a.entropy) a.entropy[at] = there && v.s != 0.f ? (log_s - v.t / v.s) * kLn2 : 0.f;
+    const Lse lse = {v.m == -INFINITY ? 0.f : v.m, __builtin_amdgcn_logf(v.s)};  // (powers of two)
+    if (a.lse) a.lse[at] = there ? (float)lse.whole() : 0.f;
+    if (a.entropy) a.entropy[at] = there && v.s != 0.f ? (lse.log_s - v.t / v.s) * kLn2 : 0.f;
     if (a.logp) {
         const int target = there ? a.targets.at(at, a.V) : -1;
         const float z = target < 0 ? 0.f : load_as_f32((const S *)a.scores, ((size_t)b * a.V + target) * a.U + u);
-        a.logp[at] = target < 0 ? 0.f : (float)(lse == -INFINITY ? lse : z - lse);
+        a.logp[at] = target < 0 ? 0.f : lse.logq(z);
     }
     return lse;
 }
@@ -179,12 +191,12 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
 #pragma unroll
                 for (int i = 1; i < G; ++i) best[h] = fmaxf(best[h], z[G * h + i]);
             }
-            const float top = fmaxf(best[0], best[kGroups - 1]) * kLog2e;
+            const float top = fmaxf(best[0], best[kGroups - 1]);
             if (top > st.m) st.rebase(top);
             const float base = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const float y = __builtin_fmaf(z[i], kLog2e, -base), e = __builtin_amdgcn_exp2f(y);
+                const float y = (z[i] - base) * kLog2e, e = __builtin_amdgcn_exp2f(y);
                 st.s += e;
                 st.t = __builtin_fmaf(e, fmaxf(y, -1e30f), st.t);  // (zero times what is barred)
             }
@@ -291,10 +303,11 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
     }
     if (K && lane < a.splits * K) mine = a.part_keys[(size_t)lane * all + at];
     for (int d = 1; d < a.splits; d <<= 1) st.join_lane(d);  // (to lane 0 all; lanes behind the last split have nothing to add)
-    double lse = 0.;
+    Lse lse = {0.f, 0.f};
     if (lane == 0) lse = finish_sums<S>(a, b, u, there, st);
     if constexpr (K > 0) {
-        lse = __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(lse)), __builtin_amdgcn_readfirstlane(__double2loint(lse)));
+        lse.m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lse.m)));
+        lse.log_s = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lse.log_s)));
         constexpr int kAll = K * G, kEach = (kAll + 63) / 64, kAtOnce = 64 / G;  // classes of all groups, of a lane; groups of 64 lanes
         const S *column = (const S *)a.scores + (size_t)b * a.V * a.U + u;
         key_t found[kEach];
@@ -323,7 +336,7 @@ __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
             if (there && found[e] != kEmpty && rank < a.top) {
                 const size_t to = ((size_t)b * a.top + rank) * a.U + u;
                 a.top_ids[to] = class_of(found[e]);
-                a.top_logp[to] = (float)(lse == -INFINITY ? lse : score_of(found[e]) - lse);
+                a.top_logp[to] = lse.logq(score_of(found[e]));
             }
         }
         if (!there && lane < a.top) {

@@ -45,7 +45,8 @@ int nm_token_scores_fwd(int B, int V, int U, const void *scores, const void *tar
                         float *logp, float *entropy, float *lse, int *top_ids, float *top_logp, int dtype, void *workspace,
                         size_t workspace_bytes, void *hip_stream);
 
-/* Backward.  lse and entropy as the forward pass gave them (entropy is read only with dentropy); dlogp with targets, dentropy: one of
+/* Backward.  lse and entropy as the forward pass gave them (entropy is read only with dentropy; up to a magnitude of 4096 q has lse's rounding,
+ * beyond that the call sums over the classes again, once for each workgroup that has such a place); dlogp with targets, dentropy: one of
  * them at least.  dscores [B][V][U] out, written whole. */
 int nm_token_scores_bwd(int B, int V, int U, const void *scores, const void *targets, int target_bytes, const int *lengths,
                         const float *lse, const float *entropy, const float *dlogp, const float *dentropy, void *dscores, int dtype,

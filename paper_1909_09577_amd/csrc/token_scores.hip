@@ -174,7 +174,8 @@ __global__ __launch_bounds__(256, K > 8 ? 2 : 4) void scores_fwd_kernel(ScoresFw
     const int others = a.B * a.splits, ut = blockIdx.x / others, rest = blockIdx.x - ut * others, split = rest % a.splits, b = rest / a.splits;
     const int lanes = 1 << a.log_lanes, u = ut * lanes + (lane & (lanes - 1)), step = 64 >> a.log_lanes;
     const int len = length_in(a.len, b, a.U);
-    const int c0 = (split * 4 + wave) * a.per, c1 = min(a.V, c0 + a.per);
+    // (the last wavefronts' shares may end beyond 2^31)
+    const int c0 = (int)min((long long)(split * 4 + wave) * a.per, (long long)a.V), c1 = (int)min((long long)c0 + a.per, (long long)a.V);
     const bool there = u < len;
     Sums st;
     List<K> list;

@@ -1,0 +1,32 @@
+"""The calls on tokens at sizes whose offsets and launches do not fit 32 bits, against torch in float64 (of the largest ones on parts)."""
+import math
+
+import pytest
+
+from paper_1909_09577_amd import binding as nm
+
+pytestmark = pytest.mark.gpu
+u_ = 2.0 ** -24
+
+
+@pytest.mark.parametrize("top", [0, 1, 3])
+def test_scores_of_as_many_classes_as_there_may_be(top):
+    """All but the last ones are barred: the sum is their number, which float32 holds exactly, so what is left are the roundings of a logarithm
+    and of the result (2 units of a number below 16 each)."""
+    import torch
+    V, n = 2 ** 31 - 2 ** 16 - 1, 8_000_000
+    z = torch.full((1, V, 1), -math.inf, device="cuda", dtype=torch.bfloat16)
+    z[0, V - n:] = 0.0
+    target = torch.tensor([[V - 5]], device="cuda")
+    of = nm.nm_token_scores_fwd(z, target, top=top)
+    tol = 4 * 16 * u_
+    for name, want in (("lse", math.log(n)), ("entropy", math.log(n)), ("logp", -math.log(n))):
+        assert abs(of[name].item() - want) <= tol, name
+    if top:
+        assert of["top_ids"].flatten().tolist() == list(range(V - n, V - n + top))
+        assert (of["top_logp"] + math.log(n)).abs().max().item() <= tol
+        return
+    g = nm.nm_token_scores_bwd(z, target, of["lse"], None, torch.ones(1, 1, device="cuda"))
+    assert abs(g[0, V - 5, 0].item() - 1) <= 2.0 ** -8 and not g[0, :V - n].any()
+    g[0, V - 5] = -1 / n
+    assert (g[0, V - n:].float() * n + 1).abs().max().item() <= 2.0 ** -8 + 20 * u_

@@ -359,9 +359,9 @@ Plan plan_of(int B, int V, int U, int top)
 {
     Plan p = {};
     // places side by side: as many as there are, and of long rows 32 where the last 64 would be less than half full (32 x 150 places: 27 us for both
-    // launches, 29 with 64)
+    // launches, 29 with 64), but not from 2^24 places on: a lane's first class lies up to 16 rows behind a wavefront's, in bytes of 32 bits
     while (p.log_lanes < 6 && (1 << p.log_lanes) < U) ++p.log_lanes;
-    if (U > 32 && U % 64 > 0 && U % 64 <= 32) p.log_lanes = 5;
+    if (U > 32 && U < 1 << 24 && U % 64 > 0 && U % 64 <= 32) p.log_lanes = 5;
     const int lanes = 1 << p.log_lanes, step = 64 >> p.log_lanes, list = list_of(top);
     p.u_tiles = (U + lanes - 1) / lanes;
     // four workgroups a CU (32 x 150 places of 5000 classes 18.3 us, with two 20.6), but a wavefront has a whole round of classes to do, and a

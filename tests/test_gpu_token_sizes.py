@@ -30,3 +30,18 @@ def test_scores_of_as_many_classes_as_there_may_be(top):
     assert abs(g[0, V - 5, 0].item() - 1) <= 2.0 ** -8 and not g[0, :V - n].any()
     g[0, V - 5] = -1 / n
     assert (g[0, V - n:].float() * n + 1).abs().max().item() <= 2.0 ** -8 + 20 * u_
+
+
+def test_scores_of_rows_whose_offsets_pass_32_bits():
+    """Sixteen rows of 67 million places are more than 2^32 bytes.  Tolerance: 32 terms, exponents of at most 20 in powers of two, two units of each."""
+    import torch
+    V, U = 32, 67108832
+    z = torch.randn(1, V, U, device="cuda")
+    of = nm.nm_token_scores_fwd(z)
+    for u0 in range(0, U, 1 << 22):
+        part = z[0, :, u0:u0 + (1 << 22)].double()
+        lse = torch.logsumexp(part, 0)
+        assert (of["lse"][0, u0:u0 + (1 << 22)] - lse).abs().max().item() <= (V + 64) * u_ + 16 * 4 * u_, u0
+        x = part - lse
+        entropy = -(x.exp() * x).sum(0)
+        assert (of["entropy"][0, u0:u0 + (1 << 22)] - entropy).abs().max().item() <= 3 * (V + 72) * u_ * 10, u0

@@ -290,7 +290,8 @@ __device__ __forceinline__ int rank_of(key_t k, key_t others, int n)
 template <typename S, int K>
 __global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
 {
-    const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = a.B * a.U;
+    const int lane = threadIdx.x & 63, all = a.B * a.U;
+    const int at = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (at >= all) return;
     const int b = at / a.U, u = at - b * a.U;
     const bool there = u < length_in(a.len, b, a.U);
@@ -388,7 +389,9 @@ hipError_t run_list(const ScoresFwd &a, hipStream_t s)
     scores_fwd_kernel<S, K><<<dim3((unsigned)a.B * a.u_tiles * a.splits), dim3(256), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (K == 0 && a.splits == 1)) return e;
-    scores_join_kernel<S, K><<<dim3((unsigned)(((long long)a.B * a.U + 3) / 4)), dim3(256), 0, s>>>(a);
+    // (a grid's side has fewer than 2^32 work items; there are fewer than 2^29 places)
+    const unsigned joins = (unsigned)(((long long)a.B * a.U + 3) / 4), side = joins < 1u << 22 ? joins : 1u << 22;
+    scores_join_kernel<S, K><<<dim3(side, (joins + side - 1) / side), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename S>
@@ -576,7 +579,7 @@ int check(int B, int V, int U, int dtype)
     if (B <= 0 || V <= 0 || U <= 0 || !known_dtype(dtype)) return NM_ERR_BAD_ARG;
     const long long most = (1LL << 31) - 1;
     if ((long long)B * V > most / U || V > most - (1 << 16) || U > 1 << 29) return NM_ERR_UNSUPPORTED;  // (classes behind the last one are counted too)
-    // the grids, below 2^32 work items: a workgroup of the backward pass has 2048 elements, or one item's rest
+    // the grids, below 2^32 work items (the join's has a second side): a workgroup of the backward pass has 2048 elements, or one item's rest
     if ((long long)B * ((U + 63) / 64) >= 1LL << 23 || (long long)B * (((long long)V * U + 2047) / 2048) >= 1LL << 24) return NM_ERR_UNSUPPORTED;
     return NM_OK;
 }

@@ -45,3 +45,18 @@ def test_scores_of_rows_whose_offsets_pass_32_bits():
         x = part - lse
         entropy = -(x.exp() * x).sum(0)
         assert (of["entropy"][0, u0:u0 + (1 << 22)] - entropy).abs().max().item() <= 3 * (V + 72) * u_ * 10, u0
+
+
+def test_alternatives_of_more_places_than_a_launch_has_wavefronts():
+    """72 million places: each place's join is a wavefront's."""
+    import torch
+    B, V, U, top = 1024, 29, 70000, 4
+    z = torch.randn(B, V, U, device="cuda", dtype=torch.bfloat16)
+    of = nm.nm_token_scores_fwd(z, top=top, out={"top_ids": torch.full((B, top, U), -7, dtype=torch.int32, device="cuda")})
+    assert of["top_ids"].min().item() >= 0
+    for b in (0, 500, 958, 959, B - 1):
+        best, ids = z[b].float().sort(dim=0, descending=True, stable=True)
+        lse = torch.logsumexp(z[b].double(), 0)
+        assert torch.equal(of["top_ids"][b].long(), ids[:top]), b
+        assert (of["lse"][b] - lse).abs().max().item() <= (V + 64) * u_ + 16 * 4 * u_, b
+        assert (of["top_logp"][b] - (best[:top].double() - lse)).abs().max().item() <= (V + 64) * u_ + 16 * 8 * u_, b

@@ -288,10 +288,10 @@ __device__ __forceinline__ int rank_of(key_t k, key_t others, int n)
 // A wavefront joins what `splits` workgroups found of a place.  A lane has one of their lists' entries, and finds its place in order by
 // comparing it with all others; then one of the classes of the K eights that come first, read again, and the same.
 template <typename S, int K>
-__global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a)
+__global__ __launch_bounds__(256) void scores_join_kernel(ScoresFwd a, int first)
 {
     const int lane = threadIdx.x & 63, all = a.B * a.U;
-    const int at = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at = (first + (int)blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (at >= all) return;
     const int b = at / a.U, u = at - b * a.U;
     const bool there = u < length_in(a.len, b, a.U);
@@ -389,10 +389,7 @@ hipError_t run_list(const ScoresFwd &a, hipStream_t s)
     scores_fwd_kernel<S, K><<<dim3((unsigned)a.B * a.u_tiles * a.splits), dim3(256), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (K == 0 && a.splits == 1)) return e;
-    // (a grid's side has fewer than 2^32 work items; there are fewer than 2^29 places)
-    const unsigned joins = (unsigned)(((long long)a.B * a.U + 3) / 4), side = joins < 1u << 22 ? joins : 1u << 22;
-    scores_join_kernel<S, K><<<dim3(side, (joins + side - 1) / side), dim3(256), 0, s>>>(a);
-    return hipGetLastError();
+    return in_launches(((size_t)a.B * a.U + 3) / 4, [&](unsigned n, int first) { scores_join_kernel<S, K><<<dim3(n), dim3(256), 0, s>>>(a, first); });
 }
 template <typename S>
 hipError_t run_fwd(const ScoresFwd &a, hipStream_t s)
@@ -579,7 +576,7 @@ int check(int B, int V, int U, int dtype)
     if (B <= 0 || V <= 0 || U <= 0 || !known_dtype(dtype)) return NM_ERR_BAD_ARG;
     const long long most = (1LL << 31) - 1;
     if ((long long)B * V > most / U || V > most - (1 << 16) || U > 1 << 29) return NM_ERR_UNSUPPORTED;  // (classes behind the last one are counted too)
-    // the grids, below 2^32 work items (the join's has a second side): a workgroup of the backward pass has 2048 elements, or one item's rest
+    // the grids, below 2^32 work items (the join has several where need be): a workgroup of the backward pass has 2048 elements, or one item's rest
     if ((long long)B * ((U + 63) / 64) >= 1LL << 23 || (long long)B * (((long long)V * U + 2047) / 2048) >= 1LL << 24) return NM_ERR_UNSUPPORTED;
     return NM_OK;
 }

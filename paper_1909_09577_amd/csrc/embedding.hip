@@ -194,7 +194,7 @@ __device__ __forceinline__ void tokens_at(const EmbedBwd &a, int p0, int lane, i
 // there, and from what the wavefronts before it counted knows where its places go.  (Every eighth token to a wavefront, one after the other: the
 // order of 25616 places took 25 us instead of 18, because a frequent token's wavefront went through the whole list.)  Where the list is too
 // short for all, it is made again for the next ones.
-__device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
+__device__ void sort_range(const EmbedBwd &a, int which, unsigned char *smem)
 {
     int *count = reinterpret_cast<int *>(smem);                    // [kRange]
     int *begin = count + kRange;                                   // [kRange]
@@ -204,7 +204,7 @@ __device__ void sort_range(const EmbedBwd &a, unsigned char *smem)
     int *place = sums + 3 * kWaves;                                // [kList]
     uint16_t *bin = reinterpret_cast<uint16_t *>(place + kList);   // [kList]
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int v0 = blockIdx.x * a.range, bins = min(a.range, a.V - v0), chunks = (a.N - 1) / kChunk + 1;
+    const int v0 = which * a.range, bins = min(a.range, a.V - v0), chunks = (a.N - 1) / kChunk + 1;
     const uint64_t lower = (1ull << lane) - 1;
     for (int r = t; r < bins; r += kThreads) count[r] = 0;
     // the range's places that are number w0 .. w0+kList-1 among them go into the list; returns how many there are in all
@@ -376,13 +376,13 @@ __device__ void turn_tile(const EmbedBwd &a, int tile, unsigned char *smem)
 constexpr int kSortBytes = kList * 6 + (3 + kWaves) * kRange * 4 + 3 * kWaves * 4;
 
 template <typename S>
-__global__ __launch_bounds__(kThreads, 6) void embed_order_kernel(EmbedBwd a)
+__global__ __launch_bounds__(kThreads, 6) void embed_order_kernel(EmbedBwd a, int first)
 {
     __shared__ __align__(16) unsigned char smem[kSortBytes];
     static_assert(Turn<S>::kBytes <= kSortBytes, "");
-    int w = blockIdx.x;
+    int w = first + blockIdx.x;
     if (w < a.sorters) {
-        sort_range(a, smem);
+        sort_range(a, w, smem);
         return;
     }
     w -= a.sorters;
@@ -458,13 +458,14 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a, int c_waves)
 }
 
 // The token that begins in a run and goes beyond it: its parts in order, a wavefront every eighth of them
-__global__ __launch_bounds__(512) void embed_join_kernel(EmbedBwd a, int c_waves)
+__global__ __launch_bounds__(512) void embed_join_kernel(EmbedBwd a, int c_waves, int first)
 {
     __shared__ float sums[7][8][64];
-    const int run = blockIdx.x / c_waves, i0 = run * kRun;
+    const uint32_t at = first + blockIdx.x;
+    const int run = at / c_waves, i0 = run * kRun;
     const Entry e = a.order[i0 + kRun - 1];
     if (i0 + kRun >= *a.total || e.from < i0 || e.to <= i0 + kRun) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.x - run * c_waves) * 512 + lane * 8, n = a.C - c;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (at - run * c_waves) * 512 + lane * 8, n = a.C - c;
     const int last = (e.to - 1) / kRun;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -508,15 +509,14 @@ template <typename S>
 hipError_t run_bwd(EmbedBwd a, int runs, hipStream_t s)
 {
     const size_t fillers = a.add ? 0 : ((size_t)a.V * a.C + kFill - 1) / kFill;
-    embed_order_kernel<S><<<dim3((unsigned)(a.sorters + a.turners + fillers)), dim3(kThreads), 0, s>>>(a);
-    hipError_t e = hipGetLastError();
+    hipError_t e = in_launches((size_t)a.sorters + a.turners + fillers,
+                               [&](unsigned n, int first) { embed_order_kernel<S><<<dim3(n), dim3(kThreads), 0, s>>>(a, first); });
     if (e != hipSuccess) return e;
     const int c_waves = (a.C + 511) / 512;
     embed_sum_kernel<S><<<dim3((unsigned)(((long long)runs * c_waves + 3) / 4)), dim3(256), 0, s>>>(a, c_waves);
     e = hipGetLastError();
     if (e != hipSuccess || runs == 1) return e;
-    embed_join_kernel<<<dim3((unsigned)(runs - 1) * c_waves), dim3(512), 0, s>>>(a, c_waves);
-    return hipGetLastError();
+    return in_launches((size_t)(runs - 1) * c_waves, [&](unsigned n, int first) { embed_join_kernel<<<dim3(n), dim3(512), 0, s>>>(a, c_waves, first); });
 }
 
 int check(int B, int V, int C, int U, int id_bytes, float scale, int dtype)
@@ -524,7 +524,8 @@ int check(int B, int V, int C, int U, int id_bytes, float scale, int dtype)
     if (B <= 0 || V <= 0 || C <= 0 || U <= 0 || (id_bytes != 4 && id_bytes != 8) || !finite_float(scale) || !known_dtype(dtype)) return NM_ERR_BAD_ARG;
     const long long most = (1LL << 31) - 1;
     if ((long long)B * U > most / C || (long long)B * U > most - (1 << 14) || (long long)V * C > most) return NM_ERR_UNSUPPORTED;  // (places behind the last one are counted too)
-    // the grids, below 2^32 work items: tiles of 64 x 64 (an item's last ones may be all but empty), and what is filled
+    // what goes in one launch, below 2^32 work items: the forward pass has 256 for a tile of 64 x 64 (an item's last ones may be all but empty), the
+    // gradient's sums a wavefront for eight places and 512 channels, eight for a tile at most
     if ((long long)B * ((U + 63) / 64) * ((C + 63) / 64) >= 1LL << 23 || B > 65535) return NM_ERR_UNSUPPORTED;
     return NM_OK;
 }

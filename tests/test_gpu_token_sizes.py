@@ -60,3 +60,42 @@ def test_alternatives_of_more_places_than_a_launch_has_wavefronts():
         assert torch.equal(of["top_ids"][b].long(), ids[:top]), b
         assert (of["lse"][b] - lse).abs().max().item() <= (V + 64) * u_ + 16 * 4 * u_, b
         assert (of["top_logp"][b] - (best[:top].double() - lse)).abs().max().item() <= (V + 64) * u_ + 16 * 8 * u_, b
+
+
+def gradient_of(dout, ids, V):
+    """The table's gradient from the places that have a token, in float64, and the sums of the terms' magnitudes and how often tokens occur."""
+    import torch
+    B, C, U = dout.shape
+    b, u = (ids >= 0).nonzero(as_tuple=True)
+    rows, to = dout.permute(0, 2, 1)[b, u].double(), ids[b, u]
+    zeros = lambda: torch.zeros(V, C, dtype=torch.float64, device="cuda")  # noqa: E731
+    return zeros().index_add_(0, to, rows), zeros().index_add_(0, to, rows.abs()), torch.bincount(to, minlength=V)
+
+
+@pytest.mark.parametrize("dtype, B, U, C, V, share", [("bf16", 1024, 65600, 16, 29, 1e-4), ("f32", 65535, 2, 8192, 1000, 0.2)], ids=["runs", "tiles"])
+def test_an_embedding_gradient_of_more_workgroups_than_a_launch_may_have(dtype, B, U, C, V, share):
+    """More than 2^26 places' joins; more tiles to turn, ranges and rows to fill than 2^23.  A share of the places has a token.  Tolerance: a
+    rounding for each term and the result."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dout = torch.randn(B, C, U, device="cuda", generator=g, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    ids = torch.randint(0, V, (B, U), device="cuda", generator=g)
+    ids[torch.rand(B, U, device="cuda", generator=g) > share] = -1
+    ids[-1, -1], ids[0, 0], ids[-1, 0] = V - 1, 0, 3
+    ids[B // 2] = torch.where(torch.arange(U, device="cuda") < 100, 7, ids[B // 2])
+    got = nm.nm_embedding_bwd(dout, ids, V)
+    ref, mag, count = gradient_of(dout, ids, V)
+    assert ((got - ref).abs() <= (count + 2)[:, None] * u_ * mag).all()
+
+
+def test_a_large_accumulated_embedding_gradient_keeps_the_other_rows():
+    import torch
+    B, U, C, V = 65535, 2, 8192, 400
+    dout = torch.ones(B, C, U, device="cuda")
+    ids = torch.full((B, U), -1, device="cuda")
+    ids[5, 1], ids[-1, 0] = 17, 399
+    dtable = torch.randn(V, C, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    want = dtable.clone()
+    want[17] += 1
+    want[399] += 1
+    assert torch.equal(nm.nm_embedding_bwd(dout, ids, V, dtable=dtable, accumulate=True), want)

@@ -252,14 +252,15 @@ class AttentionDecoder:
     # ---- decoding -----------------------------------------------------------------------------------
     def start(self, states, state_lengths, room, page=64):
         """What the tokens of a batch of utterances need: every layer's keys and values of the states, and room for those of `room`
-        tokens (channel-major, a token's column is filled when it is known; with rotated positions in pages of `page` tokens)."""
+        tokens of each utterance (channel-major, a token's column is filled when it is known; with rotated positions in pages of `page` tokens, all
+        of them set aside here)."""
         import torch
         B, width = states.shape[0], 2 * self.kv_heads * self.dim
         if self.rotated:
             each = -(-room // page)
             empty = lambda *shape: [torch.empty(B * each, self.kv_heads, *shape, dtype=self.dtype, device=self.device) for _ in range(self.layers)]  # noqa: E731
             return {"kv": [_conv(states, self.weights[f"{l}.cross.states"]) for l in range(self.layers)], "state_lengths": state_lengths, "at": 0, "room": room,
-                    "k": empty(page, self.dim), "v": empty(self.dim, page), "filled": torch.zeros(B, dtype=torch.int32, device=self.device),
+                    "ragged": False, "k": empty(page, self.dim), "v": empty(self.dim, page), "filled": torch.zeros(B, dtype=torch.int32, device=self.device),
                     "pages": torch.arange(B * each, dtype=torch.int32, device=self.device).view(B, each)}
         return {"kv": [_conv(states, self.weights[f"{l}.cross.states"]) for l in range(self.layers)], "state_lengths": state_lengths, "at": 0, "room": room,
                 "cache": [torch.empty(B, width, room, dtype=self.dtype, device=self.device) for _ in range(self.layers)],
@@ -267,10 +268,10 @@ class AttentionDecoder:
 
     def next(self, tokens, run):
         """Log-probabilities [B, vocab] of what follows the tokens int64 [B], the latest of every utterance."""
-        if run["at"] >= run["room"]:
-            raise ValueError("no room for another token")
         if self.rotated:
             return self.extend(tokens[:, None], run)[:, :, 0]
+        if run["at"] >= run["room"]:
+            raise ValueError("no room for another token")
         w, heads = self.weights, {"heads": self.heads, "kv_heads": self.kv_heads}
         _, h = self._embed(tokens[:, None], run["at"])
         run["filled"] += 1
@@ -290,14 +291,18 @@ class AttentionDecoder:
 
     def extend(self, tokens, run, counts=None):
         """Log-probabilities [B, vocab, U] of what follows each of the new tokens int64 [B, U], of which an utterance has the first counts[b]
-        (int32 [B]; None: all; what comes back behind them says nothing).  With rotated positions."""
+        (int32 [B]; None: all; what comes back behind them says nothing).  With rotated positions.  The fullest utterance's tokens have to find
+        room; after chunks with counts the device is asked how many those are, where the chunks' widths together pass the room."""
         if not self.rotated:
             raise ValueError("chunks of tokens need rotated positions")
-        if run["at"] + tokens.shape[1] > run["room"]:
-            raise ValueError("no room for so many tokens")
         w, heads = self.weights, {"heads": self.heads, "kv_heads": self.kv_heads}
         if counts is not None:
             counts = counts.clamp(0, tokens.shape[1])
+        at = run["at"] + tokens.shape[1]  # of the fullest utterance, or more
+        if at > run["room"] and (run["ragged"] or counts is not None):
+            at = int((run["filled"] + (tokens.shape[1] if counts is None else counts)).max())
+        if at > run["room"]:
+            raise ValueError("no room for so many tokens")
         _, h = self._embed(tokens, 0, counts)
         run["filled"] += tokens.shape[1] if counts is None else counts
         _, n = nm.nm_residual_norm_fwd(h, next_weight=w["0.self.next"], next_bias=self._bias("0.self.next"), layer=self.layer_norm, lengths=counts)
@@ -309,7 +314,7 @@ class AttentionDecoder:
             o, _ = nm.nm_cross_attn_fwd(_conv(n, w[f"{l}.cross.in"]), *self._split(run["kv"][l])[1:], lengths=run["state_lengths"], q_lengths=counts, **heads)
             h, n = self._around(l, "cross", h, _conv(o, w[f"{l}.cross.out"]), counts)
             h, n = self._around(l, "ffn", h, _conv(_conv(n, w[f"{l}.ffn.in"], relu=True), w[f"{l}.ffn.out"]), counts)
-        run["at"] += tokens.shape[1]
+        run["at"], run["ragged"] = at, run["ragged"] or counts is not None
         return nm.nm_decoder_logsoftmax_fwd(n, w["classes"][:, :, 0], w["classes_bias"])
 
     def best(self, logp, count):

@@ -1043,13 +1043,9 @@ def nm_head_norm_bwd(dout, x, *, heads, kv_heads, norm=True, q_weight=None, k_we
     if dx is None:
         dx = x.new_empty((B, C, U))
     dp, ds = _item_ptr(dx, x.dtype, (B, C, U), "dx")
-    if q_weight is None:
-        dq_weight = None
-    elif dq_weight is None:
+    if q_weight is not None and dq_weight is None:
         dq_weight = torch.empty_like(q_weight)
-    if k_weight is None:
-        dk_weight = None
-    elif dk_weight is None:
+    if k_weight is not None and dk_weight is None:
         dk_weight = torch.empty_like(k_weight)
     need = 0 if q_weight is None and k_weight is None else nm_head_norm_bwd_workspace_bytes(B, heads, kv_heads, D, U, code)
     ws, ws_ptr, ws_bytes = _workspace_of(need, workspace, x, stream)

@@ -1,8 +1,9 @@
 // Lookup of tokens' embeddings and its gradient (definition: include/nm_embedding.h).
 //
 // Forward: a table's rows run over the channels, activations over the tokens, so a workgroup carries 64 tokens x 64 channels across LDS and
-// reads and writes 128-byte pieces.  Calls of few tokens an item are copied element by element (32 items, 1024 channels: of 12 tokens each 4.0 us
-// against 4.4 as tiles, of 24 5.0 against 4.3).  Single tokens of 32 items: 2.5 us, the launch.
+// reads and writes 128-byte pieces.  Calls of few tokens an item are copied element by element (32 items, 1024 channels, bfloat16: of 8 and 12 tokens
+// each 3.9 us against 4.3 and 4.5 as tiles, of 24 4.9 against 4.6; 4 items of 256 channels: of 12 tokens 3.8 against 4.0; 32 items of 512 channels in float32: of 12
+// tokens 4.2 against 3.9, of 24 4.5 against 3.8).  Single tokens of 32 items: 2.5 us, the launch.
 //
 // Gradient: a sum over the places of each token, which has to come out the same every time, so the places are sorted by token, without
 // atomics on sums.  Three launches:
@@ -13,8 +14,9 @@
 //          A frequent token's runs leave parts.
 //   join   adds the parts of such a token in order.
 // 16 x 1601 places, 32000 tokens of 512 channels, bfloat16: 25 + 15 + 9 us.  What has to move, 92 MB, would take 18; the turned copy of dout
-// and rows that are filled and then written again are half as much once more, the order alone takes 18 us beside them, and the join waits for
-// the 292 parts of the most frequent token (a quarter as many workgroups, four runs each, took 8 us, and of 32 x 150 places 5.5 instead of 4.2).
+// and rows that are filled and then written again are half as much once more, the order alone takes 18 us beside them.  Of the
+// join's 9 us its 3200 workgroups take 7 that find no token to join (as where all tokens are equally likely); the 214 parts of the most frequent token do
+// not hold it up (the same without that token).  A quarter as many workgroups, four runs each, took 8 us, and of 32 x 150 places 5.5 instead of 4.2.
 #include "../../include/nm_embedding.h"
 #include "token_ops.h"
 

@@ -399,6 +399,8 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, bool back)
     Plan p = {};
     p.tiles = U >= 8;
     p.u_tiles = (U + 8 * kGroups - 1) / (8 * kGroups);
+    // forward and backward with its join, of 32 x 150 tokens (10 heads of 96) and 4 x 1333 (10 of 128): with four heads a workgroup 11.2 and 20, 12 and 22 us, with
+    // two 9.7 and 19, 11 and 23 (20 heads of 64: 11.0 and 21, 11.4 and 25), with eight 13 and 23, 14 and 26
     p.heads_each = 4;
     const long long work = p.tiles ? (long long)B * p.u_tiles : ((long long)B * U + 3) / 4;
     const long long side = p.tiles ? (work + 7) / 8 * 8 : work;

@@ -8,8 +8,10 @@
 //
 // Measured (bfloat16): 32 sequences of 4000 to 8001 places, 2 shared heads of 128, one token each: 46 + 5 us for 197 MB (4.3 TB/s; 8 of them before
 // the first loads return and after the last).  4 x 500 tokens behind 3000 to 6000 places, 8 heads of 128 over 2: 77 + 9 us; the products alone
-// would take 22, and those of the probabilities' second term half as much; a wavefront's products, exponentials and LDS reads follow one another.  One
-// sequence of 2000 places: 7 + 4 us, two launches of few workgroups.
+// would take 22, and those of the probabilities' second term half as much.  CUs are busy 63 % of the time, with one and a half wavefronts a SIMD then (LDS and
+// registers have room for two): workgroups differ in what they have to do, and are dealt in one round.  While it is busy, a wavefront's products,
+// exponentials and LDS reads follow one another (matrix pipes 24 % of the time, vector units 24, LDS 20).  One sequence of 2000 places: 7 + 3 us,
+// two launches of few workgroups.
 #include "../../include/nm_paged_attention.h"
 #include "token_ops.h"
 
@@ -232,7 +234,8 @@ __global__ __launch_bounds__(kWaves * 64) void paged_few_kernel(Paged a)
         Frag p[NC][2];  // bfloat16: the probabilities and what their rounding leaves; float: of the two blocks
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            // (as plain floats: elements of a matrix result that are changed under a branch come out wrong from this compiler)
+            // (as plain floats: with ROCm 7.2's compiler a form that set elements of the matrix result under the branch gave wrong outputs in the tests of
+            // masked tiles; why was not found)
             float z[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = s[n][j >> 2][j & 3];
@@ -750,10 +753,10 @@ Plan plan_of(int B, int H, int Hkv, int D, int U, int page_size, int max_pages, 
     p.blocks = columns > 16 ? 2 : 1;
     const int of_group = p.many ? kManyColumns : 16 * p.blocks, of_round = p.many ? kManyTile : kTile * kWaves;
     p.col_tiles = (int)((columns + of_group - 1) / of_group);
-    // workgroups share a token's places where there are fewer than two a CU (of few columns: one; two 49 us instead of 46 for 32 sequences of
-    // 4000 to 8000 places, one of many columns 83 instead of 64 for chunks of 500 tokens), but look at two rounds of places at least.  (Shares of equal size
-    // whatever the sequences' lengths, which every workgroup and every row of the join has to find: 32 sequences of 4000 to 8000 places the same,
-    // those chunks 71 us and 31 for the join against 63 and 17 then.)
+    // workgroups share a token's places where there are fewer than two a CU, of few columns one (two 47 us instead of 45 for 32 sequences of
+    // 4000 to 8000 places; of many columns one a CU 100 + 7 us for chunks of 500 tokens behind 3000 to 6000 places, two 78 + 9, four 82 + 17; chunks of 200 of
+    // two sequences 24 + 4, 24 + 7, 24 + 10), but look at two rounds of places at least.  The shares are those of the longest sequence that
+    // there may be and of all U tokens: shorter sequences have shorter ones, and columns behind q_lengths workgroups without work.
     const long long groups = (long long)B * Hkv * p.col_tiles, rounds = (room + of_round - 1) / of_round, wanted = p.many ? 512 : 256;
     long long splits = wanted / groups;
     if (splits > rounds / 2) splits = rounds / 2;

@@ -13,9 +13,9 @@
 //
 // Backward: element by element from the saved lse and entropy, a thread on the same eight places of every so many classes.
 //
-// Measured: 32 x 150 places of 5000 classes, four alternatives, bfloat16: 18 + 8 us; the scores that count, 36 MB, would take 7.  The vector units
-// are busy a third of the time (an exponential, a maximum and two sums a score), and the join reads 32 lines of memory a place again.  16 single
-// places of 32000 classes, eight alternatives, float32: 11 + 5 us, chains of exchanges between lanes.  Backward of 16 x 333 places of 5000
+// Measured: 32 x 150 places of 5000 classes, four alternatives, bfloat16: 19 + 8 us; the scores that count, 36 MB, would take 7.  The vector units
+// are busy 38 % of the time (an exponential, a maximum and two sums a score), and the join reads 32 lines of memory a place again.  16 single
+// places of 32000 classes, eight alternatives, float32: 11 + 6 us, chains of exchanges between lanes.  Backward of 16 x 333 places of 5000
 // classes, float32 to bfloat16: 37 us for 160 MB, 4.3 TB/s.
 #include "../../include/nm_token_scores.h"
 #include "token_ops.h"
@@ -359,13 +359,14 @@ struct Plan {
 Plan plan_of(int B, int V, int U, int top)
 {
     Plan p = {};
-    // places side by side: as many as there are, and of long rows 32 where the last 64 would be less than half full (32 x 150 places: 27 us for both
-    // launches, 29 with 64), but not from 2^24 places on: a lane's first class lies up to 16 rows behind a wavefront's, in bytes of 32 bits
+    // places side by side: as many as there are, and of long rows 32 where the last 64 would be less than half full (32 items of 5000 classes, four
+    // alternatives, both launches: 65 places 20 us against 22 with 64, 150 27 against 29, 280 41 against 42, 800 99 against 97; 4 x 150 places of 32000 classes
+    // 26 against 32; 32 x 150 of 1000, eight alternatives, 21 against 22), but not from 2^24 places on: a lane's first class lies up to 16 rows behind a wavefront's, in bytes of 32 bits
     while (p.log_lanes < 6 && (1 << p.log_lanes) < U) ++p.log_lanes;
     if (U > 32 && U < 1 << 24 && U % 64 > 0 && U % 64 <= 32) p.log_lanes = 5;
     const int lanes = 1 << p.log_lanes, step = 64 >> p.log_lanes, list = list_of(top);
     p.u_tiles = (U + lanes - 1) / lanes;
-    // four workgroups a CU (32 x 150 places of 5000 classes 18.3 us, with two 20.6), but a wavefront has a whole round of classes to do, and a
+    // four workgroups a CU (32 items of 5000 classes, both launches: 65 places 20.0 us, with two a CU 19.7, 90 21 and 20, 150 27 and 28, 280 41 and 53), but a wavefront has a whole round of classes to do, and a
     // wavefront joins all lists of a place
     const long long groups = (long long)B * p.u_tiles;
     long long splits = 1024 / groups;
